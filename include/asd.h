@@ -37,7 +37,8 @@ extern "C" {
 
 enum { ASD_OK = 0, ASD_E_INVAL = -1, ASD_E_STATE = -2, ASD_E_NOMEM = -3, ASD_E_IO = -4, ASD_E_HIP = -5 };
 
-enum { ASD_DT_F32 = 0, ASD_DT_BF16 = 1 };
+enum { ASD_DT_F32 = 0, ASD_DT_BF16 = 1,
+       ASD_DT_FP8 = 2 /* 8-bit caches of the operators over several sequences only (asd_kv_shape) */ };
 
 /* Tensor identifiers for asd_set_weight / asd_get_weight. */
 enum {
@@ -185,7 +186,7 @@ size_t asd_arena_bytes(const asd_config* cfg);
 int asd_create(const asd_config* cfg, void* device_arena, size_t arena_bytes, void* hip_stream, asd_engine** out);
 void asd_destroy(asd_engine* e);
 
-/* Message of the last failing call on this engine (or of the last failing asd_create when e is NULL). */
+/* Message of the last failing call on this engine (when e is NULL: of the last failing asd_create or operator call without an engine on this thread). */
 const char* asd_last_error(const asd_engine* e);
 
 /*
@@ -381,6 +382,108 @@ typedef struct {
     int32_t tile[4], slices[4];
 } asd_prompt_block;
 int asd_plan_prompt(const asd_config* cfg, int32_t n, int32_t block, asd_prompt_block* out);
+
+/*
+ * Operators over a paged cache of several sequences, for programs that bring their own batch: new rows are prepared and
+ * written (asd_kv_append), attend to all that their sequence holds (asd_kv_attend), and can be read back as values
+ * (asd_kv_read).  They need no engine: every pointer is DEVICE memory of the current device unless the comment says
+ * HOST, the calls enqueue on the stream they are given (a hipStream_t, NULL = the default stream), allocate nothing, do not
+ * synchronise, and may be captured into a graph.  The lengths and the page table are read when the kernels run, so a
+ * captured call can be replayed as the sequences grow (up to the bounds it was given).  Refusals (a message in
+ * asd_last_error(NULL)) happen before anything is enqueued.  Calls that work on different rows, pages and workspaces may overlap.
+ *
+ * Rows: the new tokens of all sequences lie packed, sequence s in rows row_start[s] .. row_start[s+1]-1 of q, k, v, out;
+ * rows outside are left as they are.  kv_len[s] counts the tokens of the sequence WITH its new ones: row i of n has
+ * position kv_len[s] - n + i and sees the keys 0 .. position of its own sequence.
+ *
+ * Pages: page p holds page_tokens consecutive tokens of one sequence for all KV heads, asd_kv_page_bytes() bytes.  The j-th
+ * page of sequence s is page_table[s * table_stride + j].  A page is, per KV head, page_tokens / 64 chunks of 64 tokens,
+ * each the chunk's K fragments, then its V^T fragments; a fragment is what a wave of 64 lanes loads at once, 16 bytes a lane
+ * (lane 16g + r), KE values (16 codes, 8 bf16, 4 fp32; D = min(KE, head_dim / 4) values of K):
+ *   K fragment (kt, hp), order kt * head_dim / 4D + hp: key(kt, r) of the chunk, dims hp * 4D + g * D ..
+ *       key(kt, r) = 16kt + r (fp32), 32(kt/2) + 8(r/4) + 4(kt%2) + r%4 (bf16), 16(r/4) + 4kt + r%4 (8 bits)
+ *   V^T fragment (ht, ks), order ht * 16 / KE + ks: dim 16ht + r, keys ks * 4KE + g * KE ..
+ * which for fp32 and bf16 is the engine's own cache of one layer.  An 8-bit cache holds e4m3 codes there and behind them 64
+ * bytes for K and 64 for V, one per token: 127 + e, where e is the least integer (in -100 .. 120; 0 for a row of zeros) with
+ * max|x| * 2^-e <= 448 over that token's finite values of the head; a code is x * 2^-e rounded to nearest even, and stands for
+ * code * 2^e.  A value that is not finite is held as NaN.
+ *
+ * What the arrays hold cannot be refused when a call is made.  Rows and lengths are cut to the bounds, a page outside the pool is
+ * neither written nor read (its keys count as hidden, its rows are not read back), a position past the rotary table takes the
+ * table's last row; each sets a bit in *status, which the caller clears and reads (ASD_KV_BAD_*; optional).
+ */
+enum { ASD_KV_BAD_ROWS = 1,     /* row_start not ascending within 0 .. n_rows, more new rows than max_new or than tokens, kv_len above max_len or the table's reach */
+       ASD_KV_BAD_PAGE = 2,     /* a page outside 0 .. n_pages-1 where a page was needed */
+       ASD_KV_BAD_POS = 4 };    /* a position past the rotary table */
+
+/* Types and widths.  head_dim 32, 64 or 128; n_heads a multiple of n_kv_heads (query head h uses KV head h / (n_heads / n_kv_heads));
+ * page_tokens a multiple of 64; dtype (rows in and out) ASD_DT_F32 or ASD_DT_BF16; kv_dtype the same or ASD_DT_FP8. */
+typedef struct {
+    int32_t n_heads, n_kv_heads, head_dim, page_tokens, dtype, kv_dtype;
+} asd_kv_shape;
+
+/* A batch: pages (16-byte aligned), the arrays described above, and bounds that hold for them: rows of the row buffers,
+ * most new rows of a sequence (1 .. n_rows), most tokens of a sequence (1 .. 2^24).  n_seqs 1 .. 65536. */
+typedef struct {
+    void* pages;
+    const int32_t* page_table;      /* [n_seqs][table_stride] */
+    const int32_t* row_start;       /* [n_seqs + 1] */
+    const int32_t* kv_len;          /* [n_seqs] */
+    int32_t* status;                /* one word, or NULL */
+    int32_t n_pages, table_stride, n_seqs, n_rows, max_new, max_len;
+} asd_kv_batch;
+
+/* Bytes of a page (0: invalid shape). */
+size_t asd_kv_page_bytes(const asd_kv_shape* s);
+
+/*
+ * New rows: queries and keys are normalised per head (x / sqrt(mean x^2 + eps) * gain, where a gain [head_dim] fp32 is given)
+ * and rotated, in fp32, and rounded once: queries into q_out, keys and (unchanged) values into the pages.  The first rot_dim
+ * dims of a head turn (0: none; a multiple of 8): pairs (j, j + rot_dim/2), or (2j, 2j+1) with interleaved != 0, by the angle
+ * whose cosine and sine are rope[(position * rot_dim/2 + j) * 2 ..] (fp32 [rope_positions][rot_dim/2][2]; asd_rope_table makes
+ * such a table).  Strides are in elements from row to row, heads lie packed within a row [heads][head_dim]; pointers
+ * and strides are multiples of 16 bytes.  q and q_out may be NULL (both: keys and values only) and may be the same buffer.
+ */
+typedef struct {
+    const float *q_gain, *k_gain;   /* NULL: no norm */
+    float eps;
+    const float* rope;
+    int32_t rope_positions, rot_dim, interleaved;
+} asd_kv_prep;
+int asd_kv_append(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_prep* p, const void* q, int64_t q_stride, const void* k,
+                  int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t out_stride, void* hip_stream);
+
+/*
+ * Attention of the batch's new rows over their sequences' pages (the new tokens' keys and values are in them already):
+ * out = sum_j softmax_j(scale * q.k_j) v_j over the keys j <= position; zeros for a row that sees no key.  scale > 0.  workspace:
+ * at least asd_kv_attend_workspace() bytes, 256-byte aligned; its contents need not be set and mean nothing afterwards, but no
+ * other work may use it until the call's kernels have run.  A captured call keeps using the workspace it was given.
+ * With 8-bit or bf16 caches and bf16 rows the weights are rounded to bf16 for the product with V; sums are fp32.
+ */
+size_t asd_kv_attend_workspace(const asd_kv_shape* s, const asd_kv_batch* b);
+int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, int64_t q_stride, void* out, int64_t out_stride, float scale,
+                  void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The batch's rows (the last row_start[s+1] - row_start[s] tokens of each sequence) out of the pages, as values in dtype: k_out and v_out
+ * [n_rows][n_kv_heads][head_dim] with a stride; either may be NULL. */
+int asd_kv_read(const asd_kv_shape* s, const asd_kv_batch* b, void* k_out, int64_t k_stride, void* v_out, int64_t v_stride, void* hip_stream);
+
+/*
+ * Rotary table [positions][rot_dim/2][cos, sin] in fp32, computed in double: angle = position * f_j, f_j = theta^(-2j / rot_dim),
+ * changed by `kind` for contexts longer than the trained one (factor >= 1; r = trained * f_j / 2 pi is the number of turns over it):
+ *   ASD_ROPE_PLAIN   f_j as it is
+ *   ASD_ROPE_LINEAR  f_j / factor
+ *   ASD_ROPE_BANDS   f_j where r >= high, f_j / factor where r <= low, in between mixed by (r - low) / (high - low)
+ *   ASD_ROPE_RAMP    mixed by the pair's index j, from f_j at the index that makes `high` turns (rounded down) to f_j / factor at the one that
+ *                    makes `low` turns (rounded up)
+ * gain (0: 1) multiplies cosines and sines.  0 < low < high and trained >= 1 for the last two kinds.
+ */
+enum { ASD_ROPE_PLAIN = 0, ASD_ROPE_LINEAR = 1, ASD_ROPE_BANDS = 2, ASD_ROPE_RAMP = 3 };
+typedef struct {
+    int32_t kind, rot_dim;
+    double theta, factor, low, high, trained, gain;
+} asd_rope;
+int asd_rope_table(const asd_rope* r, int32_t positions, float* table, void* hip_stream);
 
 #ifdef __cplusplus
 }

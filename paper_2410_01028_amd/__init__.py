@@ -15,7 +15,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libasd.so")
 
 OK, E_INVAL, E_STATE, E_NOMEM, E_IO, E_HIP = 0, -1, -2, -3, -4, -5
-DT_F32, DT_BF16 = 0, 1
+DT_F32, DT_BF16, DT_FP8 = 0, 1, 2      # DT_FP8: 8-bit pages of a KVCache only
 MAX_ROWS = 16
 MAX_SEQ = 65536
 # development / test switches of Config.debug_flags (none changes what is computed)
@@ -71,7 +71,27 @@ class KernelTimes(ctypes.Structure):
                 ("ms_total", ctypes.c_double)]
 
 
+class KvShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_heads", "n_kv_heads", "head_dim", "page_tokens", "dtype", "kv_dtype")]
+
+
+class KvBatch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("pages", "page_table", "row_start", "kv_len", "status")] + \
+               [(n, ctypes.c_int32) for n in ("n_pages", "table_stride", "n_seqs", "n_rows", "max_new", "max_len")]
+
+
+class KvPrep(ctypes.Structure):
+    _fields_ = [("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p), ("eps", ctypes.c_float), ("rope", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int32) for n in ("rope_positions", "rot_dim", "interleaved")]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("rot_dim", ctypes.c_int32)] + \
+               [(n, ctypes.c_double) for n in ("theta", "factor", "low", "high", "trained", "gain")]
+
+
 _lib = None
+_kv_ready = False
 
 
 def lib():
@@ -117,6 +137,25 @@ def lib():
         L.asd_time_step_class.argtypes = [vp, i32, i32, i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)]
         _lib = L
     return _lib
+
+
+def _kv_lib():
+    """The library with the signatures of the operators over a KVCache."""
+    global _kv_ready
+    L = lib()
+    if not _kv_ready:
+        vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+        shape, batch, prep = ctypes.POINTER(KvShape), ctypes.POINTER(KvBatch), ctypes.POINTER(KvPrep)
+        L.asd_kv_page_bytes.restype = sz
+        L.asd_kv_page_bytes.argtypes = [shape]
+        L.asd_kv_append.argtypes = [shape, batch, prep, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+        L.asd_kv_attend_workspace.restype = sz
+        L.asd_kv_attend_workspace.argtypes = [shape, batch]
+        L.asd_kv_attend.argtypes = [shape, batch, vp, i64, vp, i64, ctypes.c_float, vp, sz, vp]
+        L.asd_kv_read.argtypes = [shape, batch, vp, i64, vp, i64, vp]
+        L.asd_rope_table.argtypes = [ctypes.POINTER(Rope), i32, vp, vp]
+        _kv_ready = True
+    return L
 
 
 def make_config(shape, max_seq: int, page_tokens: int = 64, max_rows: int = MAX_ROWS, debug_flags: int = 0,
@@ -382,3 +421,182 @@ class Engine:
         ms = ctypes.c_double()
         self._ck(lib().asd_copy_bench(self._h, nbytes, reps, ctypes.byref(ms)))
         return ms.value
+
+
+# ---------------------------------------------------------------- operators over a paged cache of several sequences
+def _kv_ck(rc: int):
+    if rc:
+        raise AsdError(rc, lib().asd_last_error(None).decode())
+
+
+def kv_page_bytes(n_heads: int, n_kv_heads: int, head_dim: int, page_tokens: int, dtype: int = DT_BF16, kv_dtype: int = DT_FP8) -> int:
+    """Bytes of one page of a KVCache (asd_kv_page_bytes)."""
+    n = int(_kv_lib().asd_kv_page_bytes(ctypes.byref(KvShape(n_heads, n_kv_heads, head_dim, page_tokens, dtype, kv_dtype))))
+    if n == 0:
+        raise AsdError(E_INVAL, "invalid cache shape")
+    return n
+
+
+class _OnDevice:
+    """Makes a tensor's device the current one for the time of a call."""
+
+    def __init__(self, device):
+        import torch
+        self._torch, self._index = torch, device.index
+
+    def __enter__(self):
+        self._before = self._torch.cuda.current_device()
+        if self._before != self._index:
+            self._torch.cuda.set_device(self._index)
+        return self._torch.cuda.current_stream(self._index).cuda_stream
+
+    def __exit__(self, *exc):
+        if self._before != self._index:
+            self._torch.cuda.set_device(self._before)
+
+
+class KVBatch:
+    """New rows of several sequences (asd_kv_batch): int32 device tensors page_table [n_seqs, pages], row_start [n_seqs + 1],
+    kv_len [n_seqs] (tokens with the new ones), and the bounds that hold for them: rows of the row buffers, most new rows
+    and most tokens of a sequence.  The tensors are read when a call's kernels run: update them in place between calls.
+    status: an int32 word on the device that kernels set bits of where the arrays held something out of range; check() reads it."""
+
+    def __init__(self, page_table, row_start, kv_len, n_rows: int, max_new: int, max_len: int):
+        import torch
+        for name, t, dims in (("page_table", page_table, 2), ("row_start", row_start, 1), ("kv_len", kv_len, 1)):
+            if t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous() or t.device != kv_len.device:
+                raise AsdError(E_INVAL, f"{name} must be a contiguous int32 tensor of {dims} dimension(s) on the batch's device")
+        if kv_len.device.type != "cuda":
+            raise AsdError(E_INVAL, "the batch's tensors must be on the GPU")
+        n = kv_len.numel()
+        if row_start.numel() != n + 1 or page_table.shape[0] != n:
+            raise AsdError(E_INVAL, "page_table, row_start and kv_len must be of n_seqs, n_seqs + 1 and n_seqs sequences")
+        self.page_table, self.row_start, self.kv_len, self.device = page_table, row_start, kv_len, kv_len.device
+        self.n_rows, self.max_new, self.max_len = n_rows, max_new, max_len
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._c = KvBatch(None, page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr(), self.status.data_ptr(), 0,
+                          page_table.shape[1], n, n_rows, max_new, max_len)
+
+    def check(self):
+        """Synchronise and raise if a kernel found the arrays out of range since the last check."""
+        bits = int(self.status.item())
+        if bits:
+            self.status.zero_()
+            names = [n for b, n in ((1, "rows or lengths"), (2, "pages"), (4, "positions past the rotary table")) if bits & b]
+            raise AsdError(E_INVAL, "batch out of range: " + ", ".join(names))
+
+
+class KVCache:
+    """Pages of a paged cache for several sequences: pages is a uint8 device tensor of n_pages * kv_page_bytes(...) bytes, which the
+    caller owns.  The calls enqueue on the current stream of its device and return without synchronising; asd.h has
+    the layout and what each call does."""
+
+    def __init__(self, pages, n_heads: int, n_kv_heads: int, head_dim: int, page_tokens: int, dtype: int = DT_BF16, kv_dtype: int = DT_FP8):
+        import torch
+        each = kv_page_bytes(n_heads, n_kv_heads, head_dim, page_tokens, dtype, kv_dtype)
+        if pages.dtype != torch.uint8 or not pages.is_contiguous() or pages.device.type != "cuda" or pages.numel() == 0 or pages.numel() % each:
+            raise AsdError(E_INVAL, f"pages must be a contiguous uint8 tensor on the GPU, a multiple of {each} bytes")
+        self.pages, self.device, self.n_pages = pages, pages.device, pages.numel() // each
+        self.n_heads, self.n_kv_heads, self.head_dim = n_heads, n_kv_heads, head_dim
+        self.torch_dtype = torch.bfloat16 if dtype == DT_BF16 else torch.float32
+        self._shape = KvShape(n_heads, n_kv_heads, head_dim, page_tokens, dtype, kv_dtype)
+        self._torch = torch
+
+    def _batch(self, batch: KVBatch) -> KvBatch:
+        if batch.device != self.device:
+            raise AsdError(E_INVAL, "the batch is on another device than the pages")
+        b = KvBatch.from_buffer_copy(batch._c)
+        b.pages, b.n_pages = self.pages.data_ptr(), self.n_pages
+        return b
+
+    def _rows(self, name: str, t, batch: KVBatch, heads: int):
+        """(pointer, row stride) of a buffer of rows [>= n_rows, heads, head_dim]; heads packed."""
+        if t.dtype != self.torch_dtype or t.device != self.device:
+            raise AsdError(E_INVAL, f"{name} must be {self.torch_dtype} on {self.device}")
+        if t.dim() != 3 or t.shape[0] < batch.n_rows or t.shape[1] != heads or t.shape[2] != self.head_dim:
+            raise AsdError(E_INVAL, f"{name} must be [{batch.n_rows}, {heads}, {self.head_dim}]")
+        s = t.stride()
+        if s[2] != 1 or (heads > 1 and s[1] != self.head_dim):
+            raise AsdError(E_INVAL, f"{name}: the heads of a row must lie packed")
+        return t.data_ptr(), s[0] if batch.n_rows > 1 else max(s[0], heads * self.head_dim)
+
+    def _floats(self, name: str, t, shape):
+        if t.dtype != self._torch.float32 or t.device != self.device or not t.is_contiguous() or t.dim() != len(shape) or \
+                any(w is not None and n != w for n, w in zip(t.shape, shape)):
+            raise AsdError(E_INVAL, f"{name} must be a contiguous float32 tensor {list(shape)} on {self.device}")
+        return t.data_ptr()
+
+    def append(self, batch: KVBatch, q, k, v, q_out=None, rope=None, rot_dim: int = 0, interleaved: bool = False, q_gain=None, k_gain=None,
+               eps: float = 1e-5):
+        """Write the batch's new rows into the pages (asd_kv_append): q [n_rows, n_heads, head_dim] or None, k and v
+        [n_rows, n_kv_heads, head_dim]; rope [positions, rot_dim / 2, 2] as rope_table makes it, gains [head_dim].  Returns the
+        prepared queries (q_out, which may be q; a new tensor if it is not given)."""
+        b, prep = self._batch(batch), KvPrep(None, None, eps, None, 0, rot_dim, int(interleaved))
+        if q is None and q_out is not None:
+            raise AsdError(E_INVAL, "q_out without q")
+        if q is not None and q_out is None:
+            q_out = self._torch.empty((q.shape[0], self.n_heads, self.head_dim), dtype=self.torch_dtype, device=self.device)
+        if rope is not None:
+            prep.rope, prep.rope_positions = self._floats("rope", rope, (None, rot_dim // 2, 2)), rope.shape[0]
+        if q_gain is not None:
+            prep.q_gain = self._floats("q_gain", q_gain, (self.head_dim,))
+        if k_gain is not None:
+            prep.k_gain = self._floats("k_gain", k_gain, (self.head_dim,))
+        qp = self._rows("q", q, batch, self.n_heads) if q is not None else (None, 0)
+        op = self._rows("q_out", q_out, batch, self.n_heads) if q is not None else (None, 0)
+        kp, vp = self._rows("k", k, batch, self.n_kv_heads), self._rows("v", v, batch, self.n_kv_heads)
+        with _OnDevice(self.device) as stream:
+            _kv_ck(_kv_lib().asd_kv_append(self._shape, b, prep, *qp, *kp, *vp, *op, stream))
+        return q_out
+
+    def attend(self, batch: KVBatch, q, out=None, scale: float | None = None, workspace=None):
+        """Causal attention of the batch's new rows over their sequences' pages (asd_kv_attend); q and out [n_rows, n_heads, head_dim],
+        scale 1 / sqrt(head_dim) by default.  workspace: a uint8 tensor of attend_workspace(batch) bytes (by default one of the call's own)."""
+        b = self._batch(batch)
+        if out is None:
+            out = self._torch.empty((q.shape[0], self.n_heads, self.head_dim), dtype=self.torch_dtype, device=self.device)
+        qp, op = self._rows("q", q, batch, self.n_heads), self._rows("out", out, batch, self.n_heads)
+        L = _kv_lib()
+        need = L.asd_kv_attend_workspace(self._shape, b)
+        with _OnDevice(self.device) as stream:
+            if workspace is None and need:
+                workspace = self._torch.empty(need, dtype=self._torch.uint8, device=self.device)
+            elif workspace is not None and (workspace.device != self.device or workspace.dtype != self._torch.uint8 or not workspace.is_contiguous()):
+                raise AsdError(E_INVAL, f"workspace must be a contiguous uint8 tensor on {self.device}")
+            wp, wn = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+            _kv_ck(L.asd_kv_attend(self._shape, b, *qp, *op, self.head_dim ** -0.5 if scale is None else scale, wp, wn, stream))
+        return out
+
+    def attend_workspace(self, batch: KVBatch) -> int:
+        """Bytes of workspace that attend() of a batch with these bounds needs."""
+        return int(_kv_lib().asd_kv_attend_workspace(self._shape, self._batch(batch)))
+
+    def read(self, batch: KVBatch, k_out=None, v_out=None):
+        """The batch's rows out of the pages as values (asd_kv_read): (k, v) [n_rows, n_kv_heads, head_dim]; new tensors where none is given."""
+        b, out = self._batch(batch), []
+        for name, t in (("k_out", k_out), ("v_out", v_out)):
+            t = self._torch.empty((batch.n_rows, self.n_kv_heads, self.head_dim), dtype=self.torch_dtype, device=self.device) if t is None else t
+            out.append((t, self._rows(name, t, batch, self.n_kv_heads)))
+        with _OnDevice(self.device) as stream:
+            _kv_ck(_kv_lib().asd_kv_read(self._shape, b, *out[0][1], *out[1][1], stream))
+        return out[0][0], out[1][0]
+
+
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3
+
+
+def rope_table(rot_dim: int, positions: int, theta: float = 10000.0, kind: int = ROPE_PLAIN, factor: float = 1.0, low: float = 1.0, high: float = 32.0,
+               trained: float = 4096.0, gain: float = 1.0, device: str = "cuda:0"):
+    """Rotary table [positions, rot_dim / 2, 2] for KVCache.append (asd_rope_table), enqueued on the device's current stream."""
+    import torch
+    device = torch.device(device)
+    if device.type != "cuda":
+        raise AsdError(E_INVAL, "the table is made on the GPU")
+    if device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    if positions < 1 or rot_dim < 2:
+        raise AsdError(E_INVAL, "asd_rope_table: positions and rot_dim must be positive")
+    with _OnDevice(device) as stream:
+        out = torch.empty((positions, rot_dim // 2, 2), dtype=torch.float32, device=device)
+        _kv_ck(_kv_lib().asd_rope_table(Rope(kind, rot_dim, theta, factor, low, high, trained, gain), positions, out.data_ptr(), stream))
+    return out

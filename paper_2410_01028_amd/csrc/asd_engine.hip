@@ -1305,6 +1305,9 @@ int asd_plan_prompt(const asd_config* cfg, int32_t n, int32_t block, asd_prompt_
     return ASD_OK;
 }
 
+// Message of a failing call that has no engine (the operators of asd_kv.hip), for asd_last_error(NULL)
+extern "C++" __attribute__((visibility("hidden"))) void asd_note_error(const char* message) { g_create_error = message; }
+
 const char* asd_last_error(const asd_engine* e) { return e ? e->err.c_str() : g_create_error.c_str(); }
 
 int asd_create(const asd_config* cfg, void* device_arena, size_t arena_bytes, void* hip_stream, asd_engine** out) {

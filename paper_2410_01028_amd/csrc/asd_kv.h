@@ -1,0 +1,807 @@
+// Operators over a paged cache of several sequences: new rows prepared and written into the pages (asd_kv_append), causal
+// attention of the new rows over them (asd_kv_attend), rows read back (asd_kv_read), rotary tables (asd_rope_table).
+//
+// A page holds, per KV head, page_tokens / 64 chunks of 64 tokens: the chunk's K fragments, then its V^T fragments, in the
+// layout of the engine's own cache (asd_common.h), so that for fp32 and bf16 a layer of an engine is such a set of pages.
+// The 8-bit cache keeps e4m3 codes in the same scheme with 16 codes to a 16-byte piece, and behind the fragments one byte
+// per token for K and one for V: 127 + the exponent of that token's scale.  Scales are powers of two: scaling a value
+// before its one rounding is exact, and a code times its scale is exactly a bf16 number, so that what the attention
+// multiplies is the stored value itself; a floating-point code loses nothing to a scale that is up to 2x too large.
+#pragma once
+#include "asd_common.h"
+
+// e4m3 codes (cache only); 16 to a lane's piece
+struct FP8 {
+    using elem = uint8_t;
+    static constexpr int KE = 16;
+};
+// keys of a score tile as for the other types: the four tiles' registers of lane group g are keys 16g .. 16g + 15
+template <> __device__ __forceinline__ int score_key<FP8>(int kt, int r) { return 16 * (r >> 2) + 4 * kt + (r & 3); }
+template <> __host__ __device__ __forceinline__ void score_tile_of<FP8>(int key, int* kt, int* r) { *kt = (key >> 2) & 3; *r = 4 * (key >> 4) + (key & 3); }
+
+// Layout of a chunk of cache type C at head dim H
+template <class C, int H> struct KvLayout {
+    using E = typename C::elem;
+    static constexpr bool Q8 = sizeof(E) == 1;
+    static constexpr int KV = C::KE;                                     // keys of a V^T piece (16 bytes)
+    static constexpr int KK = C::KE < H / 4 ? C::KE : H / 4;             // dims of a K piece (8 bytes for codes at H = 32, else 16)
+    static constexpr int HP = H / (4 * KK), HT = H / 16, KST = 64 / (4 * KV);
+    static constexpr int K_BYTES = 64 * H * (int)sizeof(E);
+    static constexpr int CHUNK = 2 * K_BYTES + (Q8 ? 128 : 0);
+    static __device__ __forceinline__ int k_off(int key, int dim) {      // byte offsets of one element (key of the chunk)
+        int kt, r;
+        score_tile_of<C>(key, &kt, &r);
+        return (((kt * HP + dim / (4 * KK)) * 64 + ((dim / KK) & 3) * 16 + r) * KK + dim % KK) * (int)sizeof(E);
+    }
+    static __device__ __forceinline__ int v_off(int key, int dim) {
+        return K_BYTES + (((dim / 16 * KST + key / (4 * KV)) * 64 + ((key / KV) & 3) * 16 + dim % 16) * KV + key % KV) * (int)sizeof(E);
+    }
+};
+
+struct KvArgs {
+    char* pages;
+    const int32_t *table, *row_start, *kv_len;
+    int32_t* status;
+    int32_t n_pages, table_stride, n_seqs, n_rows, max_new, cap;        // cap: most tokens a sequence can have (max_len, the table's reach)
+    int32_t n_h, n_kv, group, page_tokens;
+};
+
+// One sequence's rows and length, held inside the buffers whatever the arrays say
+struct KvSeq { int r0, n, len; };
+__device__ __forceinline__ KvSeq kv_seq(const KvArgs& a, int s, bool* bad = nullptr) {
+    const int f0 = a.row_start[s], f1 = a.row_start[s + 1], fl = a.kv_len[s];
+    KvSeq v;
+    v.r0 = min(max(f0, 0), a.n_rows);
+    v.n = min(min(max(f1, v.r0), a.n_rows) - v.r0, a.max_new);
+    v.len = min(max(fl, 0), a.cap);
+    if (bad) *bad = v.r0 != f0 || v.r0 + v.n != f1 || v.len != fl || v.n > v.len;
+    return v;
+}
+__device__ __forceinline__ void kv_flag(const KvArgs& a, int bit) { if (a.status) atomicOr(a.status, bit); }
+// every sequence's arrays, by one wave
+__device__ __forceinline__ void kv_check_all(const KvArgs& a, int lane) {
+    if (!a.status) return;
+    for (int s = lane; s < a.n_seqs; s += 64) {
+        bool bad;
+        kv_seq(a, s, &bad);
+        if (bad) kv_flag(a, ASD_KV_BAD_ROWS);
+    }
+}
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Work items of all sequences one behind the other: count(sequence) items each.  Finds the sequence of `item` and its
+// number within it; a wave looks at 64 sequences at a time, so no list has to be built in a launch of its own.
+template <class F>
+__device__ __forceinline__ bool kv_find(const KvArgs& a, int64_t item, int lane, F count, int* seq, int* local, int64_t* first, KvSeq* view) {
+    int64_t base = 0;
+    for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
+        KvSeq v{0, 0, 0};
+        int c = 0;
+        if (s0 + lane < a.n_seqs) { v = kv_seq(a, s0 + lane); c = count(v); }
+        int incl = c;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) { const int t = __shfl_up(incl, o); if (lane >= o) incl += t; }
+        const int total = uniform(__shfl(incl, 63));
+        if (item < base + total) {
+            const int l = __ffsll((unsigned long long)__ballot(base + incl > item)) - 1;
+            *seq = uniform(s0 + l);
+            *first = base + uniform(__shfl(incl - c, l));
+            *local = (int)(item - *first);
+            *view = KvSeq{uniform(__shfl(v.r0, l)), uniform(__shfl(v.n, l)), uniform(__shfl(v.len, l))};
+            return true;
+        }
+        base += total;
+    }
+    return false;
+}
+// Chunk c of a sequence for one KV head; null where the page table holds no page of the pool
+template <class C, int H>
+__device__ __forceinline__ const char* kv_chunk(const KvArgs& a, int seq, int c, int kvh) {
+    const int per = a.page_tokens / 64, page = a.table[(size_t)seq * a.table_stride + c / per];
+    if ((unsigned)page >= (unsigned)a.n_pages) return nullptr;
+    return a.pages + (((size_t)page * a.n_kv + kvh) * per + c % per) * KvLayout<C, H>::CHUNK;
+}
+
+// ---- 8-bit values
+// exponent of the scale: the least e with top * 2^-e <= 448 = 1.75 * 2^8 (0 for top = 0), held in a range whose powers are normal numbers
+__device__ __forceinline__ int q8_exponent(float top) {
+    const uint32_t u = __float_as_uint(top);
+    const int e = (int)(u >> 23) - 127 - ((u & 0x7fffffu) <= 0x600000u ? 8 : 7);
+    return top == 0.f ? 0 : min(max(e, -100), 120);
+}
+__device__ __forceinline__ float q8_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+// four values as codes; what is not finite becomes the code of NaN (the format has no infinity)
+__device__ __forceinline__ uint32_t q8_pack(const float (&v)[4], float inv) {
+    float x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = finite(v[j]) ? v[j] * inv : __uint_as_float(0x7fc00000u);
+    int p = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+    p = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], p, true);
+    return (uint32_t)p;
+}
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+
+// A matrix-core operand register of activation type A out of step u of a piece of cache type C (codes: times `scale`)
+template <class A, class C> __device__ __forceinline__ u32x4 kv_operand(const u32x4& piece, int u, float scale) {
+    if constexpr (sizeof(typename C::elem) > 1) {
+        return piece;
+    } else if constexpr (A::KE == 8) {
+        u32x4 r;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            r[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(piece[2 * u + w], scale, false));
+            r[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(piece[2 * u + w], scale, true));
+        }
+        return r;
+    } else {
+        const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(piece[u], scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(piece[u], scale, true);
+        return u32x4{__float_as_uint(lo[0]), __float_as_uint(lo[1]), __float_as_uint(hi[0]), __float_as_uint(hi[1])};
+    }
+}
+// four consecutive elements of a row
+template <class T> __device__ __forceinline__ void load4(const typename T::elem* p, float (&v)[4]);
+template <> __device__ __forceinline__ void load4<F32>(const float* p, float (&v)[4]) {
+    const float4 x = *(const float4*)p;
+    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+}
+template <> __device__ __forceinline__ void load4<BF16>(const uint16_t* p, float (&v)[4]) {
+    const uint2 x = *(const uint2*)p;
+    v[0] = __uint_as_float(x.x << 16); v[1] = __uint_as_float(x.x & 0xffff0000u);
+    v[2] = __uint_as_float(x.y << 16); v[3] = __uint_as_float(x.y & 0xffff0000u);
+}
+template <class T> __device__ __forceinline__ void store4(typename T::elem* p, const float (&v)[4]) {
+    if constexpr (sizeof(typename T::elem) == 4) *(float4*)p = float4{v[0], v[1], v[2], v[3]};
+    else *(uint2*)p = uint2{T::from_f32(v[0]) | ((uint32_t)T::from_f32(v[1]) << 16), T::from_f32(v[2]) | ((uint32_t)T::from_f32(v[3]) << 16)};
+}
+
+// ---------------------------------------------------------------- new rows into the cache
+struct KvAppendArgs {
+    KvArgs kv;
+    const void *q, *k, *v;
+    void* q_out;
+    int64_t q_stride, k_stride, v_stride, out_stride;
+    const float *q_gain, *k_gain, *rope;
+    float eps;
+    int32_t rope_positions, rot, interleaved;
+    int32_t kv_heads_per, q_heads_per, kv_blocks;      // heads of a workgroup; grid rows 0 .. kv_blocks-1 take K and V, the others q
+};
+
+// A head's vector lies in H / 8 lanes, two units of four dims each, chosen so that both partners of every rotated pair are
+// in one lane: neighbours (interleaved), or dims 4p .. 4p+3 and those rot/2 further on (half layout), the dims behind the
+// rotated part after them.  The norm's sum of squares runs over the lanes by shuffles.
+template <class T, int H> struct HeadVec {
+    float x[2][4];
+    int d[2];                                          // first dims of the units
+    __device__ __forceinline__ void place(int p, int rot, bool inter) {
+        const bool pair = !inter && 8 * p < rot;
+        d[0] = pair ? 4 * p : 8 * p;
+        d[1] = pair ? rot / 2 + 4 * p : 8 * p + 4;
+    }
+    __device__ __forceinline__ void load(const typename T::elem* row) { load4<T>(row + d[0], x[0]); load4<T>(row + d[1], x[1]); }
+    __device__ __forceinline__ void normalise(const float* gain, float eps) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s += x[i][j] * x[i][j];
+#pragma unroll
+        for (int o = 1; o < H / 8; o <<= 1) s += __shfl_xor(s, o);
+        const float r = 1.f / sqrtf(s * (1.f / H) + eps);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float4 g = *(const float4*)(gain + d[i]);
+            x[i][0] *= r * g.x; x[i][1] *= r * g.y; x[i][2] *= r * g.z; x[i][3] *= r * g.w;
+        }
+    }
+    // cs: (cos, sin) of the position's angles 4p .. 4p+3
+    __device__ __forceinline__ void rotate(const float* cs, bool inter) {
+        const float4 t0 = ((const float4*)cs)[0], t1 = ((const float4*)cs)[1];
+        const float c[4] = {t0.x, t0.z, t1.x, t1.z}, s[4] = {t0.y, t0.w, t1.y, t1.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float& a = inter ? x[j >> 1][(j & 1) * 2] : x[0][j];
+            float& b = inter ? x[j >> 1][(j & 1) * 2 + 1] : x[1][j];
+            const float a1 = a * c[j] - b * s[j], b1 = b * c[j] + a * s[j];
+            a = a1; b = b1;
+        }
+    }
+};
+
+// A workgroup takes up to 16 tokens of one sequence (a tile at positions 16t .. 16t+15, so that a V^T piece belongs to one
+// workgroup) and some heads.  Bound by memory: every row is read once, in 8- or 16-byte pieces that fill their lines, and held
+// in registers from the load to the store.  V goes through LDS to be transposed; a piece all of whose keys are new is
+// written whole, one at the edge of the new rows element by element, so that what the cache holds beside them stays.
+template <class T, class C, int H>
+__global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
+    using L = KvLayout<C, H>;
+    using E = typename T::elem;
+    constexpr int LPV = H / 8, VPP = 256 / LPV;        // lanes of a vector, vectors of a pass
+    __shared__ __align__(16) typename C::elem vt[16][H];
+    const int tid = threadIdx.x, lane = tid & 63;
+    int seq, tile;
+    int64_t first;
+    KvSeq s;
+    auto tiles = [](const KvSeq& v) { const int p0 = max(v.len - v.n, 0); return v.n > 0 && v.len > 0 ? (v.len + 15) / 16 - p0 / 16 : 0; };
+    if (blockIdx.x == 0 && blockIdx.y == 0 && tid < 64) kv_check_all(a.kv, lane);
+    if (!kv_find(a.kv, blockIdx.x, lane, tiles, &seq, &tile, &first, &s)) return;
+    const int base = s.len - s.n;                      // position of row 0 (negative: rows in front have no place)
+    const int t16 = max(base, 0) / 16 + tile;
+    const int lo = max(max(base, 0), 16 * t16), hi = min(s.len, 16 * t16 + 16), nt = hi - lo;
+    const bool inter = a.interleaved != 0;
+    const int vec = tid / LPV, p = tid % LPV;
+    auto angles = [&](int pos) {
+        if (pos >= a.rope_positions) kv_flag(a.kv, ASD_KV_BAD_POS);
+        return a.rope + ((size_t)min(pos, a.rope_positions - 1) * (a.rot / 2) + 4 * p) * 2;
+    };
+    if ((int)blockIdx.y >= a.kv_blocks) {              // queries
+        const int h0 = ((int)blockIdx.y - a.kv_blocks) * a.q_heads_per, nh = min(a.q_heads_per, a.kv.n_h - h0);
+        for (int i = vec; i < nh * nt; i += VPP) {     // (the lanes of a vector take the same turns)
+            const int head = h0 + i % nh, pos = lo + i / nh;
+            const int64_t row = s.r0 + pos - base;
+            HeadVec<T, H> x;
+            x.place(p, a.rot, inter);
+            x.load((const E*)a.q + row * a.q_stride + head * H);
+            if (a.q_gain) x.normalise(a.q_gain, a.eps);
+            if (8 * p < a.rot) x.rotate(angles(pos), inter);
+            E* out = (E*)a.q_out + row * a.out_stride + head * H;
+            store4<T>(out + x.d[0], x.x[0]);
+            store4<T>(out + x.d[1], x.x[1]);
+        }
+        return;
+    }
+    char* chunk0 = (char*)kv_chunk<C, H>(a.kv, seq, t16 / 4, 0);
+    if (!chunk0) { if (tid == 0) kv_flag(a.kv, ASD_KV_BAD_PAGE); return; }
+    const size_t head_bytes = (size_t)(a.kv.page_tokens / 64) * L::CHUNK;
+    const int h0 = blockIdx.y * a.kv_heads_per, nh = min(a.kv_heads_per, a.kv.n_kv - h0);
+    const int slots = nh * nt;                         // at most 16
+    for (int i = vec; i < 2 * slots; i += VPP) {       // K of all slots, then V
+        const bool isv = i >= slots;
+        const int slot = isv ? i - slots : i, head = h0 + slot / nt, pos = lo + slot % nt, key = pos & 63;
+        const int64_t row = s.r0 + pos - base;
+        HeadVec<T, H> x;
+        x.place(p, a.rot, inter);
+        x.load(isv ? (const E*)a.v + row * a.v_stride + head * H : (const E*)a.k + row * a.k_stride + head * H);
+        if (!isv) {
+            if (a.k_gain) x.normalise(a.k_gain, a.eps);
+            if (8 * p < a.rot) x.rotate(angles(pos), inter);
+        }
+        char* chunk = chunk0 + head * head_bytes;
+        if constexpr (L::Q8) {
+            float top = 0.f;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) top = fmaxf(top, finite(x.x[u][j]) ? fabsf(x.x[u][j]) : 0.f);
+#pragma unroll
+            for (int o = 1; o < LPV; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+            const int e = q8_exponent(top);
+            const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+            const uint32_t c0 = q8_pack(x.x[0], inv), c1 = q8_pack(x.x[1], inv);
+            if (isv) {
+                *(uint32_t*)&vt[slot][x.d[0]] = c0; *(uint32_t*)&vt[slot][x.d[1]] = c1;
+                if (p == 0) *(uint8_t*)(chunk + 2 * L::K_BYTES + 64 + key) = (uint8_t)(e + 127);
+            } else {
+                *(uint32_t*)(chunk + L::k_off(key, x.d[0])) = c0; *(uint32_t*)(chunk + L::k_off(key, x.d[1])) = c1;
+                if (p == 0) *(uint8_t*)(chunk + 2 * L::K_BYTES + key) = (uint8_t)(e + 127);
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                store4<C>(isv ? &vt[slot][x.d[u]] : (typename C::elem*)(chunk + L::k_off(key, x.d[u])), x.x[u]);
+        }
+    }
+    __syncthreads();
+    constexpr int KV = L::KV, PPT = 16 / KV;           // V^T pieces of a dim in the tile
+    for (int i = tid; i < nh * H * PPT; i += 256) {
+        const int dim = i % H, pc = i / H % PPT, hd = i / (H * PPT);
+        const int k0 = 16 * t16 + pc * KV;             // first position of the piece
+        const int b = max(lo, k0), e = min(hi, k0 + KV);
+        if (b >= e) continue;
+        typename C::elem* dst = (typename C::elem*)(chunk0 + (h0 + hd) * head_bytes + L::v_off(k0 & 63, dim));
+        if (e - b == KV) {
+            u32x4 r;
+            typename C::elem* t = (typename C::elem*)&r;
+#pragma unroll
+            for (int j = 0; j < KV; ++j) t[j] = vt[hd * nt + k0 - lo + j][dim];
+            *(u32x4*)dst = r;
+        } else {
+            for (int j = b; j < e; ++j) dst[j - k0] = vt[hd * nt + j - lo][dim];
+        }
+    }
+}
+
+// ---------------------------------------------------------------- rows out of the cache
+struct KvReadArgs {
+    KvArgs kv;
+    void *k_out, *v_out;
+    int64_t k_stride, v_stride;
+};
+// A workgroup takes one chunk of one sequence and KV head, its K or its V: the pieces that hold wanted rows come in as they
+// lie, go through LDS as rows, and leave as rows.
+template <class T, class C, int H>
+__global__ __launch_bounds__(256) void kv_read_kernel(const KvReadArgs a) {
+    using L = KvLayout<C, H>;
+    using E = typename T::elem;
+    using CE = typename C::elem;
+    constexpr int PAD = 16 / (int)sizeof(E);
+    __shared__ __align__(16) E rows[64][H + PAD];
+    const int tid = threadIdx.x, lane = tid & 63, kvh = blockIdx.y;
+    const bool isv = blockIdx.z != 0;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && tid < 64) kv_check_all(a.kv, lane);
+    E* out = (E*)(isv ? a.v_out : a.k_out);
+    if (!out) return;
+    int seq, local;
+    int64_t first;
+    KvSeq s;
+    auto chunks = [](const KvSeq& v) { return v.n > 0 && v.len > 0 ? (v.len + 63) / 64 - max(v.len - v.n, 0) / 64 : 0; };
+    if (!kv_find(a.kv, blockIdx.x, lane, chunks, &seq, &local, &first, &s)) return;
+    const int base = s.len - s.n, c = max(base, 0) / 64 + local;
+    const int lo = max(max(base, 0) - 64 * c, 0), hi = min(s.len - 64 * c, 64);      // keys of the chunk that are wanted
+    const char* chunk = kv_chunk<C, H>(a.kv, seq, c, kvh);
+    if (!chunk) { if (tid == 0) kv_flag(a.kv, ASD_KV_BAD_PAGE); return; }
+    const uint8_t* exps = (const uint8_t*)chunk + 2 * L::K_BYTES + (isv ? 64 : 0);
+    auto value = [&](CE code, float scale) -> E {
+        if constexpr (!L::Q8) return code;
+        else return T::from_f32(__builtin_amdgcn_cvt_f32_fp8(code, 0) * scale);
+    };
+    auto element = [&](const u32x4& piece, int j) -> CE {                // element j of a piece (j known at compile time)
+        if constexpr (sizeof(CE) == 4) return __uint_as_float(piece[j]);
+        else return (CE)(piece[j * sizeof(CE) / 4] >> (8 * (j * sizeof(CE) % 4)));
+    };
+    if (!isv) {
+        constexpr int KK = L::KK;
+        for (int i = tid; i < 64 * H / KK; i += 256) {
+            const int l = i & 63, hp = i / 64 % L::HP, kt = i / (64 * L::HP), key = score_key<C>(kt, l & 15);
+            if (key < lo || key >= hi) continue;
+            u32x4 piece;
+            if constexpr (KK * sizeof(CE) == 16) piece = *(const u32x4*)(chunk + (size_t)i * 16);
+            else { const uint2 x = *(const uint2*)(chunk + (size_t)i * 8); piece = u32x4{x.x, x.y, 0u, 0u}; }
+            float scale = 1.f;
+            if constexpr (L::Q8) scale = q8_scale(exps[key]);
+            E* dst = &rows[key][hp * 4 * KK + (l >> 4) * KK];
+            if constexpr (sizeof(CE) == 4) { *(u32x4*)dst = piece; }
+            else {
+#pragma unroll
+                for (int j = 0; j < KK; ++j) dst[j] = value(element(piece, j), scale);
+            }
+        }
+    } else {
+        constexpr int KV = L::KV;
+        for (int i = tid; i < 64 * H / KV; i += 256) {
+            const int l = i & 63, ks = i / 64 % L::KST, ht = i / (64 * L::KST), key = ks * 4 * KV + (l >> 4) * KV, dim = ht * 16 + (l & 15);
+            if (key + KV <= lo || key >= hi) continue;
+            const u32x4 piece = *(const u32x4*)(chunk + L::K_BYTES + (size_t)i * 16);
+            u32x4 ex{};
+            if constexpr (L::Q8) ex = *(const u32x4*)(exps + key);
+#pragma unroll
+            for (int j = 0; j < KV; ++j) {
+                float scale = 1.f;
+                if constexpr (L::Q8) scale = q8_scale((ex[j / 4] >> (8 * (j % 4))) & 255u);
+                rows[key + j][dim] = value(element(piece, j), scale);
+            }
+        }
+    }
+    __syncthreads();
+    const int64_t stride = isv ? a.v_stride : a.k_stride;
+    constexpr int PPR = H * (int)sizeof(E) / 16;       // 16-byte pieces of a row
+    for (int i = tid; i < (hi - lo) * PPR; i += 256) {
+        const int key = lo + i / PPR, pc = i % PPR;
+        *(u32x4*)(out + (s.r0 + (int64_t)64 * c + key - base) * stride + kvh * H + pc * PAD) = *(const u32x4*)&rows[key][pc * PAD];
+    }
+}
+
+// ---------------------------------------------------------------- attention of the new rows
+struct KvAttendArgs {
+    KvArgs kv;
+    const void* q;
+    void* out;
+    int64_t q_stride, out_stride;
+    float c2;                       // scale * log2(e)
+    float *o_part, *ml_part;        // [item][rows of a tile][H] unnormalised sums; [item][rows][2] (maximum, sum)
+    int32_t target;                 // work items to cut the batch into
+    int32_t max_tiles;              // tiles a batch of these bounds can have: with target, the places in the workspace
+};
+// How a batch is cut.  The rows of a sequence and KV head are its new tokens x the heads of the group; a tile is 16 * NT of
+// them.  All tiles' key ranges are cut into runs of `run` chunks, the same for every sequence, so that about `target` items come out
+// whatever the lengths are: one long conversation among short ones is spread over the card.
+template <int NT> __device__ __forceinline__ int kv_tiles(const KvArgs& a, const KvSeq& v) { return (int)(((int64_t)v.n * a.group + 16 * NT - 1) / (16 * NT)); }
+template <int NT> __device__ __forceinline__ int kv_run(const KvAttendArgs& a, int lane) {
+    int64_t t = 0;
+    for (int s = lane; s < a.kv.n_seqs; s += 64) {
+        const KvSeq v = kv_seq(a.kv, s);
+        t += (int64_t)kv_tiles<NT>(a.kv, v) * ((v.len + 63) / 64);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);
+    const int64_t run = (t * a.kv.n_kv + a.target - 1) / a.target;
+    return uniform((int)min(max(run + 3, (int64_t)4) / 4 * 4, (int64_t)1 << 28));
+}
+__device__ __forceinline__ int kv_splits(const KvSeq& v, int run) { return max(1, ((v.len + 63) / 64 + run - 1) / run); }
+
+// 16 * NT rows against a run of chunks: four waves, wave w the chunks w, w + 4, ... of the run with a running maximum and sum per
+// row, merged through LDS at the end.  Scores S[key][row] = K q^T and the output O[dim][row] = V^T P are matrix-core products with the rows as
+// columns (see asd_attn.h); a chunk's fragments go from memory into registers, and the next chunk's K is asked for when the
+// scores are done, its V when the output is: memory-bound while the rows are few.
+// 8 bits: K is widened with its scale, V without: V's scales go into the probabilities, one value per key.
+template <class A, class C, int H, int NT>
+__global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(const KvAttendArgs a) {
+    using L = KvLayout<C, H>;
+    using E = typename A::elem;
+    constexpr int AE = A::KE, KK = L::KK, HP = L::HP, US = KK / AE, QS = HP * US;      // operand steps of a K piece, of a row
+    constexpr int HT = L::HT, KST = L::KST, VS = L::KV / AE, PS = KST * VS;            // ... of a V^T piece, of a chunk's keys
+    __shared__ float so[4][16][H];
+    __shared__ float sml[4][16][2];
+    const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), g = lane >> 4, m = lane & 15;
+    int seq, local;
+    int64_t first;
+    KvSeq s;
+    if (blockIdx.x == 0 && w == 0) kv_check_all(a.kv, lane);
+    const int run = kv_run<NT>(a, lane);
+    const int n_kv = a.kv.n_kv;
+    if (!kv_find(a.kv, blockIdx.x, lane, [&](const KvSeq& v) { return kv_tiles<NT>(a.kv, v) * kv_splits(v, run) * n_kv; }, &seq, &local, &first, &s)) return;
+    const int n_tiles = kv_tiles<NT>(a.kv, s), n_splits = kv_splits(s, run);
+    const int kvh = local % n_kv, tile = local / n_kv % n_tiles, split = local / n_kv / n_tiles;
+    const int rows = s.n * a.kv.group, base = s.len - s.n;
+    int pos[NT];                                        // last key of this lane's rows (-1: no such row, or none)
+    u32x4 qf[NT][QS];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int row = (tile * NT + t) * 16 + m, token = row / a.kv.group, head = kvh * a.kv.group + row % a.kv.group;
+        const bool on = row < rows;
+        pos[t] = on ? base + token : -1;
+        const E* qp = (const E*)a.q + (s.r0 + (int64_t)token) * a.q_stride + head * H;
+#pragma unroll
+        for (int i = 0; i < QS; ++i) qf[t][i] = on ? *(const u32x4*)(qp + i / US * 4 * KK + g * KK + i % US * AE) : u32x4{0u, 0u, 0u, 0u};
+    }
+    const int last = base + (min((tile + 1) * NT * 16, rows) - 1) / a.kv.group, from = base + tile * NT * 16 / a.kv.group;      // positions of the tile's rows
+    const int c_end = min((last + 64) / 64, (split + 1) * run);       // (last >= -n: nothing to do where it is negative)
+
+    f32x4 o[NT][HT];
+    float mx[NT], l[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        mx[t] = -INFINITY; l[t] = 0.f;
+#pragma unroll
+        for (int ht = 0; ht < HT; ++ht) o[t][ht] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    u32x4 kf[4][HP], vf[HT][KST], ke, ve;
+    auto ask_k = [&](const char* p) {
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int hp = 0; hp < HP; ++hp) {
+                if constexpr (KK * sizeof(typename C::elem) == 16) kf[kt][hp] = __builtin_nontemporal_load((const u32x4*)(p + ((kt * HP + hp) * 64 + lane) * 16));
+                else { const uint64_t x = __builtin_nontemporal_load((const uint64_t*)(p + ((kt * HP + hp) * 64 + lane) * 8)); kf[kt][hp] = u32x4{(uint32_t)x, (uint32_t)(x >> 32), 0u, 0u}; }
+            }
+        if constexpr (L::Q8) { ke = *(const u32x4*)(p + 2 * L::K_BYTES + 16 * (m >> 2)); }
+    };
+    auto ask_v = [&](const char* p) {
+#pragma unroll
+        for (int ht = 0; ht < HT; ++ht)
+#pragma unroll
+            for (int ks = 0; ks < KST; ++ks) vf[ht][ks] = __builtin_nontemporal_load((const u32x4*)(p + L::K_BYTES + ((ht * KST + ks) * 64 + lane) * 16));
+        if constexpr (L::Q8) ve = *(const u32x4*)(p + 2 * L::K_BYTES + 64 + 16 * g);
+    };
+    // a chunk without a page counts as hidden
+    auto next = [&](int c, const char** p) {
+        for (; c < c_end; c += 4) {
+            *p = kv_chunk<C, H>(a.kv, seq, c, kvh);
+            if (*p) break;
+            if (lane == 0) kv_flag(a.kv, ASD_KV_BAD_PAGE);
+        }
+        return c;
+    };
+    const char* p = nullptr;
+    int c = next(split * run + w, &p);
+    if (c < c_end) { ask_k(p); ask_v(p); }
+    while (c < c_end) {
+        const char* pn = nullptr;
+        const int cn = next(c + 4, &pn);
+        f32x4 sc[NT][4];
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+            float scale = 1.f;
+            if constexpr (L::Q8) scale = q8_scale((ke[kt] >> (8 * (m & 3))) & 255u);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) sc[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < QS; ++i) {
+                const u32x4 x = kv_operand<A, C>(kf[kt][i / US], i % US, scale);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) mma16<A>(sc[t][kt], x, qf[t][i]);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (cn < c_end) ask_k(pn);
+        __builtin_amdgcn_sched_barrier(0);
+        // some rows do not see all of the chunk; some of its keys are behind the sequence's end
+        const bool edge = c * 64 + 63 > from;
+        const int n_keys = s.len - c * 64;
+        float vs[4][4];
+        if constexpr (L::Q8)
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) vs[kt][j] = q8_scale((ve[kt] >> (8 * j)) & 255u);
+        u32x4 pf[NT][PS];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if (edge) {
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (c * 64 + score_key<C>(kt, 4 * g + j) > pos[t]) sc[t][kt][j] = -INFINITY;
+            }
+            float cm = sc[t][0][0];
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) cm = fmaxf(cm, sc[t][kt][j]);
+            cm = fmaxf(cm, __shfl_xor(cm, 16));
+            cm = fmaxf(cm, __shfl_xor(cm, 32));
+            const float mn = fmaxf(mx[t], cm), ref = mn == -INFINITY ? 0.f : mn;      // nothing seen yet: all weights are 0
+            const float alpha = __builtin_amdgcn_exp2f((mx[t] - ref) * a.c2);
+            mx[t] = mn;
+            l[t] *= alpha;
+#pragma unroll
+            for (int ht = 0; ht < HT; ++ht) { o[t][ht][0] *= alpha; o[t][ht][1] *= alpha; o[t][ht][2] *= alpha; o[t][ht][3] *= alpha; }
+            float pr[4][4];
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float e = __builtin_amdgcn_exp2f((sc[t][kt][j] - ref) * a.c2);
+                    l[t] += e;
+                    pr[kt][j] = e;
+                    if constexpr (L::Q8) {
+                        pr[kt][j] = e * vs[kt][j];
+                        // (an unwritten scale may be anything)
+                        if (edge && c * 64 + score_key<C>(kt, 4 * g + j) > pos[t]) pr[kt][j] = 0.f;
+                    }
+                }
+            // the probabilities as operands: lane group g holds, in order, the keys of its V^T pieces
+#pragma unroll
+            for (int i = 0; i < PS; ++i) {
+                if constexpr (AE == 8) {
+                    // bf16, as V is: each weight is off by at most 2^-9 of itself, and the sum of weights is taken unrounded
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int e = 2 * x, kt = 2 * i + e / 4;
+                        pf[t][i][x] = BF16::from_f32(pr[kt][e & 3]) | ((uint32_t)BF16::from_f32(pr[kt][(e & 3) + 1]) << 16);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) pf[t][i][j] = __float_as_uint(pr[i][j]);
+                }
+            }
+        }
+        // What is behind the end is cleared: 0 times whatever lies there must be 0
+        if (n_keys < 64) {
+            constexpr int EB = 8 * (int)sizeof(typename C::elem), PER = 32 / EB;      // bits of an element, elements of a word
+#pragma unroll
+            for (int ks = 0; ks < KST; ++ks)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int left = n_keys - (ks * 4 * L::KV + g * L::KV + x * PER);
+                    const uint32_t keep = left >= PER ? 0xffffffffu : left <= 0 ? 0u : (1u << (left * EB & 31)) - 1u;
+#pragma unroll
+                    for (int ht = 0; ht < HT; ++ht) vf[ht][ks][x] &= keep;
+                }
+        }
+        // A value that is not finite, at a key that some row of the tile does not see: 0 times it is not 0 either, so the products
+        // run without it and it is added where it is seen, from products of indicators.
+        bool odd = false;
+        if (edge && s.n > 1) {
+            uint32_t hit = 0;
+#pragma unroll
+            for (int ht = 0; ht < HT; ++ht)
+#pragma unroll
+                for (int ks = 0; ks < KST; ++ks)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const uint32_t v = vf[ht][ks][x];
+                        if constexpr (sizeof(typename C::elem) == 4) hit |= (v & 0x7f800000u) == 0x7f800000u;
+                        else if constexpr (sizeof(typename C::elem) == 2) hit |= (v & 0x7f800000u) == 0x7f800000u || (v & 0x7f80u) == 0x7f80u;
+                        else hit |= ((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                    }
+            odd = __any(hit != 0);
+        }
+        auto product = [&](auto checked) {
+#pragma unroll
+            for (int ht = 0; ht < HT; ++ht)
+#pragma unroll
+                for (int i = 0; i < PS; ++i) {
+                    u32x4 v = kv_operand<A, C>(vf[ht][i / VS], i % VS, 1.f);
+                    if constexpr (decltype(checked)::value) {
+                        constexpr int N = AE == 8 ? 2 : 1;                           // elements of a word
+                        u32x4 clean = v, kind[3] = {};                               // kinds: +inf, -inf, NaN
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+#pragma unroll
+                            for (int h = 0; h < N; ++h) {
+                                const int sh = N == 2 ? 16 * h : 0;
+                                const uint32_t f = N == 2 ? ((v[x] >> sh) & 0xffffu) << 16 : v[x], one = N == 2 ? 0x3f80u << sh : 0x3f800000u;
+                                if ((f & 0x7f800000u) == 0x7f800000u) {
+                                    clean[x] &= N == 2 ? ~(0xffffu << sh) : 0u;
+                                    kind[(f & 0x7fffffu) ? 2 : (f >> 31)][x] |= one;
+                                }
+                            }
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            mma16<A>(o[t][ht], clean, pf[t][i]);
+                            u32x4 seen{};
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                                for (int h = 0; h < N; ++h) {
+                                    const int e = N * x + h, key = i / VS * 4 * L::KV + g * L::KV + i % VS * AE + e;
+                                    if (c * 64 + key <= pos[t]) seen[x] |= N == 2 ? 0x3f80u << (16 * h) : 0x3f800000u;
+                                }
+#pragma unroll
+                            for (int y = 0; y < 3; ++y) {
+                                f32x4 n = f32x4{0.f, 0.f, 0.f, 0.f};
+                                mma16<A>(n, kind[y], seen);
+                                const float add = y == 0 ? INFINITY : y == 1 ? -INFINITY : __uint_as_float(0x7fc00000u);
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) if (n[j] > 0.f) o[t][ht][j] += add;
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) mma16<A>(o[t][ht], v, pf[t][i]);
+                    }
+                }
+        };
+        if (odd) product(std::true_type{}); else product(std::false_type{});
+        __builtin_amdgcn_sched_barrier(0);
+        if (cn < c_end) ask_v(pn);
+        __builtin_amdgcn_sched_barrier(0);
+        c = cn;
+    }
+
+    // ---- the waves' results, 16 rows at a time, wave order
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        if (t) __syncthreads();
+        l[t] += __shfl_xor(l[t], 16);
+        l[t] += __shfl_xor(l[t], 32);
+        if (g == 0) { sml[w][m][0] = mx[t]; sml[w][m][1] = l[t]; }
+#pragma unroll
+        for (int ht = 0; ht < HT; ++ht) *(f32x4*)&so[w][m][ht * 16 + 4 * g] = o[t][ht];
+        __syncthreads();
+        const int r = tid & 15, row = (tile * NT + t) * 16 + r, token = row / a.kv.group, head = kvh * a.kv.group + row % a.kv.group;
+        float top = -INFINITY, sum = 0.f, wt[4];
+#pragma unroll
+        for (int ww = 0; ww < 4; ++ww) top = fmaxf(top, sml[ww][r][0]);
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int ww = 0; ww < 4; ++ww) { wt[ww] = __builtin_amdgcn_exp2f((sml[ww][r][0] - ref) * a.c2); sum += sml[ww][r][1] * wt[ww]; }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        for (int d = (tid >> 4) * 4; d < H; d += 64) {
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ww = 0; ww < 4; ++ww) {
+                const f32x4 x = *(const f32x4*)&so[ww][r][d];
+                v[0] += x[0] * wt[ww]; v[1] += x[1] * wt[ww]; v[2] += x[2] * wt[ww]; v[3] += x[3] * wt[ww];
+            }
+            if (row >= rows) continue;
+            if (n_splits == 1) {
+                v[0] *= inv; v[1] *= inv; v[2] *= inv; v[3] *= inv;
+                store4<A>((E*)a.out + (s.r0 + (int64_t)token) * a.out_stride + head * H + d, v);
+            } else {
+                const size_t at = (size_t)blockIdx.x * (16 * NT) + t * 16 + r;
+                *(float4*)(a.o_part + at * H + d) = float4{v[0], v[1], v[2], v[3]};
+                if (d == 0) { a.ml_part[at * 2] = top; a.ml_part[at * 2 + 1] = sum; }
+            }
+        }
+    }
+}
+
+// Joins the runs of every row whose keys were cut: a wave per row and head, runs in ascending order.
+template <class A, int H, int NT>
+__global__ __launch_bounds__(256) void kv_join_kernel(const KvAttendArgs a) {
+    using E = typename A::elem;
+    const int lane = threadIdx.x & 63;
+    const int64_t item = (int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6);
+    const int run = kv_run<NT>(a, lane), n_kv = a.kv.n_kv, group = a.kv.group;
+    int64_t base = 0, first = 0;                        // (rows x heads) and work items of the sequences in front
+    KvSeq s{0, 0, 0};
+    int seq = -1;
+    for (int s0 = 0; s0 < a.kv.n_seqs && seq < 0; s0 += 64) {
+        KvSeq v{0, 0, 0};
+        if (s0 + lane < a.kv.n_seqs) v = kv_seq(a.kv, s0 + lane);
+        const int cr = v.n * a.kv.n_h, cw = v.n ? kv_tiles<NT>(a.kv, v) * kv_splits(v, run) * n_kv : 0;
+        int ir = cr, iw = cw;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(ir, o), y = __shfl_up(iw, o);
+            if (lane >= o) { ir += x; iw += y; }
+        }
+        const int tr = uniform(__shfl(ir, 63)), tw = uniform(__shfl(iw, 63));
+        if (item < base + tr) {
+            const int at = __ffsll((unsigned long long)__ballot(base + ir > item)) - 1;
+            seq = s0 + at;
+            base += uniform(__shfl(ir - cr, at));
+            first += uniform(__shfl(iw - cw, at));
+            s = KvSeq{uniform(__shfl(v.r0, at)), uniform(__shfl(v.n, at)), uniform(__shfl(v.len, at))};
+        } else { base += tr; first += tw; }
+    }
+    if (seq < 0) return;
+    const int n_splits = kv_splits(s, run);
+    if (n_splits == 1) return;
+    const int local = (int)(item - base), token = local / a.kv.n_h, head = local % a.kv.n_h, kvh = head / group;
+    const int row = token * group + head % group, tile = row / (16 * NT), n_tiles = kv_tiles<NT>(a.kv, s);
+    const int64_t step = (int64_t)n_tiles * n_kv * (16 * NT);       // a run's place to the next run's
+    const int64_t at = (first + (int64_t)tile * n_kv + kvh) * (16 * NT) + row % (16 * NT);
+    const float* ml = a.ml_part + at * 2;
+    float top = -INFINITY;
+    for (int i = lane; i < n_splits; i += 64) top = fmaxf(top, ml[i * step * 2]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const float ref = top == -INFINITY ? 0.f : top;
+    constexpr int DL = H / 64 > 0 ? H / 64 : 1, U = 8;              // dims of a lane, runs in flight
+    float acc[DL] = {}, sum = 0.f;
+    const bool mine = lane * DL < H;
+    const float* op = a.o_part + at * H + lane * DL;
+    for (int i0 = 0; i0 < n_splits; i0 += U) {
+        float x[U][DL], wm[U], ws[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool on = i0 + u < n_splits;
+            const int64_t r = (on ? i0 + u : i0) * step;
+            wm[u] = on ? ml[r * 2] : -INFINITY;
+            ws[u] = ml[r * 2 + 1];
+#pragma unroll
+            for (int d = 0; d < DL; ++d) x[u][d] = mine ? op[r * H + d] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float wt = __builtin_amdgcn_exp2f((wm[u] - ref) * a.c2);
+            if (i0 + u < n_splits) {
+                sum += ws[u] * wt;
+#pragma unroll
+                for (int d = 0; d < DL; ++d) acc[d] += x[u][d] * wt;
+            }
+        }
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    if (!mine) return;
+    E* out = (E*)a.out + (s.r0 + (int64_t)token) * a.out_stride + head * H + lane * DL;
+    if constexpr (DL == 2 && sizeof(E) == 2) *(uint32_t*)out = A::from_f32(acc[0] * inv) | ((uint32_t)A::from_f32(acc[1] * inv) << 16);
+    else {
+#pragma unroll
+        for (int d = 0; d < DL; ++d) out[d] = A::from_f32(acc[d] * inv);
+    }
+}
+
+// ---------------------------------------------------------------- rotary tables
+// (cos, sin) of pos * frequency, in double; frequencies theta^(-2j / rot), changed for contexts longer than the trained one
+// (turns of frequency f over the trained length: r = trained * f / 2 pi):
+//   ASD_ROPE_LINEAR  f / factor
+//   ASD_ROPE_BANDS   f where r >= high, f / factor where r <= low, in between mixed by (r - low) / (high - low)
+//   ASD_ROPE_RAMP    mixed by the pair's index between the indexes that make `high` and `low` turns (rounded outwards), values times `gain`
+struct RopeArgs { double theta, factor, low, high, trained, gain; int32_t rot, kind, positions; };
+__global__ __launch_bounds__(256) void kv_rope_kernel(const RopeArgs a, float* out) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int hr = a.rot / 2;
+    if (i >= (int64_t)a.positions * hr) return;
+    const int j = (int)(i % hr), pos = (int)(i / hr);
+    const double two_pi = 6.283185307179586476925;
+    double f = pow(a.theta, -2.0 * j / a.rot);
+    if (a.kind == ASD_ROPE_LINEAR) f /= a.factor;
+    if (a.kind == ASD_ROPE_BANDS) {
+        const double keep = fmin(1.0, fmax(0.0, (a.trained * f / two_pi - a.low) / (a.high - a.low)));
+        f = keep * f + (1.0 - keep) * f / a.factor;
+    }
+    if (a.kind == ASD_ROPE_RAMP) {
+        auto index = [&](double turns) { return a.rot * log(a.trained / (turns * two_pi)) / (2.0 * log(a.theta)); };
+        const double lo = fmax(0.0, floor(index(a.high))), hi = fmin(a.rot - 1.0, ceil(index(a.low)));
+        const double keep = 1.0 - fmin(1.0, fmax(0.0, (j - lo) / fmax(hi - lo, 1e-3)));
+        f = keep * f + (1.0 - keep) * f / a.factor;
+    }
+    out[2 * i] = (float)(cos(pos * f) * a.gain);
+    out[2 * i + 1] = (float)(sin(pos * f) * a.gain);
+}

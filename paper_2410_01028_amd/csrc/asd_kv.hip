@@ -1,0 +1,230 @@
+// Host side of the operators over a paged cache of several sequences: argument checks, launch rules, the C ABI of asd.h.
+#include "../../include/asd.h"
+#include "asd_kv.h"
+
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+
+__attribute__((visibility("hidden"))) void asd_note_error(const char* message);
+
+namespace {
+
+int refuse(int code, const char* fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    try { asd_note_error(buf); } catch (...) {}
+    return code;
+}
+
+const char* shape_fault(const asd_kv_shape* s) {
+    if (!s) return "shape is NULL";
+    if (s->n_heads < 1 || s->n_kv_heads < 1 || s->n_heads % s->n_kv_heads) return "n_heads must be a positive multiple of n_kv_heads";
+    if (s->n_heads > 4096) return "more than 4096 heads";
+    if (s->head_dim != 32 && s->head_dim != 64 && s->head_dim != 128) return "head_dim must be 32, 64 or 128";
+    if (s->page_tokens < 64 || s->page_tokens % 64 || s->page_tokens > 1 << 24) return "page_tokens must be a positive multiple of 64";
+    if (s->dtype != ASD_DT_F32 && s->dtype != ASD_DT_BF16) return "dtype must be ASD_DT_F32 or ASD_DT_BF16";
+    if (s->kv_dtype != s->dtype && s->kv_dtype != ASD_DT_FP8) return "kv_dtype must be dtype or ASD_DT_FP8";
+    return nullptr;
+}
+
+const char* batch_fault(const asd_kv_shape* s, const asd_kv_batch* b) {
+    if (!b) return "batch is NULL";
+    if (!b->pages || (uintptr_t)b->pages % 16) return "pages must be a device pointer, 16-byte aligned";
+    if (!b->page_table || !b->row_start || !b->kv_len) return "page_table, row_start and kv_len must be device pointers";
+    if (((uintptr_t)b->page_table | (uintptr_t)b->row_start | (uintptr_t)b->kv_len | (uintptr_t)b->status) % 4) return "the batch's arrays must be 4-byte aligned";
+    if (b->n_pages < 1 || b->table_stride < 1) return "n_pages and table_stride must be positive";
+    if (b->n_seqs < 1 || b->n_seqs > 65536) return "n_seqs must be in 1..65536";
+    if (b->n_rows < 1 || (int64_t)b->n_rows * s->n_heads >= (int64_t)1 << 31) return "n_rows must be positive, and n_rows * n_heads below 2^31";
+    if (b->max_new < 1 || b->max_new > b->n_rows) return "max_new must be in 1..n_rows";
+    if (b->max_len < 1 || b->max_len > 1 << 24) return "max_len must be in 1..2^24";
+    return nullptr;
+}
+
+// a buffer of rows: pointer, stride from row to row, heads of a row
+const char* rows_fault(const asd_kv_shape* s, const void* p, int64_t stride, int heads) {
+    const int es = s->dtype == ASD_DT_BF16 ? 2 : 4;
+    if ((uintptr_t)p % 16 || stride * es % 16) return "row pointers and strides must be multiples of 16 bytes";
+    if (stride < (int64_t)heads * s->head_dim || stride > (int64_t)1 << 40) return "a row stride is smaller than a row";
+    return nullptr;
+}
+
+KvArgs kv_args(const asd_kv_shape* s, const asd_kv_batch* b) {
+    KvArgs a{};
+    a.pages = (char*)b->pages; a.table = b->page_table; a.row_start = b->row_start; a.kv_len = b->kv_len; a.status = b->status;
+    a.n_pages = b->n_pages; a.table_stride = b->table_stride; a.n_seqs = b->n_seqs; a.n_rows = b->n_rows; a.max_new = b->max_new;
+    const int64_t reach = (int64_t)b->table_stride * s->page_tokens;
+    a.cap = (int32_t)(reach < b->max_len ? reach : b->max_len);
+    a.n_h = s->n_heads; a.n_kv = s->n_kv_heads; a.group = s->n_heads / s->n_kv_heads; a.page_tokens = s->page_tokens;
+    return a;
+}
+
+// f<row type, cache type, head dim>() for the shape
+template <class F> void by_shape(const asd_kv_shape* s, F f) {
+    auto dim = [&](auto t, auto c) {
+        if (s->head_dim == 32) f(t, c, std::integral_constant<int, 32>{});
+        else if (s->head_dim == 64) f(t, c, std::integral_constant<int, 64>{});
+        else f(t, c, std::integral_constant<int, 128>{});
+    };
+    const bool q8 = s->kv_dtype == ASD_DT_FP8;
+    if (s->dtype == ASD_DT_BF16) { if (q8) dim(BF16{}, FP8{}); else dim(BF16{}, BF16{}); }
+    else { if (q8) dim(F32{}, FP8{}); else dim(F32{}, F32{}); }
+}
+
+int launched(const char* what) {
+    const hipError_t r = hipGetLastError();
+    return r == hipSuccess ? ASD_OK : refuse(ASD_E_HIP, "%s: %s", what, hipGetErrorString(r));
+}
+
+int units() {
+    static const int n = [] {
+        int dev = 0, v = 0;
+        return hipGetDevice(&dev) == hipSuccess && hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && v > 0 ? v : 256;
+    }();
+    return n;
+}
+
+// How asd_kv_attend runs a batch of these bounds
+struct AttendPlan {
+    int nt;                        // 16-row column blocks of a tile
+    int32_t target, max_tiles;
+    int64_t grid;                  // most work items
+    bool join;                     // some sequence's keys may be cut
+    size_t o_bytes, bytes;
+};
+AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b) {
+    AttendPlan p{};
+    const int group = s->n_heads / s->n_kv_heads;
+    const int64_t rows = (int64_t)b->max_new * group, chunks = (kv_args(s, b).cap + 63) / 64;
+    // Rows share a chunk's fragments: as many columns as the largest sequence fills, up to 64 (fp32: 32, whose operands take twice the registers)
+    p.nt = rows <= 16 ? 1 : s->dtype == ASD_DT_F32 ? 2 : rows <= 32 ? 2 : 4;
+    p.target = 4 * units();
+    p.max_tiles = (int32_t)((int64_t)b->n_rows * group / (16 * p.nt) + (b->n_seqs < b->n_rows ? b->n_seqs : b->n_rows));
+    const int64_t whole = (int64_t)p.max_tiles * s->n_kv_heads;
+    p.join = chunks > 4;
+    p.grid = whole + p.target;
+    if (whole * ((chunks + 3) / 4) < p.grid) p.grid = whole * ((chunks + 3) / 4);
+    if (p.join) {
+        p.o_bytes = ((size_t)p.grid * 16 * p.nt * s->head_dim * 4 + 255) / 256 * 256;
+        p.bytes = p.o_bytes + (size_t)p.grid * 16 * p.nt * 8;
+    }
+    return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t asd_kv_page_bytes(const asd_kv_shape* s) {
+    if (shape_fault(s)) return 0;
+    const int es = s->kv_dtype == ASD_DT_FP8 ? 1 : s->kv_dtype == ASD_DT_BF16 ? 2 : 4;
+    return (size_t)s->n_kv_heads * (s->page_tokens / 64) * (128 * (size_t)s->head_dim * es + (es == 1 ? 128 : 0));
+}
+
+int asd_kv_append(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_prep* p, const void* q, int64_t q_stride, const void* k,
+                  int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t out_stride, void* hip_stream) {
+    const char* why = shape_fault(s);
+    if (!why) why = batch_fault(s, b);
+    if (!why && !p) why = "prep is NULL";
+    if (!why && (!k || !v)) why = "k and v must be device pointers";
+    if (!why && !q != !q_out) why = "q and q_out go together";
+    if (!why) why = rows_fault(s, k, k_stride, s->n_kv_heads);
+    if (!why) why = rows_fault(s, v, v_stride, s->n_kv_heads);
+    if (!why && q) why = rows_fault(s, q, q_stride, s->n_heads);
+    if (!why && q) why = rows_fault(s, q_out, out_stride, s->n_heads);
+    if (!why && (p->rot_dim < 0 || p->rot_dim > s->head_dim || p->rot_dim % 8)) why = "rot_dim must be a multiple of 8 in 0..head_dim";
+    if (!why && p->rot_dim && (!p->rope || (uintptr_t)p->rope % 16 || p->rope_positions < 1)) why = "rope must be a 16-byte aligned table of at least one position";
+    if (!why && ((uintptr_t)p->q_gain | (uintptr_t)p->k_gain) % 16) why = "gains must be 16-byte aligned";
+    if (!why && (p->q_gain || p->k_gain) && !(p->eps >= 0.f && std::isfinite(p->eps))) why = "eps must be a number >= 0";
+    if (why) return refuse(ASD_E_INVAL, "asd_kv_append: %s", why);
+    KvAppendArgs a{};
+    a.kv = kv_args(s, b);
+    a.q = q; a.k = k; a.v = v; a.q_out = q_out;
+    a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.out_stride = out_stride;
+    a.q_gain = p->q_gain; a.k_gain = p->k_gain; a.rope = p->rope; a.eps = p->eps;
+    a.rope_positions = p->rope_positions; a.rot = p->rot_dim; a.interleaved = p->interleaved;
+    const int most = b->max_new < 16 ? b->max_new : 16;             // tokens of a tile
+    a.kv_heads_per = 16 / most < s->n_kv_heads ? 16 / most : s->n_kv_heads;
+    a.q_heads_per = 64 / most < s->n_heads ? 64 / most : s->n_heads;
+    a.kv_blocks = (s->n_kv_heads + a.kv_heads_per - 1) / a.kv_heads_per;
+    const int q_blocks = q ? (s->n_heads + a.q_heads_per - 1) / a.q_heads_per : 0;
+    // tiles at positions divisible by 16: rows / 16 and two more at a sequence's ends, but no more than it has rows
+    const int64_t seqs = b->n_seqs < b->n_rows ? b->n_seqs : b->n_rows, loose = b->n_rows / 16 + 2 * seqs;
+    const dim3 grid((unsigned)(loose < b->n_rows ? loose : b->n_rows), a.kv_blocks + q_blocks);
+    by_shape(s, [&](auto t, auto c, auto h) { kv_append_kernel<decltype(t), decltype(c), h.value><<<grid, 256, 0, (hipStream_t)hip_stream>>>(a); });
+    return launched("asd_kv_append");
+}
+
+size_t asd_kv_attend_workspace(const asd_kv_shape* s, const asd_kv_batch* b) {
+    if (shape_fault(s) || batch_fault(s, b)) return 0;
+    return attend_plan(s, b).bytes;
+}
+
+int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, int64_t q_stride, void* out, int64_t out_stride, float scale,
+                  void* workspace, size_t workspace_bytes, void* hip_stream) {
+    const char* why = shape_fault(s);
+    if (!why) why = batch_fault(s, b);
+    if (!why && (!q || !out)) why = "q and out must be device pointers";
+    if (!why) why = rows_fault(s, q, q_stride, s->n_heads);
+    if (!why) why = rows_fault(s, out, out_stride, s->n_heads);
+    if (!why && !(scale > 0.f && std::isfinite(scale))) why = "scale must be a positive number";
+    if (why) return refuse(ASD_E_INVAL, "asd_kv_attend: %s", why);
+    const AttendPlan p = attend_plan(s, b);
+    if (p.bytes && (!workspace || (uintptr_t)workspace % 256)) return refuse(ASD_E_INVAL, "asd_kv_attend: workspace must be 256-byte aligned");
+    if (workspace_bytes < p.bytes) return refuse(ASD_E_NOMEM, "asd_kv_attend: workspace too small: %zu bytes given, %zu needed", workspace_bytes, p.bytes);
+    if (p.grid >= (int64_t)1 << 31) return refuse(ASD_E_INVAL, "asd_kv_attend: the batch is too large");
+    KvAttendArgs a{};
+    a.kv = kv_args(s, b);
+    a.q = q; a.out = out; a.q_stride = q_stride; a.out_stride = out_stride;
+    a.c2 = (float)((double)scale * 1.4426950408889634074);
+    a.o_part = (float*)workspace; a.ml_part = (float*)((char*)workspace + p.o_bytes);
+    a.target = p.target; a.max_tiles = p.max_tiles;
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    auto go = [&](auto t, auto c, auto h, auto nt) {
+        kv_attend_kernel<decltype(t), decltype(c), h.value, nt.value><<<(unsigned)p.grid, 256, 0, stream>>>(a);
+        if (p.join) kv_join_kernel<decltype(t), h.value, nt.value><<<(unsigned)(((int64_t)b->n_rows * s->n_heads + 3) / 4), 256, 0, stream>>>(a);
+    };
+    by_shape(s, [&](auto t, auto c, auto h) {
+        if (p.nt == 1) go(t, c, h, std::integral_constant<int, 1>{});
+        else if (p.nt == 2) go(t, c, h, std::integral_constant<int, 2>{});
+        else if constexpr (sizeof(typename decltype(t)::elem) == 2) go(t, c, h, std::integral_constant<int, 4>{});
+    });
+    return launched("asd_kv_attend");
+}
+
+int asd_kv_read(const asd_kv_shape* s, const asd_kv_batch* b, void* k_out, int64_t k_stride, void* v_out, int64_t v_stride, void* hip_stream) {
+    const char* why = shape_fault(s);
+    if (!why) why = batch_fault(s, b);
+    if (!why && k_out) why = rows_fault(s, k_out, k_stride, s->n_kv_heads);
+    if (!why && v_out) why = rows_fault(s, v_out, v_stride, s->n_kv_heads);
+    if (why) return refuse(ASD_E_INVAL, "asd_kv_read: %s", why);
+    if (!k_out && !v_out) return ASD_OK;
+    KvReadArgs a{};
+    a.kv = kv_args(s, b);
+    a.k_out = k_out; a.v_out = v_out; a.k_stride = k_stride; a.v_stride = v_stride;
+    const int64_t seqs = b->n_seqs < b->n_rows ? b->n_seqs : b->n_rows, loose = b->n_rows / 64 + 2 * seqs;
+    const dim3 grid((unsigned)(loose < b->n_rows ? loose : b->n_rows), s->n_kv_heads, 2);
+    by_shape(s, [&](auto t, auto c, auto h) { kv_read_kernel<decltype(t), decltype(c), h.value><<<grid, 256, 0, (hipStream_t)hip_stream>>>(a); });
+    return launched("asd_kv_read");
+}
+
+int asd_rope_table(const asd_rope* r, int32_t positions, float* table, void* hip_stream) {
+    const char* why = nullptr;
+    if (!r || !table || (uintptr_t)table % 16) why = "rope and table (16-byte aligned) must be given";
+    else if (r->kind < ASD_ROPE_PLAIN || r->kind > ASD_ROPE_RAMP) why = "unknown kind";
+    else if (r->rot_dim < 8 || r->rot_dim % 8 || r->rot_dim > 128) why = "rot_dim must be a multiple of 8 in 8..128";
+    else if (positions < 1 || positions > 1 << 24) why = "positions must be in 1..2^24";
+    else if (!(r->theta > 1.0) || !std::isfinite(r->theta)) why = "theta must be above 1";
+    else if (r->kind != ASD_ROPE_PLAIN && (!(r->factor >= 1.0) || !std::isfinite(r->factor))) why = "factor must be at least 1";
+    else if (r->kind >= ASD_ROPE_BANDS && !(r->low > 0.0 && r->high > r->low && std::isfinite(r->high) && r->trained >= 1.0 && std::isfinite(r->trained))) why = "0 < low < high and trained >= 1 are needed";
+    else if (!(r->gain >= 0.0) || !std::isfinite(r->gain)) why = "gain must be a number >= 0";
+    if (why) return refuse(ASD_E_INVAL, "asd_rope_table: %s", why);
+    const RopeArgs a{r->theta, r->factor, r->low, r->high, r->trained, r->gain == 0.0 ? 1.0 : r->gain, r->rot_dim, r->kind, positions};
+    kv_rope_kernel<<<(unsigned)(((int64_t)positions * (r->rot_dim / 2) + 255) / 256), 256, 0, (hipStream_t)hip_stream>>>(a, table);
+    return launched("asd_rope_table");
+}
+
+}  // extern "C"
