@@ -420,24 +420,56 @@ template <int NT> __device__ __forceinline__ int kv_run(const KvAttendArgs& a, i
 }
 __device__ __forceinline__ int kv_splits(const KvSeq& v, int run) { return max(1, ((v.len + 63) / 64 + run - 1) / run); }
 
+// ---- V that is not finite at a key that some rows of a tile do not see: 0 times it is not 0.  In the chunks where that can be (edge
+// chunks: not all rows of the tile see all keys) such values are taken out of the products, and what a row sees of them is added to
+// its sums when they have been stored (infinities and NaN may be added in any order).  Rare, so that path is a plain loop over memory.
+// a word of a V^T piece without them
+template <class C> __device__ __forceinline__ uint32_t kv_clean(uint32_t v) {
+    if constexpr (sizeof(typename C::elem) == 4) return (v & 0x7f800000u) == 0x7f800000u ? 0u : v;
+    else if constexpr (sizeof(typename C::elem) == 2) return v & ((v & 0x7f800000u) == 0x7f800000u ? 0xffffu : ~0u) & ((v & 0x7f80u) == 0x7f80u ? ~0xffffu : ~0u);
+    else return v & ~((((v & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xffu);
+}
+// their sum over the keys key0 .. last at one dim (0: there are none)
+template <class C, int H> __device__ float kv_odd_sum(const KvArgs& a, int seq, int kvh, int key0, int last, int dim) {
+    float sum = 0.f;
+    for (int key = key0; key <= last; ++key) {
+        const char* p = kv_chunk<C, H>(a, seq, key / 64, kvh);
+        if (!p) continue;
+        const typename C::elem v = *(const typename C::elem*)(p + KvLayout<C, H>::v_off(key % 64, dim));
+        float f;
+        if constexpr (sizeof(v) == 1) f = (v & 0x7f) == 0x7f ? __uint_as_float(0x7fc00000u) : 0.f;
+        else f = C::to_f32(v);
+        if (!finite(f)) sum += f;
+    }
+    return sum;
+}
+// the bits of word x of a lane's V^T piece ks whose keys are among the first n_keys of the chunk
+template <class C> __device__ __forceinline__ uint32_t kv_kept(int n_keys, int ks, int g, int x) {
+    constexpr int EB = 8 * (int)sizeof(typename C::elem), PER = 32 / EB;      // bits of an element, elements of a word
+    const int left = n_keys - (ks * 4 * C::KE + g * C::KE + x * PER);
+    return left >= PER ? 0xffffffffu : left <= 0 ? 0u : (1u << (left * EB & 31)) - 1u;
+}
+
 // 16 * NT rows against a run of chunks: four waves, wave w the chunks w, w + 4, ... of the run with a running maximum and sum per
 // row, merged through LDS at the end.  Scores S[key][row] = K q^T and the output O[dim][row] = V^T P are matrix-core products with the rows as
 // columns (see asd_attn.h); a chunk's fragments go from memory into registers, and the next chunk's K is asked for when the
 // scores are done, its V when the output is: memory-bound while the rows are few.
 // 8 bits: K is widened with its scale, V without: V's scales go into the probabilities, one value per key.
 template <class A, class C, int H, int NT>
-__global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(const KvAttendArgs a) {
+__global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_kernel(const KvAttendArgs a) {
     using L = KvLayout<C, H>;
     using E = typename A::elem;
     constexpr int AE = A::KE, KK = L::KK, HP = L::HP, US = KK / AE, QS = HP * US;      // operand steps of a K piece, of a row
     constexpr int HT = L::HT, KST = L::KST, VS = L::KV / AE, PS = KST * VS;            // ... of a V^T piece, of a chunk's keys
     __shared__ float so[4][16][H];
     __shared__ float sml[4][16][2];
+    __shared__ int s_odd;
     const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), g = lane >> 4, m = lane & 15;
     int seq, local;
     int64_t first;
     KvSeq s;
     if (blockIdx.x == 0 && w == 0) kv_check_all(a.kv, lane);
+    if (tid == 0) s_odd = 0;
     const int run = kv_run<NT>(a, lane);
     const int n_kv = a.kv.n_kv;
     if (!kv_find(a.kv, blockIdx.x, lane, [&](const KvSeq& v) { return kv_tiles<NT>(a.kv, v) * kv_splits(v, run) * n_kv; }, &seq, &local, &first, &s)) return;
@@ -493,6 +525,7 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(cons
         }
         return c;
     };
+    bool odd = false;
     const char* p = nullptr;
     int c = next(split * run + w, &p);
     if (c < c_end) { ask_k(p); ask_v(p); }
@@ -578,84 +611,30 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(cons
                 }
             }
         }
-        // What is behind the end is cleared: 0 times whatever lies there must be 0
-        if (n_keys < 64) {
-            constexpr int EB = 8 * (int)sizeof(typename C::elem), PER = 32 / EB;      // bits of an element, elements of a word
+        if (edge) {                                     // what is behind the end is cleared: 0 times whatever lies there must be 0
+            uint32_t hit = 0;
 #pragma unroll
             for (int ks = 0; ks < KST; ++ks)
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const int left = n_keys - (ks * 4 * L::KV + g * L::KV + x * PER);
-                    const uint32_t keep = left >= PER ? 0xffffffffu : left <= 0 ? 0u : (1u << (left * EB & 31)) - 1u;
+                    const uint32_t keep = kv_kept<C>(n_keys, ks, g, x);
 #pragma unroll
-                    for (int ht = 0; ht < HT; ++ht) vf[ht][ks][x] &= keep;
-                }
-        }
-        // A value that is not finite, at a key that some row of the tile does not see: 0 times it is not 0 either, so the products
-        // run without it and it is added where it is seen, from products of indicators.
-        bool odd = false;
-        if (edge && s.n > 1) {
-            uint32_t hit = 0;
-#pragma unroll
-            for (int ht = 0; ht < HT; ++ht)
-#pragma unroll
-                for (int ks = 0; ks < KST; ++ks)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const uint32_t v = vf[ht][ks][x];
-                        if constexpr (sizeof(typename C::elem) == 4) hit |= (v & 0x7f800000u) == 0x7f800000u;
-                        else if constexpr (sizeof(typename C::elem) == 2) hit |= (v & 0x7f800000u) == 0x7f800000u || (v & 0x7f80u) == 0x7f80u;
-                        else hit |= ((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-                    }
-            odd = __any(hit != 0);
-        }
-        auto product = [&](auto checked) {
-#pragma unroll
-            for (int ht = 0; ht < HT; ++ht)
-#pragma unroll
-                for (int i = 0; i < PS; ++i) {
-                    u32x4 v = kv_operand<A, C>(vf[ht][i / VS], i % VS, 1.f);
-                    if constexpr (decltype(checked)::value) {
-                        constexpr int N = AE == 8 ? 2 : 1;                           // elements of a word
-                        u32x4 clean = v, kind[3] = {};                               // kinds: +inf, -inf, NaN
-#pragma unroll
-                        for (int x = 0; x < 4; ++x)
-#pragma unroll
-                            for (int h = 0; h < N; ++h) {
-                                const int sh = N == 2 ? 16 * h : 0;
-                                const uint32_t f = N == 2 ? ((v[x] >> sh) & 0xffffu) << 16 : v[x], one = N == 2 ? 0x3f80u << sh : 0x3f800000u;
-                                if ((f & 0x7f800000u) == 0x7f800000u) {
-                                    clean[x] &= N == 2 ? ~(0xffffu << sh) : 0u;
-                                    kind[(f & 0x7fffffu) ? 2 : (f >> 31)][x] |= one;
-                                }
-                            }
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            mma16<A>(o[t][ht], clean, pf[t][i]);
-                            u32x4 seen{};
-#pragma unroll
-                            for (int x = 0; x < 4; ++x)
-#pragma unroll
-                                for (int h = 0; h < N; ++h) {
-                                    const int e = N * x + h, key = i / VS * 4 * L::KV + g * L::KV + i % VS * AE + e;
-                                    if (c * 64 + key <= pos[t]) seen[x] |= N == 2 ? 0x3f80u << (16 * h) : 0x3f800000u;
-                                }
-#pragma unroll
-                            for (int y = 0; y < 3; ++y) {
-                                f32x4 n = f32x4{0.f, 0.f, 0.f, 0.f};
-                                mma16<A>(n, kind[y], seen);
-                                const float add = y == 0 ? INFINITY : y == 1 ? -INFINITY : __uint_as_float(0x7fc00000u);
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) if (n[j] > 0.f) o[t][ht][j] += add;
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) mma16<A>(o[t][ht], v, pf[t][i]);
+                    for (int ht = 0; ht < HT; ++ht) {
+                        const uint32_t v = vf[ht][ks][x] & keep;
+                        vf[ht][ks][x] = kv_clean<C>(v);
+                        hit |= v ^ vf[ht][ks][x];
                     }
                 }
-        };
-        if (odd) product(std::true_type{}); else product(std::false_type{});
+            if (__any(hit != 0)) odd = true;
+        }
+#pragma unroll
+        for (int ht = 0; ht < HT; ++ht)
+#pragma unroll
+            for (int i = 0; i < PS; ++i) {
+                const u32x4 v = kv_operand<A, C>(vf[ht][i / VS], i % VS, 1.f);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) mma16<A>(o[t][ht], v, pf[t][i]);
+            }
         __builtin_amdgcn_sched_barrier(0);
         if (cn < c_end) ask_v(pn);
         __builtin_amdgcn_sched_barrier(0);
@@ -663,6 +642,8 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(cons
     }
 
     // ---- the waves' results, 16 rows at a time, wave order
+    __syncthreads();                                    // (s_odd is cleared)
+    if (odd && lane == 0) s_odd = 1;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         if (t) __syncthreads();
@@ -688,6 +669,10 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(cons
                 v[0] += x[0] * wt[ww]; v[1] += x[1] * wt[ww]; v[2] += x[2] * wt[ww]; v[3] += x[3] * wt[ww];
             }
             if (row >= rows) continue;
+            if (s_odd) {
+                const int key0 = max((from + 1) / 64, split * run) * 64, key1 = min(base + token, c_end * 64 - 1);
+                for (int j = 0; j < 4; ++j) v[j] += kv_odd_sum<C, H>(a.kv, seq, kvh, key0, key1, d + j);
+            }
             if (n_splits == 1) {
                 v[0] *= inv; v[1] *= inv; v[2] *= inv; v[3] *= inv;
                 store4<A>((E*)a.out + (s.r0 + (int64_t)token) * a.out_stride + head * H + d, v);
@@ -695,6 +680,251 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(cons
                 const size_t at = (size_t)blockIdx.x * (16 * NT) + t * 16 + r;
                 *(float4*)(a.o_part + at * H + d) = float4{v[0], v[1], v[2], v[3]};
                 if (d == 0) { a.ml_part[at * 2] = top; a.ml_part[at * 2 + 1] = sum; }
+            }
+        }
+    }
+}
+
+// Many rows (bf16): four waves with 16 * NT rows each walk a run of chunks together.  A chunk's halves (K with the scales, V^T) come into an LDS
+// ring by direct loads, once for the 64 * NT rows; a step waits for its half, one barrier, asks for the half SLOTS - 1 steps on
+// (its slot was last read one step ago) and computes.  Two workgroups share a compute unit, one's products beside the other's exponentials.
+template <class C, int H, int NT> struct KvRowsLds {
+    using L = KvLayout<C, H>;
+    static constexpr int HF = L::K_BYTES / 1024, LH = HF / 4, SLOTS = 5, SC = 4;      // fragments of a half, requests per wave and half; chunks' scales
+    u32x4 mem[SLOTS * HF * 64 + (L::Q8 ? SC * 8 : 0)];      // (bf16 at head dim 128: two of them are a unit's whole LDS)
+    __device__ __forceinline__ u32x4* ring(int i) { return mem + i * HF * 64; }
+    __device__ __forceinline__ u32x4* scales(int i) { return mem + SLOTS * HF * 64 + i * 8; }
+};
+template <class C, int H, int NT>
+__global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
+    using A = BF16;
+    using L = KvLayout<C, H>;
+    using Lds = KvRowsLds<C, H, NT>;
+    constexpr int AE = A::KE, KK = L::KK, HP = L::HP, US = KK / AE, QS = HP * US, HT = L::HT, KST = L::KST, VS = L::KV / AE, PS = KST * VS;
+    constexpr int HF = Lds::HF, LH = Lds::LH, SLOTS = Lds::SLOTS, SC = Lds::SC, X = L::Q8 ? 1 : 0;
+    static_assert(HF % 4 == 0, "every wave asks for the same number of fragments");
+    __shared__ Lds lds;
+    const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), g = lane >> 4, m = lane & 15;
+    int seq, local;
+    int64_t first;
+    KvSeq s;
+    if (blockIdx.x == 0 && w == 0) kv_check_all(a.kv, lane);
+    const int run = kv_run<4 * NT>(a, lane), n_kv = a.kv.n_kv;
+    if (!kv_find(a.kv, blockIdx.x, lane, [&](const KvSeq& v) { return kv_tiles<4 * NT>(a.kv, v) * kv_splits(v, run) * n_kv; }, &seq, &local, &first, &s)) return;
+    const int n_tiles = kv_tiles<4 * NT>(a.kv, s), n_splits = kv_splits(s, run);
+    const int kvh = local % n_kv, tile = n_tiles - 1 - local / n_kv % n_tiles, split = local / n_kv / n_tiles;      // longest first
+    const int rows = s.n * a.kv.group, base = s.len - s.n, row0 = (tile * 4 + w) * NT * 16;
+    int pos[NT];
+    u32x4 qf[NT][QS];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int row = row0 + t * 16 + m, token = row / a.kv.group, head = kvh * a.kv.group + row % a.kv.group;
+        const bool on = row < rows;
+        pos[t] = on ? base + token : -1;
+        const uint16_t* qp = (const uint16_t*)a.q + (s.r0 + (int64_t)token) * a.q_stride + head * H;
+#pragma unroll
+        for (int i = 0; i < QS; ++i) qf[t][i] = on ? *(const u32x4*)(qp + i / US * 4 * KK + g * KK + i % US * AE) : u32x4{0u, 0u, 0u, 0u};
+    }
+    auto chunks_of = [&](int row_end) { return (base + (min(row_end, rows) - 1) / a.kv.group + 64) / 64; };      // chunks that rows up to there see
+    const int c0 = split * run, c_end = min(chunks_of((tile + 1) * 64 * NT), c0 + run);                         // ... of the workgroup
+    const int c_my = row0 < rows ? min(chunks_of(row0 + 16 * NT), c_end) : 0;                                   // ... of this wave
+    const int from = base + row0 / a.kv.group;
+    bool odd = false;
+    uint32_t gone = 0;                                   // bit c % 32: chunk c has no page
+    // half i of the run: K (i even) or V^T of chunk c0 + i / 2; past the end the last one is asked for again
+    const int n_halves = 2 * (c_end - c0);
+    const char* src = nullptr;
+    auto issue = [&](const int i_) {
+        const int i = min(i_, n_halves - 2 + (i_ & 1)), c = c0 + (i >> 1);
+        if (!(i & 1)) {                                  // (the V^T half that follows is of the same chunk)
+            typedef const __attribute__((address_space(4))) int32_t* const_i32_ptr;
+            const int per = a.kv.page_tokens / 64;
+            const int page = ((const_i32_ptr)(uintptr_t)a.kv.table)[(size_t)seq * a.kv.table_stride + c / per];
+            const bool ok = (unsigned)page < (unsigned)a.kv.n_pages;
+            src = ok ? a.kv.pages + (((size_t)page * n_kv + kvh) * per + c % per) * L::CHUNK : nullptr;
+            gone = ok ? gone & ~(1u << (c & 31)) : gone | 1u << (c & 31);
+            if (!ok && tid == 0) kv_flag(a.kv, ASD_KV_BAD_PAGE);
+        }
+        const uint32_t bytes = src ? 0xffffffffu : 0u;
+        u32x4* slot = lds.ring(i_ % SLOTS);
+#pragma unroll
+        for (int q = 0; q < LH; ++q) frag_to_lds(src + (i & 1) * L::K_BYTES + (w + 4 * q) * 1024, bytes, slot + (w + 4 * q) * 64, lane);
+        if constexpr (L::Q8)
+            if (!(i_ & 1) && lane < 8) frag_to_lds(src + 2 * L::K_BYTES, src ? 128u : 0u, lds.scales((i_ >> 1) % SC), lane);
+    };
+    f32x4 o[NT][HT];
+    float mx[NT], l[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        mx[t] = -INFINITY; l[t] = 0.f;
+#pragma unroll
+        for (int ht = 0; ht < HT; ++ht) o[t][ht] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    wait_vm<0, true>();                                  // from here on only the ring's requests count
+    if (n_halves > 0) {
+#pragma unroll
+        for (int i = 0; i < SLOTS - 1; ++i) issue(i);
+    }
+    static_assert(SLOTS == 5, "the waits below");
+    auto step = [&](const int i, auto k_half) {          // behind half i there are three: V K V, or K V K
+        wait_vm<3 * LH + (decltype(k_half)::value ? X : 2 * X), true>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        issue(i + SLOTS - 1);
+    };
+    for (int c = c0; c < c_end; ++c) {
+        const int i = 2 * (c - c0);
+        u32x4 pf[NT][PS];
+        step(i, std::true_type{});
+        const bool mine = c < c_my && !((gone >> (c & 31)) & 1u);
+        const bool edge = c * 64 + 63 > from;
+        if (mine) {
+            f32x4 sc[NT][4];
+            const u32x4* kp = lds.ring(i % SLOTS);
+            const uint8_t* ex = (const uint8_t*)lds.scales((i >> 1) % SC);
+            u32x4 ke{}, ve{};
+            if constexpr (L::Q8) { ke = *(const u32x4*)(ex + 16 * (m >> 2)); ve = *(const u32x4*)(ex + 64 + 16 * g); }
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+                float scale = 1.f;
+                if constexpr (L::Q8) scale = q8_scale((ke[kt] >> (8 * (m & 3))) & 255u);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) sc[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int hp = 0; hp < HP; ++hp) {
+                    const u32x4 piece = kp[(kt * HP + hp) * 64 + lane];
+#pragma unroll
+                    for (int u = 0; u < US; ++u) {
+                        const u32x4 x = kv_operand<A, C>(piece, u, scale);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) mma16<A>(sc[t][kt], x, qf[t][hp * US + u]);
+                    }
+                }
+            }
+            float vs[4][4];
+            if constexpr (L::Q8)
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) vs[kt][j] = q8_scale((ve[kt] >> (8 * j)) & 255u);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                if (edge) {
+#pragma unroll
+                    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (c * 64 + score_key<C>(kt, 4 * g + j) > pos[t]) sc[t][kt][j] = -INFINITY;
+                }
+                float cm = sc[t][0][0];
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) cm = fmaxf(cm, sc[t][kt][j]);
+                cm = fmaxf(cm, __shfl_xor(cm, 16));
+                cm = fmaxf(cm, __shfl_xor(cm, 32));
+                if (__any(cm > mx[t])) {
+                    const float mn = fmaxf(mx[t], cm), alpha = mn == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mx[t] - mn) * a.c2);
+                    mx[t] = mn;
+                    l[t] *= alpha;
+#pragma unroll
+                    for (int ht = 0; ht < HT; ++ht) { o[t][ht][0] *= alpha; o[t][ht][1] *= alpha; o[t][ht][2] *= alpha; o[t][ht][3] *= alpha; }
+                }
+                const float off = mx[t] == -INFINITY ? 0.f : -mx[t] * a.c2;
+                float pr[4][4];
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float e = __builtin_amdgcn_exp2f(fmaf(sc[t][kt][j], a.c2, off));
+                        l[t] += e;
+                        pr[kt][j] = e;
+                        if constexpr (L::Q8) pr[kt][j] = e * vs[kt][j];
+                    }
+                if constexpr (L::Q8)
+                    if (edge) {                          // (an unwritten scale may be anything)
+#pragma unroll
+                        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) if (c * 64 + score_key<C>(kt, 4 * g + j) > pos[t]) pr[kt][j] = 0.f;
+                    }
+#pragma unroll
+                for (int x = 0; x < PS; ++x)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) pf[t][x][y] = BF16::from_f32(pr[2 * x + y / 2][2 * (y & 1)]) | ((uint32_t)BF16::from_f32(pr[2 * x + y / 2][2 * (y & 1) + 1]) << 16);
+            }
+        }
+        step(i + 1, std::false_type{});
+        if (mine) {
+            const u32x4* vp = lds.ring((i + 1) % SLOTS);
+            if (!edge) {
+#pragma unroll
+                for (int ht = 0; ht < HT; ++ht)
+#pragma unroll
+                    for (int ks = 0; ks < KST; ++ks) {
+                        const u32x4 piece = vp[(ht * KST + ks) * 64 + lane];
+#pragma unroll
+                        for (int u = 0; u < VS; ++u) {
+                            const u32x4 v = kv_operand<A, C>(piece, u, 1.f);
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) mma16<A>(o[t][ht], v, pf[t][ks * VS + u]);
+                        }
+                    }
+            } else {                                     // keys that a row does not see: see kv_attend_kernel
+                const int n_keys = s.len - c * 64;
+                uint32_t hit = 0;
+#pragma unroll
+                for (int ht = 0; ht < HT; ++ht)
+#pragma unroll
+                    for (int ks = 0; ks < KST; ++ks) {
+                        u32x4 piece = vp[(ht * KST + ks) * 64 + lane];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const uint32_t v = piece[x] & kv_kept<C>(n_keys, ks, g, x);
+                            piece[x] = kv_clean<C>(v);
+                            hit |= v ^ piece[x];
+                        }
+#pragma unroll
+                        for (int u = 0; u < VS; ++u) {
+                            const u32x4 v = kv_operand<A, C>(piece, u, 1.f);
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) mma16<A>(o[t][ht], v, pf[t][ks * VS + u]);
+                        }
+                    }
+                if (__any(hit != 0)) odd = true;
+            }
+        }
+    }
+    wait_vm<0, true>();                                  // no request may outlive the workgroup's LDS
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        float z = l[t];
+        z += __shfl_xor(z, 16);
+        z += __shfl_xor(z, 32);
+        const int row = row0 + t * 16 + m, token = row / a.kv.group, head = kvh * a.kv.group + row % a.kv.group;
+        if (row >= rows) continue;
+        if (n_splits == 1) {
+            const float inv = z == 0.f ? 0.f : 1.f / z;
+#pragma unroll
+            for (int ht = 0; ht < HT; ++ht) {
+                const float v[4] = {o[t][ht][0] * inv, o[t][ht][1] * inv, o[t][ht][2] * inv, o[t][ht][3] * inv};
+                store4<A>((uint16_t*)a.out + (s.r0 + (int64_t)token) * a.out_stride + head * H + ht * 16 + 4 * g, v);
+            }
+        } else {
+            const size_t at = (size_t)(first + (int64_t)(split * n_tiles + tile) * n_kv + kvh) * (64 * NT) + row - tile * 64 * NT;
+#pragma unroll
+            for (int ht = 0; ht < HT; ++ht) *(f32x4*)(a.o_part + at * H + ht * 16 + 4 * g) = o[t][ht];
+            if (g == 0) { a.ml_part[at * 2] = mx[t]; a.ml_part[at * 2 + 1] = z; }
+        }
+        if (odd) {                                       // (each lane changes what it has stored)
+            const size_t at = (size_t)(first + (int64_t)(split * n_tiles + tile) * n_kv + kvh) * (64 * NT) + row - tile * 64 * NT;
+            uint16_t* out = (uint16_t*)a.out + (s.r0 + (int64_t)token) * a.out_stride + head * H;
+            for (int d = 0; d < H / 4; ++d) {
+                const int dim = d / 4 * 16 + 4 * g + d % 4;
+                const float x = kv_odd_sum<C, H>(a.kv, seq, kvh, max((from + 1) / 64, c0) * 64, min(pos[t], c_end * 64 - 1), dim);
+                if (finite(x)) continue;
+                if (n_splits == 1) out[dim] = BF16::from_f32(BF16::to_f32(out[dim]) + x); else a.o_part[at * H + dim] += x;
             }
         }
     }

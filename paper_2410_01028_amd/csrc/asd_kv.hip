@@ -87,9 +87,13 @@ int units() {
     return n;
 }
 
+#ifndef ROWS_NT
+#define ROWS_NT 2
+#endif
 // How asd_kv_attend runs a batch of these bounds
 struct AttendPlan {
     int nt;                        // 16-row column blocks of a tile
+    bool rows;                     // kv_rows_kernel
     int32_t target, max_tiles;
     int64_t grid;                  // most work items
     bool join;                     // some sequence's keys may be cut
@@ -101,7 +105,9 @@ AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b) {
     const int64_t rows = (int64_t)b->max_new * group, chunks = (kv_args(s, b).cap + 63) / 64;
     // Rows share a chunk's fragments: as many columns as the largest sequence fills, up to 64 (fp32: 32, whose operands take twice the registers)
     p.nt = rows <= 16 ? 1 : s->dtype == ASD_DT_F32 ? 2 : rows <= 32 ? 2 : 4;
-    p.target = 4 * units();
+    p.rows = s->dtype == ASD_DT_BF16 && s->head_dim >= 64 && rows > 64;
+    if (p.rows) p.nt = 4 * ROWS_NT;
+    p.target = p.rows ? 4 * units() : 4 * units();
     p.max_tiles = (int32_t)((int64_t)b->n_rows * group / (16 * p.nt) + (b->n_seqs < b->n_rows ? b->n_seqs : b->n_rows));
     const int64_t whole = (int64_t)p.max_tiles * s->n_kv_heads;
     p.join = chunks > 4;
@@ -188,7 +194,12 @@ int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, i
         if (p.join) kv_join_kernel<decltype(t), h.value, nt.value><<<(unsigned)(((int64_t)b->n_rows * s->n_heads + 3) / 4), 256, 0, stream>>>(a);
     };
     by_shape(s, [&](auto t, auto c, auto h) {
-        if (p.nt == 1) go(t, c, h, std::integral_constant<int, 1>{});
+        if (p.rows) {
+            if constexpr (sizeof(typename decltype(t)::elem) == 2 && h.value >= 64) {
+                kv_rows_kernel<decltype(c), h.value, ROWS_NT><<<(unsigned)p.grid, 256, 0, stream>>>(a);
+                if (p.join) kv_join_kernel<decltype(t), h.value, 4 * ROWS_NT><<<(unsigned)(((int64_t)b->n_rows * s->n_heads + 3) / 4), 256, 0, stream>>>(a);
+            }
+        } else if (p.nt == 1) go(t, c, h, std::integral_constant<int, 1>{});
         else if (p.nt == 2) go(t, c, h, std::integral_constant<int, 2>{});
         else if constexpr (sizeof(typename decltype(t)::elem) == 2) go(t, c, h, std::integral_constant<int, 4>{});
     });
