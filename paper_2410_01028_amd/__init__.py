@@ -437,22 +437,17 @@ def kv_page_bytes(n_heads: int, n_kv_heads: int, head_dim: int, page_tokens: int
     return n
 
 
-class _OnDevice:
-    """Makes a tensor's device the current one for the time of a call."""
-
-    def __init__(self, device):
-        import torch
-        self._torch, self._index = torch, device.index
-
-    def __enter__(self):
-        self._before = self._torch.cuda.current_device()
-        if self._before != self._index:
-            self._torch.cuda.set_device(self._index)
-        return self._torch.cuda.current_stream(self._index).cuda_stream
-
-    def __exit__(self, *exc):
-        if self._before != self._index:
-            self._torch.cuda.set_device(self._before)
+def _on_device(device, call):
+    """call(stream) with `device` as the current one and its current stream, as the library's launches expect them."""
+    import torch
+    index, before = device.index, torch.cuda.current_device()
+    if before == index:
+        return call(torch.cuda.current_stream(index).cuda_stream)
+    torch.cuda.set_device(index)
+    try:
+        return call(torch.cuda.current_stream(index).cuda_stream)
+    finally:
+        torch.cuda.set_device(before)
 
 
 class KVBatch:
@@ -476,6 +471,7 @@ class KVBatch:
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._c = KvBatch(None, page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr(), self.status.data_ptr(), 0,
                           page_table.shape[1], n, n_rows, max_new, max_len)
+        self._workspace = {}                            # bytes of an attend call, by cache shape: the bounds do not change
 
     def check(self):
         """Synchronise and raise if a kernel found the arrays out of range since the last check."""
@@ -500,25 +496,28 @@ class KVCache:
         self.n_heads, self.n_kv_heads, self.head_dim = n_heads, n_kv_heads, head_dim
         self.torch_dtype = torch.bfloat16 if dtype == DT_BF16 else torch.float32
         self._shape = KvShape(n_heads, n_kv_heads, head_dim, page_tokens, dtype, kv_dtype)
-        self._torch = torch
+        self._torch, self._lib, self._scale = torch, _kv_lib(), head_dim ** -0.5
+        self._key = (n_heads, n_kv_heads, head_dim, page_tokens, dtype, kv_dtype)
+        self._pool = pages.data_ptr()
 
     def _batch(self, batch: KVBatch) -> KvBatch:
         if batch.device != self.device:
             raise AsdError(E_INVAL, "the batch is on another device than the pages")
-        b = KvBatch.from_buffer_copy(batch._c)
-        b.pages, b.n_pages = self.pages.data_ptr(), self.n_pages
+        b = KvBatch.from_buffer_copy(batch._c)          # (calls of several threads may share a batch)
+        b.pages, b.n_pages = self._pool, self.n_pages
         return b
 
     def _rows(self, name: str, t, batch: KVBatch, heads: int):
         """(pointer, row stride) of a buffer of rows [>= n_rows, heads, head_dim]; heads packed."""
-        if t.dtype != self.torch_dtype or t.device != self.device:
+        h = self.head_dim
+        if t.dtype is not self.torch_dtype or t.device != self.device:
             raise AsdError(E_INVAL, f"{name} must be {self.torch_dtype} on {self.device}")
-        if t.dim() != 3 or t.shape[0] < batch.n_rows or t.shape[1] != heads or t.shape[2] != self.head_dim:
-            raise AsdError(E_INVAL, f"{name} must be [{batch.n_rows}, {heads}, {self.head_dim}]")
-        s = t.stride()
-        if s[2] != 1 or (heads > 1 and s[1] != self.head_dim):
+        if t.dim() != 3 or t.shape[1:] != (heads, h) or t.shape[0] < batch.n_rows:
+            raise AsdError(E_INVAL, f"{name} must be [{batch.n_rows}, {heads}, {h}]")
+        row, head, one = t.stride()
+        if one != 1 or (heads > 1 and head != h):
             raise AsdError(E_INVAL, f"{name}: the heads of a row must lie packed")
-        return t.data_ptr(), s[0] if batch.n_rows > 1 else max(s[0], heads * self.head_dim)
+        return t.data_ptr(), row if batch.n_rows > 1 else max(row, heads * h)
 
     def _floats(self, name: str, t, shape):
         if t.dtype != self._torch.float32 or t.device != self.device or not t.is_contiguous() or t.dim() != len(shape) or \
@@ -545,8 +544,7 @@ class KVCache:
         qp = self._rows("q", q, batch, self.n_heads) if q is not None else (None, 0)
         op = self._rows("q_out", q_out, batch, self.n_heads) if q is not None else (None, 0)
         kp, vp = self._rows("k", k, batch, self.n_kv_heads), self._rows("v", v, batch, self.n_kv_heads)
-        with _OnDevice(self.device) as stream:
-            _kv_ck(_kv_lib().asd_kv_append(self._shape, b, prep, *qp, *kp, *vp, *op, stream))
+        _kv_ck(_on_device(self.device, lambda stream: self._lib.asd_kv_append(self._shape, b, prep, *qp, *kp, *vp, *op, stream)))
         return q_out
 
     def attend(self, batch: KVBatch, q, out=None, scale: float | None = None, workspace=None):
@@ -556,20 +554,26 @@ class KVCache:
         if out is None:
             out = self._torch.empty((q.shape[0], self.n_heads, self.head_dim), dtype=self.torch_dtype, device=self.device)
         qp, op = self._rows("q", q, batch, self.n_heads), self._rows("out", out, batch, self.n_heads)
-        L = _kv_lib()
-        need = L.asd_kv_attend_workspace(self._shape, b)
-        with _OnDevice(self.device) as stream:
-            if workspace is None and need:
+        need = batch._workspace.get(self._key)
+        if need is None:
+            need = batch._workspace[self._key] = self._lib.asd_kv_attend_workspace(self._shape, b)
+        if workspace is None:
+            wp, wn = None, 0
+            if need:
                 workspace = self._torch.empty(need, dtype=self._torch.uint8, device=self.device)
-            elif workspace is not None and (workspace.device != self.device or workspace.dtype != self._torch.uint8 or not workspace.is_contiguous()):
-                raise AsdError(E_INVAL, f"workspace must be a contiguous uint8 tensor on {self.device}")
-            wp, wn = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
-            _kv_ck(L.asd_kv_attend(self._shape, b, *qp, *op, self.head_dim ** -0.5 if scale is None else scale, wp, wn, stream))
+                wp, wn = workspace.data_ptr(), need
+        elif workspace.device != self.device or workspace.dtype != self._torch.uint8 or not workspace.is_contiguous():
+            raise AsdError(E_INVAL, f"workspace must be a contiguous uint8 tensor on {self.device}")
+        else:
+            wp, wn = workspace.data_ptr(), workspace.numel()
+        if scale is None:
+            scale = self._scale
+        _kv_ck(_on_device(self.device, lambda stream: self._lib.asd_kv_attend(self._shape, b, *qp, *op, scale, wp, wn, stream)))
         return out
 
     def attend_workspace(self, batch: KVBatch) -> int:
         """Bytes of workspace that attend() of a batch with these bounds needs."""
-        return int(_kv_lib().asd_kv_attend_workspace(self._shape, self._batch(batch)))
+        return int(self._lib.asd_kv_attend_workspace(self._shape, self._batch(batch)))
 
     def read(self, batch: KVBatch, k_out=None, v_out=None):
         """The batch's rows out of the pages as values (asd_kv_read): (k, v) [n_rows, n_kv_heads, head_dim]; new tensors where none is given."""
@@ -577,8 +581,7 @@ class KVCache:
         for name, t in (("k_out", k_out), ("v_out", v_out)):
             t = self._torch.empty((batch.n_rows, self.n_kv_heads, self.head_dim), dtype=self.torch_dtype, device=self.device) if t is None else t
             out.append((t, self._rows(name, t, batch, self.n_kv_heads)))
-        with _OnDevice(self.device) as stream:
-            _kv_ck(_kv_lib().asd_kv_read(self._shape, b, *out[0][1], *out[1][1], stream))
+        _kv_ck(_on_device(self.device, lambda stream: self._lib.asd_kv_read(self._shape, b, *out[0][1], *out[1][1], stream)))
         return out[0][0], out[1][0]
 
 
@@ -596,7 +599,7 @@ def rope_table(rot_dim: int, positions: int, theta: float = 10000.0, kind: int =
         device = torch.device("cuda", torch.cuda.current_device())
     if positions < 1 or rot_dim < 2:
         raise AsdError(E_INVAL, "asd_rope_table: positions and rot_dim must be positive")
-    with _OnDevice(device) as stream:
-        out = torch.empty((positions, rot_dim // 2, 2), dtype=torch.float32, device=device)
-        _kv_ck(_kv_lib().asd_rope_table(Rope(kind, rot_dim, theta, factor, low, high, trained, gain), positions, out.data_ptr(), stream))
+    out = torch.empty((positions, rot_dim // 2, 2), dtype=torch.float32, device=device)
+    rope = Rope(kind, rot_dim, theta, factor, low, high, trained, gain)
+    _kv_ck(_on_device(device, lambda stream: _kv_lib().asd_rope_table(rope, positions, out.data_ptr(), stream)))
     return out

@@ -58,41 +58,50 @@ __device__ __forceinline__ KvSeq kv_seq(const KvArgs& a, int s, bool* bad = null
     return v;
 }
 __device__ __forceinline__ void kv_flag(const KvArgs& a, int bit) { if (a.status) atomicOr(a.status, bit); }
-// every sequence's arrays, by one wave
-__device__ __forceinline__ void kv_check_all(const KvArgs& a, int lane) {
-    if (!a.status) return;
-    for (int s = lane; s < a.n_seqs; s += 64) {
-        bool bad;
-        kv_seq(a, s, &bad);
-        if (bad) kv_flag(a, ASD_KV_BAD_ROWS);
-    }
-}
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// Work items of all sequences one behind the other: count(sequence) items each.  Finds the sequence of `item` and its
-// number within it; a wave looks at 64 sequences at a time, so no list has to be built in a launch of its own.
-template <class F>
-__device__ __forceinline__ bool kv_find(const KvArgs& a, int64_t item, int lane, F count, int* seq, int* local, int64_t* first, KvSeq* view) {
-    int64_t base = 0;
-    for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-        KvSeq v{0, 0, 0};
-        int c = 0;
-        if (s0 + lane < a.n_seqs) { v = kv_seq(a, s0 + lane); c = count(v); }
-        int incl = c;
+// A wave's view of the batch, 64 sequences at a time: the first 64 stay in registers.  check: the wave reports arrays out of range.
+struct KvLanes {
+    KvSeq v;
+    __device__ __forceinline__ void load(const KvArgs& a, int s0, int lane, bool check) {
+        v = KvSeq{0, 0, 0};
+        bool bad = false;
+        if (s0 + lane < a.n_seqs) v = kv_seq(a, s0 + lane, &bad);
+        if (check && bad) kv_flag(a, ASD_KV_BAD_ROWS);
+    }
+};
+__device__ __forceinline__ int wave_sum_upto(int c, int lane) {          // inclusive
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) { const int t = __shfl_up(incl, o); if (lane >= o) incl += t; }
-        const int total = uniform(__shfl(incl, 63));
+    for (int o = 1; o < 64; o <<= 1) { const int t = __shfl_up(c, o); if (lane >= o) c += t; }
+    return c;
+}
+// Work items of all sequences one behind the other: count(sequence) items each.  Finds the sequence of `item`, its
+// number within it and the first item of the sequence; each wave counts for itself, so no list has to be built in a launch of its own.
+template <class F>
+__device__ __forceinline__ bool kv_find(const KvArgs& a, KvLanes x, int64_t item, int lane, bool check, F count, int* seq, int* local, int64_t* first, KvSeq* view) {
+    int64_t base = 0;
+    for (int s0 = 0;;) {
+        const int c = count(x.v);
+        if (a.n_seqs == 1) {                            // (nothing to add up)
+            *seq = 0; *first = 0; *local = (int)item;
+            *view = KvSeq{uniform(x.v.r0), uniform(x.v.n), uniform(x.v.len)};
+            return item < uniform(c);
+        }
+        const int incl = wave_sum_upto(c, lane), total = uniform(__shfl(incl, 63));
         if (item < base + total) {
             const int l = __ffsll((unsigned long long)__ballot(base + incl > item)) - 1;
             *seq = uniform(s0 + l);
             *first = base + uniform(__shfl(incl - c, l));
             *local = (int)(item - *first);
-            *view = KvSeq{uniform(__shfl(v.r0, l)), uniform(__shfl(v.n, l)), uniform(__shfl(v.len, l))};
+            *view = KvSeq{uniform(__shfl(x.v.r0, l)), uniform(__shfl(x.v.n, l)), uniform(__shfl(x.v.len, l))};
+            if (check) for (s0 += 64; s0 < a.n_seqs; s0 += 64) x.load(a, s0, lane, true);
             return true;
         }
         base += total;
+        s0 += 64;
+        if (s0 >= a.n_seqs) return false;
+        x.load(a, s0, lane, check);
     }
-    return false;
 }
 // Chunk c of a sequence for one KV head; null where the page table holds no page of the pool
 template <class C, int H>
@@ -224,8 +233,10 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
     int64_t first;
     KvSeq s;
     auto tiles = [](const KvSeq& v) { const int p0 = max(v.len - v.n, 0); return v.n > 0 && v.len > 0 ? (v.len + 15) / 16 - p0 / 16 : 0; };
-    if (blockIdx.x == 0 && blockIdx.y == 0 && tid < 64) kv_check_all(a.kv, lane);
-    if (!kv_find(a.kv, blockIdx.x, lane, tiles, &seq, &tile, &first, &s)) return;
+    const bool check = blockIdx.x == 0 && blockIdx.y == 0 && tid < 64;
+    KvLanes all;
+    all.load(a.kv, 0, lane, check);
+    if (!kv_find(a.kv, all, blockIdx.x, lane, check, tiles, &seq, &tile, &first, &s)) return;
     const int base = s.len - s.n;                      // position of row 0 (negative: rows in front have no place)
     const int t16 = max(base, 0) / 16 + tile;
     const int lo = max(max(base, 0), 16 * t16), hi = min(s.len, 16 * t16 + 16), nt = hi - lo;
@@ -329,14 +340,16 @@ __global__ __launch_bounds__(256) void kv_read_kernel(const KvReadArgs a) {
     __shared__ __align__(16) E rows[64][H + PAD];
     const int tid = threadIdx.x, lane = tid & 63, kvh = blockIdx.y;
     const bool isv = blockIdx.z != 0;
-    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && tid < 64) kv_check_all(a.kv, lane);
     E* out = (E*)(isv ? a.v_out : a.k_out);
     if (!out) return;
     int seq, local;
     int64_t first;
     KvSeq s;
     auto chunks = [](const KvSeq& v) { return v.n > 0 && v.len > 0 ? (v.len + 63) / 64 - max(v.len - v.n, 0) / 64 : 0; };
-    if (!kv_find(a.kv, blockIdx.x, lane, chunks, &seq, &local, &first, &s)) return;
+    const bool check = blockIdx.x == 0 && blockIdx.y == 0 && tid < 64;
+    KvLanes all;
+    all.load(a.kv, 0, lane, check);
+    if (!kv_find(a.kv, all, blockIdx.x, lane, check, chunks, &seq, &local, &first, &s)) return;
     const int base = s.len - s.n, c = max(base, 0) / 64 + local;
     const int lo = max(max(base, 0) - 64 * c, 0), hi = min(s.len - 64 * c, 64);      // keys of the chunk that are wanted
     const char* chunk = kv_chunk<C, H>(a.kv, seq, c, kvh);
@@ -400,22 +413,23 @@ struct KvAttendArgs {
     int64_t q_stride, out_stride;
     float c2;                       // scale * log2(e)
     float *o_part, *ml_part;        // [item][rows of a tile][H] unnormalised sums; [item][rows][2] (maximum, sum)
-    int32_t target;                 // work items to cut the batch into
-    int32_t max_tiles;              // tiles a batch of these bounds can have: with target, the places in the workspace
+    int32_t target_log2;            // work items to cut the batch into
+    int32_t cut;                    // 0: every tile's keys stay together
 };
 // How a batch is cut.  The rows of a sequence and KV head are its new tokens x the heads of the group; a tile is 16 * NT of
-// them.  All tiles' key ranges are cut into runs of `run` chunks, the same for every sequence, so that about `target` items come out
+// them.  With `cut`, all tiles' key ranges are cut into runs of `run` chunks, the same for every sequence, so that about 2^target_log2 items come out
 // whatever the lengths are: one long conversation among short ones is spread over the card.
 template <int NT> __device__ __forceinline__ int kv_tiles(const KvArgs& a, const KvSeq& v) { return (int)(((int64_t)v.n * a.group + 16 * NT - 1) / (16 * NT)); }
-template <int NT> __device__ __forceinline__ int kv_run(const KvAttendArgs& a, int lane) {
-    int64_t t = 0;
-    for (int s = lane; s < a.kv.n_seqs; s += 64) {
-        const KvSeq v = kv_seq(a.kv, s);
-        t += (int64_t)kv_tiles<NT>(a.kv, v) * ((v.len + 63) / 64);
-    }
+template <int NT> __device__ __forceinline__ int kv_run(const KvAttendArgs& a, const KvLanes& all, int lane) {
+    if (!a.cut) return 1 << 28;
+    auto units = [&](const KvSeq& v) { return (int64_t)kv_tiles<NT>(a.kv, v) * ((v.len + 63) / 64); };
+    int64_t t = units(all.v);
+    for (int s = lane + 64; s < a.kv.n_seqs; s += 64) t += units(kv_seq(a.kv, s));
+    if (a.kv.n_seqs > 1) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);
-    const int64_t run = (t * a.kv.n_kv + a.target - 1) / a.target;
+        for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);
+    }
+    const int64_t run = ((t * a.kv.n_kv - 1) >> a.target_log2) + 1;
     return uniform((int)min(max(run + 3, (int64_t)4) / 4 * 4, (int64_t)1 << 28));
 }
 __device__ __forceinline__ int kv_splits(const KvSeq& v, int run) { return max(1, ((v.len + 63) / 64 + run - 1) / run); }
@@ -468,11 +482,12 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
     int seq, local;
     int64_t first;
     KvSeq s;
-    if (blockIdx.x == 0 && w == 0) kv_check_all(a.kv, lane);
     if (tid == 0) s_odd = 0;
-    const int run = kv_run<NT>(a, lane);
-    const int n_kv = a.kv.n_kv;
-    if (!kv_find(a.kv, blockIdx.x, lane, [&](const KvSeq& v) { return kv_tiles<NT>(a.kv, v) * kv_splits(v, run) * n_kv; }, &seq, &local, &first, &s)) return;
+    const bool check = blockIdx.x == 0 && w == 0;
+    KvLanes all;
+    all.load(a.kv, 0, lane, check);
+    const int run = kv_run<NT>(a, all, lane), n_kv = a.kv.n_kv;
+    if (!kv_find(a.kv, all, blockIdx.x, lane, check, [&](const KvSeq& v) { return kv_tiles<NT>(a.kv, v) * kv_splits(v, run) * n_kv; }, &seq, &local, &first, &s)) return;
     const int n_tiles = kv_tiles<NT>(a.kv, s), n_splits = kv_splits(s, run);
     const int kvh = local % n_kv, tile = local / n_kv % n_tiles, split = local / n_kv / n_tiles;
     const int rows = s.n * a.kv.group, base = s.len - s.n;
@@ -708,9 +723,11 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
     int seq, local;
     int64_t first;
     KvSeq s;
-    if (blockIdx.x == 0 && w == 0) kv_check_all(a.kv, lane);
-    const int run = kv_run<4 * NT>(a, lane), n_kv = a.kv.n_kv;
-    if (!kv_find(a.kv, blockIdx.x, lane, [&](const KvSeq& v) { return kv_tiles<4 * NT>(a.kv, v) * kv_splits(v, run) * n_kv; }, &seq, &local, &first, &s)) return;
+    const bool check = blockIdx.x == 0 && w == 0;
+    KvLanes all;
+    all.load(a.kv, 0, lane, check);
+    const int run = kv_run<4 * NT>(a, all, lane), n_kv = a.kv.n_kv;
+    if (!kv_find(a.kv, all, blockIdx.x, lane, check, [&](const KvSeq& v) { return kv_tiles<4 * NT>(a.kv, v) * kv_splits(v, run) * n_kv; }, &seq, &local, &first, &s)) return;
     const int n_tiles = kv_tiles<4 * NT>(a.kv, s), n_splits = kv_splits(s, run);
     const int kvh = local % n_kv, tile = n_tiles - 1 - local / n_kv % n_tiles, split = local / n_kv / n_tiles;      // longest first
     const int rows = s.n * a.kv.group, base = s.len - s.n, row0 = (tile * 4 + w) * NT * 16;
@@ -930,80 +947,97 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
     }
 }
 
-// Joins the runs of every row whose keys were cut: a wave per row and head, runs in ascending order.
+// Joins the runs of tiles whose keys were cut: a workgroup per tile, KV head and 16 of its rows.  16 lanes hold a row's dims;
+// where fewer rows are in use than 16, the lanes left over take every second (fourth, ..) run, added up through LDS at the end.
 template <class A, int H, int NT>
 __global__ __launch_bounds__(256) void kv_join_kernel(const KvAttendArgs a) {
     using E = typename A::elem;
-    const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6);
-    const int run = kv_run<NT>(a, lane), n_kv = a.kv.n_kv, group = a.kv.group;
-    int64_t base = 0, first = 0;                        // (rows x heads) and work items of the sequences in front
-    KvSeq s{0, 0, 0};
-    int seq = -1;
-    for (int s0 = 0; s0 < a.kv.n_seqs && seq < 0; s0 += 64) {
-        KvSeq v{0, 0, 0};
-        if (s0 + lane < a.kv.n_seqs) v = kv_seq(a.kv, s0 + lane);
-        const int cr = v.n * a.kv.n_h, cw = v.n ? kv_tiles<NT>(a.kv, v) * kv_splits(v, run) * n_kv : 0;
-        int ir = cr, iw = cw;
+    constexpr int R = 16 * NT, DL = H / 16, U = 8;      // rows of a tile, dims of a lane, runs in flight
+    __shared__ float so[16][H];
+    __shared__ float sml[16][2];
+    const int tid = threadIdx.x, lane = tid & 63, n_kv = a.kv.n_kv, group = a.kv.group;
+    int seq, local;
+    int64_t first;
+    KvSeq s;
+    KvLanes all;
+    all.load(a.kv, 0, lane, false);
+    const int run = kv_run<NT>(a, all, lane);
+    // (tile, KV head) pairs of the cut sequences
+    if (!kv_find(a.kv, all, blockIdx.x, lane, false, [&](const KvSeq& v) { return kv_splits(v, run) > 1 ? kv_tiles<NT>(a.kv, v) * n_kv : 0; }, &seq, &local, &first, &s)) return;
+    // the first work item of the sequence
+    int64_t item0 = 0;
+    for (int s0 = 0; s0 <= seq; s0 += 64) {
+        if (s0) all.load(a.kv, s0, lane, false);
+        int64_t c = s0 + lane < seq ? (int64_t)kv_tiles<NT>(a.kv, all.v) * kv_splits(all.v, run) * n_kv : 0;
+        if (seq)
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(ir, o), y = __shfl_up(iw, o);
-            if (lane >= o) { ir += x; iw += y; }
-        }
-        const int tr = uniform(__shfl(ir, 63)), tw = uniform(__shfl(iw, 63));
-        if (item < base + tr) {
-            const int at = __ffsll((unsigned long long)__ballot(base + ir > item)) - 1;
-            seq = s0 + at;
-            base += uniform(__shfl(ir - cr, at));
-            first += uniform(__shfl(iw - cw, at));
-            s = KvSeq{uniform(__shfl(v.r0, at)), uniform(__shfl(v.n, at)), uniform(__shfl(v.len, at))};
-        } else { base += tr; first += tw; }
+            for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o);
+        item0 += c;
     }
-    if (seq < 0) return;
-    const int n_splits = kv_splits(s, run);
-    if (n_splits == 1) return;
-    const int local = (int)(item - base), token = local / a.kv.n_h, head = local % a.kv.n_h, kvh = head / group;
-    const int row = token * group + head % group, tile = row / (16 * NT), n_tiles = kv_tiles<NT>(a.kv, s);
-    const int64_t step = (int64_t)n_tiles * n_kv * (16 * NT);       // a run's place to the next run's
-    const int64_t at = (first + (int64_t)tile * n_kv + kvh) * (16 * NT) + row % (16 * NT);
-    const float* ml = a.ml_part + at * 2;
-    float top = -INFINITY;
-    for (int i = lane; i < n_splits; i += 64) top = fmaxf(top, ml[i * step * 2]);
+    const int n_splits = kv_splits(s, run), n_tiles = kv_tiles<NT>(a.kv, s), kvh = local % n_kv, tile = local / n_kv;
+    const int row0 = tile * R + blockIdx.y * 16, left = min(s.n * group - row0, 16);
+    if (left <= 0) return;
+    const int lg = left > 8 ? 4 : left > 4 ? 3 : left > 2 ? 2 : left > 1 ? 1 : 0, phases = 16 >> lg;
+    const int r = (tid >> 4) & ((1 << lg) - 1), phase = tid >> (4 + lg), d0 = (tid & 15) * DL;
+    const int64_t step = (int64_t)n_tiles * n_kv * R, at = (item0 + (int64_t)tile * n_kv + kvh) * R + blockIdx.y * 16 + r;      // a run's place to the next run's
+    float acc[DL] = {}, top = -INFINITY, sum = 0.f;
+    if (r < left)
+        for (int i0 = phase; i0 < n_splits; i0 += U * phases) {
+            float x[U][DL];
+            float2 ml[U];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float ref = top == -INFINITY ? 0.f : top;
-    constexpr int DL = H / 64 > 0 ? H / 64 : 1, U = 8;              // dims of a lane, runs in flight
-    float acc[DL] = {}, sum = 0.f;
-    const bool mine = lane * DL < H;
-    const float* op = a.o_part + at * H + lane * DL;
-    for (int i0 = 0; i0 < n_splits; i0 += U) {
-        float x[U][DL], wm[U], ws[U];
+            for (int u = 0; u < U; ++u) {
+                const bool on = i0 + u * phases < n_splits;
+                const int64_t p = at + (on ? i0 + u * phases : i0) * step;
+                ml[u] = *(const float2*)(a.ml_part + p * 2);
+                if (!on) ml[u] = float2{-INFINITY, 0.f};
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const bool on = i0 + u < n_splits;
-            const int64_t r = (on ? i0 + u : i0) * step;
-            wm[u] = on ? ml[r * 2] : -INFINITY;
-            ws[u] = ml[r * 2 + 1];
+                for (int d = 0; d < DL; d += 2) { const float2 y = *(const float2*)(a.o_part + p * H + d0 + d); x[u][d] = y.x; x[u][d + 1] = y.y; }
+            }
+            float mn = top;
 #pragma unroll
-            for (int d = 0; d < DL; ++d) x[u][d] = mine ? op[r * H + d] : 0.f;
-        }
+            for (int u = 0; u < U; ++u) mn = fmaxf(mn, ml[u].x);
+            const float ref = mn == -INFINITY ? 0.f : mn, alpha = __builtin_amdgcn_exp2f((top - ref) * a.c2);
+            top = mn;
+            sum *= alpha;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const float wt = __builtin_amdgcn_exp2f((wm[u] - ref) * a.c2);
-            if (i0 + u < n_splits) {
-                sum += ws[u] * wt;
+            for (int d = 0; d < DL; ++d) acc[d] *= alpha;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (i0 + u * phases >= n_splits) break;
+                const float wt = __builtin_amdgcn_exp2f((ml[u].x - ref) * a.c2);
+                sum += ml[u].y * wt;
 #pragma unroll
                 for (int d = 0; d < DL; ++d) acc[d] += x[u][d] * wt;
             }
         }
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    if (!mine) return;
-    E* out = (E*)a.out + (s.r0 + (int64_t)token) * a.out_stride + head * H + lane * DL;
-    if constexpr (DL == 2 && sizeof(E) == 2) *(uint32_t*)out = A::from_f32(acc[0] * inv) | ((uint32_t)A::from_f32(acc[1] * inv) << 16);
-    else {
+    if (phases > 1) {
 #pragma unroll
-        for (int d = 0; d < DL; ++d) out[d] = A::from_f32(acc[d] * inv);
+        for (int d = 0; d < DL; ++d) so[tid >> 4][d0 + d] = acc[d];
+        if ((tid & 15) == 0) { sml[tid >> 4][0] = top; sml[tid >> 4][1] = sum; }
+        __syncthreads();
+        if (phase) return;
+        float mn = -INFINITY;
+        for (int q = 0; q < phases; ++q) mn = fmaxf(mn, sml[(q << lg) + r][0]);
+        const float ref = mn == -INFINITY ? 0.f : mn;
+        sum = 0.f;
+#pragma unroll
+        for (int d = 0; d < DL; ++d) acc[d] = 0.f;
+        for (int q = 0; q < phases; ++q) {
+            const float wt = __builtin_amdgcn_exp2f((sml[(q << lg) + r][0] - ref) * a.c2);
+            sum += sml[(q << lg) + r][1] * wt;
+#pragma unroll
+            for (int d = 0; d < DL; ++d) acc[d] += so[(q << lg) + r][d0 + d] * wt;
+        }
+    }
+    if (r >= left) return;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int row = row0 + r, token = row / group, head = kvh * group + row % group;
+    E* out = (E*)a.out + (s.r0 + (int64_t)token) * a.out_stride + head * H + d0;
+#pragma unroll
+    for (int d = 0; d < DL; d += 2) {
+        if constexpr (sizeof(E) == 2) *(uint32_t*)(out + d) = A::from_f32(acc[d] * inv) | ((uint32_t)A::from_f32(acc[d + 1] * inv) << 16);
+        else *(float2*)(out + d) = float2{acc[d] * inv, acc[d + 1] * inv};
     }
 }
 

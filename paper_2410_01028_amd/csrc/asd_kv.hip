@@ -94,7 +94,7 @@ int units() {
 struct AttendPlan {
     int nt;                        // 16-row column blocks of a tile
     bool rows;                     // kv_rows_kernel
-    int32_t target, max_tiles;
+    int32_t target_log2, max_tiles;
     int64_t grid;                  // most work items
     bool join;                     // some sequence's keys may be cut
     size_t o_bytes, bytes;
@@ -107,11 +107,14 @@ AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b) {
     p.nt = rows <= 16 ? 1 : s->dtype == ASD_DT_F32 ? 2 : rows <= 32 ? 2 : 4;
     p.rows = s->dtype == ASD_DT_BF16 && s->head_dim >= 64 && rows > 64;
     if (p.rows) p.nt = 4 * ROWS_NT;
-    p.target = p.rows ? 4 * units() : 4 * units();
+    p.target_log2 = 0;
+    while ((2 << p.target_log2) <= 4 * units()) ++p.target_log2;
+    const int64_t target = (int64_t)1 << p.target_log2;
     p.max_tiles = (int32_t)((int64_t)b->n_rows * group / (16 * p.nt) + (b->n_seqs < b->n_rows ? b->n_seqs : b->n_rows));
     const int64_t whole = (int64_t)p.max_tiles * s->n_kv_heads;
-    p.join = chunks > 4;
-    p.grid = whole + p.target;
+    // No cut where the tiles alone are work enough for every compute unit, or the keys are too few
+    p.join = chunks > 4 && !(p.rows && whole >= target);
+    p.grid = p.join ? whole + target : whole;
     if (whole * ((chunks + 3) / 4) < p.grid) p.grid = whole * ((chunks + 3) / 4);
     if (p.join) {
         p.o_bytes = ((size_t)p.grid * 16 * p.nt * s->head_dim * 4 + 255) / 256 * 256;
@@ -187,17 +190,18 @@ int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, i
     a.q = q; a.out = out; a.q_stride = q_stride; a.out_stride = out_stride;
     a.c2 = (float)((double)scale * 1.4426950408889634074);
     a.o_part = (float*)workspace; a.ml_part = (float*)((char*)workspace + p.o_bytes);
-    a.target = p.target; a.max_tiles = p.max_tiles;
+    a.target_log2 = p.target_log2; a.cut = p.join;
     const hipStream_t stream = (hipStream_t)hip_stream;
+    const dim3 join_grid((unsigned)((int64_t)p.max_tiles * s->n_kv_heads), p.nt);
     auto go = [&](auto t, auto c, auto h, auto nt) {
         kv_attend_kernel<decltype(t), decltype(c), h.value, nt.value><<<(unsigned)p.grid, 256, 0, stream>>>(a);
-        if (p.join) kv_join_kernel<decltype(t), h.value, nt.value><<<(unsigned)(((int64_t)b->n_rows * s->n_heads + 3) / 4), 256, 0, stream>>>(a);
+        if (p.join) kv_join_kernel<decltype(t), h.value, nt.value><<<join_grid, 256, 0, stream>>>(a);
     };
     by_shape(s, [&](auto t, auto c, auto h) {
         if (p.rows) {
             if constexpr (sizeof(typename decltype(t)::elem) == 2 && h.value >= 64) {
                 kv_rows_kernel<decltype(c), h.value, ROWS_NT><<<(unsigned)p.grid, 256, 0, stream>>>(a);
-                if (p.join) kv_join_kernel<decltype(t), h.value, 4 * ROWS_NT><<<(unsigned)(((int64_t)b->n_rows * s->n_heads + 3) / 4), 256, 0, stream>>>(a);
+                if (p.join) kv_join_kernel<decltype(t), h.value, 4 * ROWS_NT><<<join_grid, 256, 0, stream>>>(a);
             }
         } else if (p.nt == 1) go(t, c, h, std::integral_constant<int, 1>{});
         else if (p.nt == 2) go(t, c, h, std::integral_constant<int, 2>{});
