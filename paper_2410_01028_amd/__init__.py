@@ -440,12 +440,12 @@ def kv_page_bytes(n_heads: int, n_kv_heads: int, head_dim: int, page_tokens: int
 def _on_device(device, call):
     """call(stream) with `device` as the current one and its current stream, as the library's launches expect them."""
     import torch
-    index, before = device.index, torch.cuda.current_device()
+    index, before = device.index, torch._C._cuda_getDevice()
     if before == index:
-        return call(torch.cuda.current_stream(index).cuda_stream)
+        return call(torch._C._cuda_getCurrentRawStream(index))
     torch.cuda.set_device(index)
     try:
-        return call(torch.cuda.current_stream(index).cuda_stream)
+        return call(torch._C._cuda_getCurrentRawStream(index))
     finally:
         torch.cuda.set_device(before)
 
@@ -509,20 +509,20 @@ class KVCache:
 
     def _rows(self, name: str, t, batch: KVBatch, heads: int):
         """(pointer, row stride) of a buffer of rows [>= n_rows, heads, head_dim]; heads packed."""
-        h = self.head_dim
+        h, shape = self.head_dim, t.shape
         if t.dtype is not self.torch_dtype or t.device != self.device:
             raise AsdError(E_INVAL, f"{name} must be {self.torch_dtype} on {self.device}")
-        if t.dim() != 3 or t.shape[1:] != (heads, h) or t.shape[0] < batch.n_rows:
+        if len(shape) != 3 or shape[0] < batch.n_rows or shape[1] != heads or shape[2] != h:
             raise AsdError(E_INVAL, f"{name} must be [{batch.n_rows}, {heads}, {h}]")
         row, head, one = t.stride()
         if one != 1 or (heads > 1 and head != h):
             raise AsdError(E_INVAL, f"{name}: the heads of a row must lie packed")
         return t.data_ptr(), row if batch.n_rows > 1 else max(row, heads * h)
 
-    def _floats(self, name: str, t, shape):
-        if t.dtype != self._torch.float32 or t.device != self.device or not t.is_contiguous() or t.dim() != len(shape) or \
-                any(w is not None and n != w for n, w in zip(t.shape, shape)):
-            raise AsdError(E_INVAL, f"{name} must be a contiguous float32 tensor {list(shape)} on {self.device}")
+    def _floats(self, name: str, t, *shape):
+        """Pointer of a float32 tensor whose last dimensions are `shape`."""
+        if t.dtype is not self._torch.float32 or t.device != self.device or not t.is_contiguous() or t.shape[-len(shape):] != shape:
+            raise AsdError(E_INVAL, f"{name} must be a contiguous float32 tensor [.., {', '.join(map(str, shape))}] on {self.device}")
         return t.data_ptr()
 
     def append(self, batch: KVBatch, q, k, v, q_out=None, rope=None, rot_dim: int = 0, interleaved: bool = False, q_gain=None, k_gain=None,
@@ -536,11 +536,11 @@ class KVCache:
         if q is not None and q_out is None:
             q_out = self._torch.empty((q.shape[0], self.n_heads, self.head_dim), dtype=self.torch_dtype, device=self.device)
         if rope is not None:
-            prep.rope, prep.rope_positions = self._floats("rope", rope, (None, rot_dim // 2, 2)), rope.shape[0]
+            prep.rope, prep.rope_positions = self._floats("rope", rope, rot_dim // 2, 2), rope.shape[0]
         if q_gain is not None:
-            prep.q_gain = self._floats("q_gain", q_gain, (self.head_dim,))
+            prep.q_gain = self._floats("q_gain", q_gain, self.head_dim)
         if k_gain is not None:
-            prep.k_gain = self._floats("k_gain", k_gain, (self.head_dim,))
+            prep.k_gain = self._floats("k_gain", k_gain, self.head_dim)
         qp = self._rows("q", q, batch, self.n_heads) if q is not None else (None, 0)
         op = self._rows("q_out", q_out, batch, self.n_heads) if q is not None else (None, 0)
         kp, vp = self._rows("k", k, batch, self.n_kv_heads), self._rows("v", v, batch, self.n_kv_heads)

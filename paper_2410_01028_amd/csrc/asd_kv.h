@@ -414,6 +414,7 @@ struct KvAttendArgs {
     float c2;                       // scale * log2(e)
     float *o_part, *ml_part;        // [item][rows of a tile][H] unnormalised sums; [item][rows][2] (maximum, sum)
     int32_t target_log2;            // work items to cut the batch into
+    int32_t min_run;                // chunks that are worth a run
     int32_t cut;                    // 0: every tile's keys stay together
 };
 // How a batch is cut.  The rows of a sequence and KV head are its new tokens x the heads of the group; a tile is 16 * NT of
@@ -430,9 +431,11 @@ template <int NT> __device__ __forceinline__ int kv_run(const KvAttendArgs& a, c
         for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);
     }
     const int64_t run = ((t * a.kv.n_kv - 1) >> a.target_log2) + 1;
-    return uniform((int)min(max(run + 3, (int64_t)4) / 4 * 4, (int64_t)1 << 28));
+    return uniform((int)min(max(run, (int64_t)a.min_run), (int64_t)1 << 28));
 }
-__device__ __forceinline__ int kv_splits(const KvSeq& v, int run) { return max(1, ((v.len + 63) / 64 + run - 1) / run); }
+// runs of a sequence, of equal length: its chunks / run, to the nearest
+__device__ __forceinline__ int kv_splits(const KvSeq& v, int run) { return max(1, (int)(((int64_t)(v.len + 63) / 64 + run / 2) / run)); }
+__device__ __forceinline__ int kv_per_split(const KvSeq& v, int n_splits) { return ((v.len + 63) / 64 + n_splits - 1) / n_splits; }
 
 // ---- V that is not finite at a key that some rows of a tile do not see: 0 times it is not 0.  In the chunks where that can be (edge
 // chunks: not all rows of the tile see all keys) such values are taken out of the products, and what a row sees of them is added to
@@ -464,9 +467,14 @@ template <class C> __device__ __forceinline__ uint32_t kv_kept(int n_keys, int k
     return left >= PER ? 0xffffffffu : left <= 0 ? 0u : (1u << (left * EB & 31)) - 1u;
 }
 
-// 16 * NT rows against a run of chunks: four waves, wave w the chunks w, w + 4, ... of the run with a running maximum and sum per
-// row, merged through LDS at the end.  Scores S[key][row] = K q^T and the output O[dim][row] = V^T P are matrix-core products with the rows as
-// columns (see asd_attn.h); a chunk's fragments go from memory into registers, and the next chunk's K is asked for when the
+// Units of a chunk, so that a wave's share is small where the work of a key is large (fp32 products) and one step of V^T pieces needs no more
+#define KV_UNITS(C) (sizeof(typename C::elem) == 4 ? 4 : sizeof(typename C::elem) == 2 ? KV_BF16_UNITS : 1)
+#ifndef KV_BF16_UNITS
+#define KV_BF16_UNITS 2
+#endif
+// 16 * NT rows against a run of chunks, in units: the keys of one step of V^T pieces (16 fp32, 32 bf16, 64 codes).  Four waves, wave w
+// the units w, w + 4, ... of the run with a running maximum and sum per row, merged through LDS at the end.  Scores S[key][row] = K q^T and the output O[dim][row] = V^T P are matrix-core products with the rows as
+// columns (see asd_attn.h); a unit's fragments go from memory into registers, and the next unit's K is asked for when the
 // scores are done, its V when the output is: memory-bound while the rows are few.
 // 8 bits: K is widened with its scale, V without: V's scales go into the probabilities, one value per key.
 template <class A, class C, int H, int NT>
@@ -474,7 +482,8 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
     using L = KvLayout<C, H>;
     using E = typename A::elem;
     constexpr int AE = A::KE, KK = L::KK, HP = L::HP, US = KK / AE, QS = HP * US;      // operand steps of a K piece, of a row
-    constexpr int HT = L::HT, KST = L::KST, VS = L::KV / AE, PS = KST * VS;            // ... of a V^T piece, of a chunk's keys
+    constexpr int HT = L::HT, KST = L::KST, VS = L::KV / AE;                           // ... of a V^T piece
+    constexpr int UPC = KV_UNITS(C), UK = 64 / UPC, KT = 4 / UPC, KSU = KST / UPC, PS = KSU * VS;      // units of a chunk; keys, score tiles, V^T pieces, steps of a unit
     __shared__ float so[4][16][H];
     __shared__ float sml[4][16][2];
     __shared__ int s_odd;
@@ -488,7 +497,7 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
     all.load(a.kv, 0, lane, check);
     const int run = kv_run<NT>(a, all, lane), n_kv = a.kv.n_kv;
     if (!kv_find(a.kv, all, blockIdx.x, lane, check, [&](const KvSeq& v) { return kv_tiles<NT>(a.kv, v) * kv_splits(v, run) * n_kv; }, &seq, &local, &first, &s)) return;
-    const int n_tiles = kv_tiles<NT>(a.kv, s), n_splits = kv_splits(s, run);
+    const int n_tiles = kv_tiles<NT>(a.kv, s), n_splits = kv_splits(s, run), per = kv_per_split(s, n_splits);
     const int kvh = local % n_kv, tile = local / n_kv % n_tiles, split = local / n_kv / n_tiles;
     const int rows = s.n * a.kv.group, base = s.len - s.n;
     int pos[NT];                                        // last key of this lane's rows (-1: no such row, or none)
@@ -503,7 +512,7 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
         for (int i = 0; i < QS; ++i) qf[t][i] = on ? *(const u32x4*)(qp + i / US * 4 * KK + g * KK + i % US * AE) : u32x4{0u, 0u, 0u, 0u};
     }
     const int last = base + (min((tile + 1) * NT * 16, rows) - 1) / a.kv.group, from = base + tile * NT * 16 / a.kv.group;      // positions of the tile's rows
-    const int c_end = min((last + 64) / 64, (split + 1) * run);       // (last >= -n: nothing to do where it is negative)
+    const int u_end = min((last + UK) / UK, (split + 1) * per * UPC);      // (nothing to do where last is negative)
 
     f32x4 o[NT][HT];
     float mx[NT], l[NT];
@@ -513,10 +522,10 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
 #pragma unroll
         for (int ht = 0; ht < HT; ++ht) o[t][ht] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    u32x4 kf[4][HP], vf[HT][KST], ke, ve;
+    u32x4 kf[KT][HP], vf[HT][KSU], ke, ve;
     auto ask_k = [&](const char* p) {
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
+        for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
             for (int hp = 0; hp < HP; ++hp) {
                 if constexpr (KK * sizeof(typename C::elem) == 16) kf[kt][hp] = __builtin_nontemporal_load((const u32x4*)(p + ((kt * HP + hp) * 64 + lane) * 16));
@@ -528,28 +537,29 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
 #pragma unroll
         for (int ht = 0; ht < HT; ++ht)
 #pragma unroll
-            for (int ks = 0; ks < KST; ++ks) vf[ht][ks] = __builtin_nontemporal_load((const u32x4*)(p + L::K_BYTES + ((ht * KST + ks) * 64 + lane) * 16));
-        if constexpr (L::Q8) ve = *(const u32x4*)(p + 2 * L::K_BYTES + 64 + 16 * g);
+            for (int ks = 0; ks < KSU; ++ks) vf[ht][ks] = __builtin_nontemporal_load((const u32x4*)(p + ((ht * KST + ks) * 64 + lane) * 16));
+        if constexpr (L::Q8) ve = *(const u32x4*)(p + L::K_BYTES + 64 + 16 * g);
     };
-    // a chunk without a page counts as hidden
-    auto next = [&](int c, const char** p) {
-        for (; c < c_end; c += 4) {
-            *p = kv_chunk<C, H>(a.kv, seq, c, kvh);
-            if (*p) break;
+    // a unit without a page counts as hidden
+    auto next = [&](int u, const char** k, const char** v) {
+        for (; u < u_end; u += 4) {
+            const char* p = kv_chunk<C, H>(a.kv, seq, u / UPC, kvh);
+            *k = p + u % UPC * KT * HP * 64 * KK * sizeof(typename C::elem);
+            *v = p + L::K_BYTES + u % UPC * KSU * 1024;
+            if (p) break;
             if (lane == 0) kv_flag(a.kv, ASD_KV_BAD_PAGE);
         }
-        return c;
+        return u;
     };
     bool odd = false;
-    const char* p = nullptr;
-    int c = next(split * run + w, &p);
-    if (c < c_end) { ask_k(p); ask_v(p); }
-    while (c < c_end) {
-        const char* pn = nullptr;
-        const int cn = next(c + 4, &pn);
-        f32x4 sc[NT][4];
+    const char *k = nullptr, *v = nullptr;
+    int unit = next(split * per * UPC + w, &k, &v);
+    if (unit < u_end) { ask_k(k); ask_v(v); }
+    while (unit < u_end) {
+        const int un = next(unit + 4, &k, &v), key0 = unit * UK;
+        f32x4 sc[NT][KT];
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
+        for (int kt = 0; kt < KT; ++kt) {
             float scale = 1.f;
             if constexpr (L::Q8) scale = q8_scale((ke[kt] >> (8 * (m & 3))) & 255u);
 #pragma unroll
@@ -562,15 +572,15 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        if (cn < c_end) ask_k(pn);
+        if (un < u_end) ask_k(k);
         __builtin_amdgcn_sched_barrier(0);
-        // some rows do not see all of the chunk; some of its keys are behind the sequence's end
-        const bool edge = c * 64 + 63 > from;
-        const int n_keys = s.len - c * 64;
-        float vs[4][4];
+        // some rows do not see all of the unit; some of its keys are behind the sequence's end
+        const bool edge = key0 + UK - 1 > from;
+        const int n_keys = s.len - key0;
+        float vs[KT][4];
         if constexpr (L::Q8)
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
+            for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) vs[kt][j] = q8_scale((ve[kt] >> (8 * j)) & 255u);
         u32x4 pf[NT][PS];
@@ -578,14 +588,14 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
         for (int t = 0; t < NT; ++t) {
             if (edge) {
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
+                for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        if (c * 64 + score_key<C>(kt, 4 * g + j) > pos[t]) sc[t][kt][j] = -INFINITY;
+                        if (key0 + score_key<C>(kt, 4 * g + j) > pos[t]) sc[t][kt][j] = -INFINITY;
             }
             float cm = sc[t][0][0];
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
+            for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) cm = fmaxf(cm, sc[t][kt][j]);
             cm = fmaxf(cm, __shfl_xor(cm, 16));
@@ -596,9 +606,9 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
             l[t] *= alpha;
 #pragma unroll
             for (int ht = 0; ht < HT; ++ht) { o[t][ht][0] *= alpha; o[t][ht][1] *= alpha; o[t][ht][2] *= alpha; o[t][ht][3] *= alpha; }
-            float pr[4][4];
+            float pr[KT][4];
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
+            for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float e = __builtin_amdgcn_exp2f((sc[t][kt][j] - ref) * a.c2);
@@ -607,7 +617,7 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
                     if constexpr (L::Q8) {
                         pr[kt][j] = e * vs[kt][j];
                         // (an unwritten scale may be anything)
-                        if (edge && c * 64 + score_key<C>(kt, 4 * g + j) > pos[t]) pr[kt][j] = 0.f;
+                        if (edge && key0 + score_key<C>(kt, 4 * g + j) > pos[t]) pr[kt][j] = 0.f;
                     }
                 }
             // the probabilities as operands: lane group g holds, in order, the keys of its V^T pieces
@@ -629,7 +639,7 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
         if (edge) {                                     // what is behind the end is cleared: 0 times whatever lies there must be 0
             uint32_t hit = 0;
 #pragma unroll
-            for (int ks = 0; ks < KST; ++ks)
+            for (int ks = 0; ks < KSU; ++ks)
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const uint32_t keep = kv_kept<C>(n_keys, ks, g, x);
@@ -651,9 +661,9 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
                 for (int t = 0; t < NT; ++t) mma16<A>(o[t][ht], v, pf[t][i]);
             }
         __builtin_amdgcn_sched_barrier(0);
-        if (cn < c_end) ask_v(pn);
+        if (un < u_end) ask_v(v);
         __builtin_amdgcn_sched_barrier(0);
-        c = cn;
+        unit = un;
     }
 
     // ---- the waves' results, 16 rows at a time, wave order
@@ -685,8 +695,8 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
             }
             if (row >= rows) continue;
             if (s_odd) {
-                const int key0 = max((from + 1) / 64, split * run) * 64, key1 = min(base + token, c_end * 64 - 1);
-                for (int j = 0; j < 4; ++j) v[j] += kv_odd_sum<C, H>(a.kv, seq, kvh, key0, key1, d + j);
+                const int first_key = max((from + 1) / UK * UK, split * per * 64), last_key = min(base + token, u_end * UK - 1);
+                for (int j = 0; j < 4; ++j) v[j] += kv_odd_sum<C, H>(a.kv, seq, kvh, first_key, last_key, d + j);
             }
             if (n_splits == 1) {
                 v[0] *= inv; v[1] *= inv; v[2] *= inv; v[3] *= inv;
@@ -728,7 +738,7 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
     all.load(a.kv, 0, lane, check);
     const int run = kv_run<4 * NT>(a, all, lane), n_kv = a.kv.n_kv;
     if (!kv_find(a.kv, all, blockIdx.x, lane, check, [&](const KvSeq& v) { return kv_tiles<4 * NT>(a.kv, v) * kv_splits(v, run) * n_kv; }, &seq, &local, &first, &s)) return;
-    const int n_tiles = kv_tiles<4 * NT>(a.kv, s), n_splits = kv_splits(s, run);
+    const int n_tiles = kv_tiles<4 * NT>(a.kv, s), n_splits = kv_splits(s, run), per = kv_per_split(s, n_splits);
     const int kvh = local % n_kv, tile = n_tiles - 1 - local / n_kv % n_tiles, split = local / n_kv / n_tiles;      // longest first
     const int rows = s.n * a.kv.group, base = s.len - s.n, row0 = (tile * 4 + w) * NT * 16;
     int pos[NT];
@@ -743,7 +753,7 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
         for (int i = 0; i < QS; ++i) qf[t][i] = on ? *(const u32x4*)(qp + i / US * 4 * KK + g * KK + i % US * AE) : u32x4{0u, 0u, 0u, 0u};
     }
     auto chunks_of = [&](int row_end) { return (base + (min(row_end, rows) - 1) / a.kv.group + 64) / 64; };      // chunks that rows up to there see
-    const int c0 = split * run, c_end = min(chunks_of((tile + 1) * 64 * NT), c0 + run);                         // ... of the workgroup
+    const int c0 = split * per, c_end = min(chunks_of((tile + 1) * 64 * NT), c0 + per);                         // ... of the workgroup
     const int c_my = row0 < rows ? min(chunks_of(row0 + 16 * NT), c_end) : 0;                                   // ... of this wave
     const int from = base + row0 / a.kv.group;
     bool odd = false;
@@ -755,10 +765,10 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
         const int i = min(i_, n_halves - 2 + (i_ & 1)), c = c0 + (i >> 1);
         if (!(i & 1)) {                                  // (the V^T half that follows is of the same chunk)
             typedef const __attribute__((address_space(4))) int32_t* const_i32_ptr;
-            const int per = a.kv.page_tokens / 64;
-            const int page = ((const_i32_ptr)(uintptr_t)a.kv.table)[(size_t)seq * a.kv.table_stride + c / per];
+            const int cpp = a.kv.page_tokens / 64;
+            const int page = ((const_i32_ptr)(uintptr_t)a.kv.table)[(size_t)seq * a.kv.table_stride + c / cpp];
             const bool ok = (unsigned)page < (unsigned)a.kv.n_pages;
-            src = ok ? a.kv.pages + (((size_t)page * n_kv + kvh) * per + c % per) * L::CHUNK : nullptr;
+            src = ok ? a.kv.pages + (((size_t)page * n_kv + kvh) * cpp + c % cpp) * L::CHUNK : nullptr;
             gone = ok ? gone & ~(1u << (c & 31)) : gone | 1u << (c & 31);
             if (!ok && tid == 0) kv_flag(a.kv, ASD_KV_BAD_PAGE);
         }

@@ -90,11 +90,17 @@ int units() {
 #ifndef ROWS_NT
 #define ROWS_NT 2
 #endif
+#ifdef KV_DEV
+#include <cstdlib>
+#define DEV_TUNE if (getenv("KV_TL")) p.target_log2 = atoi(getenv("KV_TL")); if (getenv("KV_MR")) p.min_run = atoi(getenv("KV_MR"));
+#else
+#define DEV_TUNE
+#endif
 // How asd_kv_attend runs a batch of these bounds
 struct AttendPlan {
     int nt;                        // 16-row column blocks of a tile
     bool rows;                     // kv_rows_kernel
-    int32_t target_log2, max_tiles;
+    int32_t target_log2, max_tiles, min_run;
     int64_t grid;                  // most work items
     bool join;                     // some sequence's keys may be cut
     size_t o_bytes, bytes;
@@ -105,17 +111,20 @@ AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b) {
     const int64_t rows = (int64_t)b->max_new * group, chunks = (kv_args(s, b).cap + 63) / 64;
     // Rows share a chunk's fragments: as many columns as the largest sequence fills, up to 64 (fp32: 32, whose operands take twice the registers)
     p.nt = rows <= 16 ? 1 : s->dtype == ASD_DT_F32 ? 2 : rows <= 32 ? 2 : 4;
+    if (s->dtype == ASD_DT_F32 && (int64_t)b->n_rows * s->n_heads / 32 < 2 * units()) p.nt = 1;
     p.rows = s->dtype == ASD_DT_BF16 && s->head_dim >= 64 && rows > 64;
     if (p.rows) p.nt = 4 * ROWS_NT;
+    p.min_run = 16;
     p.target_log2 = 0;
     while ((2 << p.target_log2) <= 4 * units()) ++p.target_log2;
-    const int64_t target = (int64_t)1 << p.target_log2;
     p.max_tiles = (int32_t)((int64_t)b->n_rows * group / (16 * p.nt) + (b->n_seqs < b->n_rows ? b->n_seqs : b->n_rows));
     const int64_t whole = (int64_t)p.max_tiles * s->n_kv_heads;
     // No cut where the tiles alone are work enough for every compute unit, or the keys are too few
-    p.join = chunks > 4 && !(p.rows && whole >= target);
-    p.grid = p.join ? whole + target : whole;
-    if (whole * ((chunks + 3) / 4) < p.grid) p.grid = whole * ((chunks + 3) / 4);
+    auto target = [&] { return (int64_t)1 << p.target_log2; };
+    DEV_TUNE
+    p.join = (chunks + p.min_run / 2) / p.min_run > 1 && !(p.rows && whole >= target());
+    p.grid = p.join ? whole + target() : whole;
+    if (p.join && whole * ((chunks + p.min_run / 2) / p.min_run) < p.grid) p.grid = whole * ((chunks + p.min_run / 2) / p.min_run);
     if (p.join) {
         p.o_bytes = ((size_t)p.grid * 16 * p.nt * s->head_dim * 4 + 255) / 256 * 256;
         p.bytes = p.o_bytes + (size_t)p.grid * 16 * p.nt * 8;
@@ -190,7 +199,7 @@ int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, i
     a.q = q; a.out = out; a.q_stride = q_stride; a.out_stride = out_stride;
     a.c2 = (float)((double)scale * 1.4426950408889634074);
     a.o_part = (float*)workspace; a.ml_part = (float*)((char*)workspace + p.o_bytes);
-    a.target_log2 = p.target_log2; a.cut = p.join;
+    a.target_log2 = p.target_log2; a.cut = p.join; a.min_run = p.min_run;
     const hipStream_t stream = (hipStream_t)hip_stream;
     const dim3 join_grid((unsigned)((int64_t)p.max_tiles * s->n_kv_heads), p.nt);
     auto go = [&](auto t, auto c, auto h, auto nt) {
