@@ -131,6 +131,10 @@ __device__ __forceinline__ uint32_t q8_pack(const float (&v)[4], float inv) {
 }
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
+// two values as a word of bf16
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+}
 
 // A matrix-core operand register of activation type A out of step u of a piece of cache type C (codes: times `scale`)
 template <class A, class C> __device__ __forceinline__ u32x4 kv_operand(const u32x4& piece, int u, float scale) {
@@ -162,7 +166,7 @@ template <> __device__ __forceinline__ void load4<BF16>(const uint16_t* p, float
 }
 template <class T> __device__ __forceinline__ void store4(typename T::elem* p, const float (&v)[4]) {
     if constexpr (sizeof(typename T::elem) == 4) *(float4*)p = float4{v[0], v[1], v[2], v[3]};
-    else *(uint2*)p = uint2{T::from_f32(v[0]) | ((uint32_t)T::from_f32(v[1]) << 16), T::from_f32(v[2]) | ((uint32_t)T::from_f32(v[3]) << 16)};
+    else *(uint2*)p = uint2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
 }
 
 // ---------------------------------------------------------------- new rows into the cache
@@ -440,11 +444,17 @@ __device__ __forceinline__ int kv_per_split(const KvSeq& v, int n_splits) { retu
 // ---- V that is not finite at a key that some rows of a tile do not see: 0 times it is not 0.  In the chunks where that can be (edge
 // chunks: not all rows of the tile see all keys) such values are taken out of the products, and what a row sees of them is added to
 // its sums when they have been stored (infinities and NaN may be added in any order).  Rare, so that path is a plain loop over memory.
-// a word of a V^T piece without them
+// the top bits of a word's elements of a V^T piece that are not finite
+template <class C> __device__ __forceinline__ uint32_t kv_odd(uint32_t v) {
+    if constexpr (sizeof(typename C::elem) == 4) return (v & 0x7f800000u) == 0x7f800000u ? 0x80000000u : 0u;
+    else if constexpr (sizeof(typename C::elem) == 2) return ~(((v & 0x7f807f80u) ^ 0x7f807f80u) + 0x7fff7fffu) & 0x80008000u;      // (no carry leaves a half)
+    else return ((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+}
+// the word without them
 template <class C> __device__ __forceinline__ uint32_t kv_clean(uint32_t v) {
-    if constexpr (sizeof(typename C::elem) == 4) return (v & 0x7f800000u) == 0x7f800000u ? 0u : v;
-    else if constexpr (sizeof(typename C::elem) == 2) return v & ((v & 0x7f800000u) == 0x7f800000u ? 0xffffu : ~0u) & ((v & 0x7f80u) == 0x7f80u ? ~0xffffu : ~0u);
-    else return v & ~((((v & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xffu);
+    constexpr int B = 8 * (int)sizeof(typename C::elem) - 1;
+    const uint32_t t = kv_odd<C>(v);
+    return v & ~((t - (t >> B)) | t);
 }
 // their sum over the keys key0 .. last at one dim (0: there are none)
 template <class C, int H> __device__ float kv_odd_sum(const KvArgs& a, int seq, int kvh, int key0, int last, int dim) {
@@ -628,7 +638,7 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
                         const int e = 2 * x, kt = 2 * i + e / 4;
-                        pf[t][i][x] = BF16::from_f32(pr[kt][e & 3]) | ((uint32_t)BF16::from_f32(pr[kt][(e & 3) + 1]) << 16);
+                        pf[t][i][x] = bf16_pair(pr[kt][e & 3], pr[kt][(e & 3) + 1]);
                     }
                 } else {
 #pragma unroll
@@ -636,21 +646,33 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
                 }
             }
         }
-        if (edge) {                                     // what is behind the end is cleared: 0 times whatever lies there must be 0
+        if (edge) {
+            if (n_keys < UK) {                           // what is behind the end is cleared: 0 times whatever lies there must be 0
+#pragma unroll
+                for (int ks = 0; ks < KSU; ++ks)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const uint32_t keep = kv_kept<C>(n_keys, ks, g, x);
+#pragma unroll
+                        for (int ht = 0; ht < HT; ++ht) vf[ht][ks][x] &= keep;
+                    }
+            }
             uint32_t hit = 0;
 #pragma unroll
-            for (int ks = 0; ks < KSU; ++ks)
+            for (int ht = 0; ht < HT; ++ht)
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const uint32_t keep = kv_kept<C>(n_keys, ks, g, x);
+                for (int ks = 0; ks < KSU; ++ks)
 #pragma unroll
-                    for (int ht = 0; ht < HT; ++ht) {
-                        const uint32_t v = vf[ht][ks][x] & keep;
-                        vf[ht][ks][x] = kv_clean<C>(v);
-                        hit |= v ^ vf[ht][ks][x];
-                    }
-                }
-            if (__any(hit != 0)) odd = true;
+                    for (int x = 0; x < 4; ++x) hit |= kv_odd<C>(vf[ht][ks][x]);
+            if (__any(hit != 0)) {
+                odd = true;
+#pragma unroll
+                for (int ht = 0; ht < HT; ++ht)
+#pragma unroll
+                    for (int ks = 0; ks < KSU; ++ks)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) vf[ht][ks][x] = kv_clean<C>(vf[ht][ks][x]);
+            }
         }
 #pragma unroll
         for (int ht = 0; ht < HT; ++ht)
@@ -710,25 +732,19 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
     }
 }
 
+
 // Many rows (bf16): four waves with 16 * NT rows each walk a run of chunks together.  A chunk's halves (K with the scales, V^T) come into an LDS
-// ring by direct loads, once for the 64 * NT rows; a step waits for its half, one barrier, asks for the half SLOTS - 1 steps on
-// (its slot was last read one step ago) and computes.  Two workgroups share a compute unit, one's products beside the other's exponentials.
-template <class C, int H, int NT> struct KvRowsLds {
-    using L = KvLayout<C, H>;
-    static constexpr int HF = L::K_BYTES / 1024, LH = HF / 4, SLOTS = 5, SC = 4;      // fragments of a half, requests per wave and half; chunks' scales
-    u32x4 mem[SLOTS * HF * 64 + (L::Q8 ? SC * 8 : 0)];      // (bf16 at head dim 128: two of them are a unit's whole LDS)
-    __device__ __forceinline__ u32x4* ring(int i) { return mem + i * HF * 64; }
-    __device__ __forceinline__ u32x4* scales(int i) { return mem + SLOTS * HF * 64 + i * 8; }
-};
+// ring of five by direct loads, once for the 64 * NT rows; two workgroups share a compute unit, one's products beside the other's
+// exponentials.  One barrier per chunk c: V^T of c and K of c + 1 have landed, and the two slots read last are asked for anew.  The fragments of the next
+// product are read from LDS into the registers that the present one frees, so that neither product waits for LDS.
 template <class C, int H, int NT>
 __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
     using A = BF16;
     using L = KvLayout<C, H>;
-    using Lds = KvRowsLds<C, H, NT>;
     constexpr int AE = A::KE, KK = L::KK, HP = L::HP, US = KK / AE, QS = HP * US, HT = L::HT, KST = L::KST, VS = L::KV / AE, PS = KST * VS;
-    constexpr int HF = Lds::HF, LH = Lds::LH, SLOTS = Lds::SLOTS, SC = Lds::SC, X = L::Q8 ? 1 : 0;
-    static_assert(HF % 4 == 0, "every wave asks for the same number of fragments");
-    __shared__ Lds lds;
+    constexpr int HF = L::K_BYTES / 1024, LH = HF / 4, SLOTS = 5, SC = 4, X = L::Q8 ? 1 : 0;      // fragments of a half, requests per wave and half; chunks' scales
+    static_assert(HF % 4 == 0 && HF == 4 * HP && HF == HT * KST, "every wave asks for the same number of fragments");
+    __shared__ u32x4 mem[SLOTS * HF * 64 + (L::Q8 ? SC * 8 : 0)];       // (bf16 at head dim 128: two of them are a unit's whole LDS)
     const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), g = lane >> 4, m = lane & 15;
     int seq, local;
     int64_t first;
@@ -756,29 +772,6 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
     const int c0 = split * per, c_end = min(chunks_of((tile + 1) * 64 * NT), c0 + per);                         // ... of the workgroup
     const int c_my = row0 < rows ? min(chunks_of(row0 + 16 * NT), c_end) : 0;                                   // ... of this wave
     const int from = base + row0 / a.kv.group;
-    bool odd = false;
-    uint32_t gone = 0;                                   // bit c % 32: chunk c has no page
-    // half i of the run: K (i even) or V^T of chunk c0 + i / 2; past the end the last one is asked for again
-    const int n_halves = 2 * (c_end - c0);
-    const char* src = nullptr;
-    auto issue = [&](const int i_) {
-        const int i = min(i_, n_halves - 2 + (i_ & 1)), c = c0 + (i >> 1);
-        if (!(i & 1)) {                                  // (the V^T half that follows is of the same chunk)
-            typedef const __attribute__((address_space(4))) int32_t* const_i32_ptr;
-            const int cpp = a.kv.page_tokens / 64;
-            const int page = ((const_i32_ptr)(uintptr_t)a.kv.table)[(size_t)seq * a.kv.table_stride + c / cpp];
-            const bool ok = (unsigned)page < (unsigned)a.kv.n_pages;
-            src = ok ? a.kv.pages + (((size_t)page * n_kv + kvh) * cpp + c % cpp) * L::CHUNK : nullptr;
-            gone = ok ? gone & ~(1u << (c & 31)) : gone | 1u << (c & 31);
-            if (!ok && tid == 0) kv_flag(a.kv, ASD_KV_BAD_PAGE);
-        }
-        const uint32_t bytes = src ? 0xffffffffu : 0u;
-        u32x4* slot = lds.ring(i_ % SLOTS);
-#pragma unroll
-        for (int q = 0; q < LH; ++q) frag_to_lds(src + (i & 1) * L::K_BYTES + (w + 4 * q) * 1024, bytes, slot + (w + 4 * q) * 64, lane);
-        if constexpr (L::Q8)
-            if (!(i_ & 1) && lane < 8) frag_to_lds(src + 2 * L::K_BYTES, src ? 128u : 0u, lds.scales((i_ >> 1) % SC), lane);
-    };
     f32x4 o[NT][HT];
     float mx[NT], l[NT];
 #pragma unroll
@@ -787,29 +780,59 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
 #pragma unroll
         for (int ht = 0; ht < HT; ++ht) o[t][ht] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    wait_vm<0, true>();                                  // from here on only the ring's requests count
-    if (n_halves > 0) {
+    bool odd = false;
+    if (c_end > c0) {
+        // The page of the chunk asked for next: 64 entries of the table lie in the wave's lanes (-1: no page of the pool)
+        const int cpp = a.kv.page_tokens / 64;
+        int page_i = c0 / cpp, in_page = c0 % cpp, page_base = page_i, pages = 0;
+        auto fetch_pages = [&]() {
+            const int i = page_base + lane;
+            pages = i < a.kv.table_stride ? a.kv.table[(size_t)seq * a.kv.table_stride + i] : -1;
+            if ((unsigned)pages >= (unsigned)a.kv.n_pages) pages = -1;
+        };
+        fetch_pages();
+        uint32_t gone = 0;                               // bit c % 32: chunk c has no page
+        bool lost = false;
+        int asked = c0;                                  // chunk whose K is asked for next
+        const char* src = nullptr;                       // ... and where it is; n_bytes 0: nowhere, zeros come back
+        int n_bytes = 0;
+        auto half = [&](const int i, int off, const char* from_) {      // half i of the ring's sequence K V K V ..
+            u32x4* slot = mem + i % SLOTS * HF * 64;
+            // (a descriptor in scalar registers: the loads would be issued lane by lane otherwise)
+            from_ = (const char*)((uint64_t)(uint32_t)uniform((int)(uintptr_t)from_) | (uint64_t)(uint32_t)uniform((int)((uintptr_t)from_ >> 32)) << 32);
+            const uint32_t bytes = (uint32_t)uniform(n_bytes);
 #pragma unroll
-        for (int i = 0; i < SLOTS - 1; ++i) issue(i);
-    }
-    static_assert(SLOTS == 5, "the waits below");
-    auto step = [&](const int i, auto k_half) {          // behind half i there are three: V K V, or K V K
-        wait_vm<3 * LH + (decltype(k_half)::value ? X : 2 * X), true>();
+            for (int q = 0; q < LH; ++q) frag_to_lds(from_ + off + (w + 4 * q) * 1024, bytes, slot + (w + 4 * q) * 64, lane);
+        };
+        auto ask_k = [&](const int i) {                  // past the end: the last chunk again
+            if (asked < c_end) {
+                const int page = __builtin_amdgcn_readlane(pages, page_i - page_base);
+                src = a.kv.pages + (((size_t)max(page, 0) * n_kv + kvh) * cpp + in_page) * L::CHUNK;
+                n_bytes = page >= 0 ? -1 : 0;
+                gone = page >= 0 ? gone & ~(1u << (asked & 31)) : gone | 1u << (asked & 31);
+                lost |= page < 0;
+                if (++in_page == cpp) { in_page = 0; ++page_i; }
+                ++asked;
+            }
+            half(i, 0, src);
+            if constexpr (L::Q8)
+                if (lane < 8) frag_to_lds(src + 2 * L::K_BYTES, (uint32_t)uniform(n_bytes & 128), mem + SLOTS * HF * 64 + (i >> 1) % SC * 8, lane);
+        };
+        auto ask_v = [&](const int i) { half(i, L::K_BYTES, src); };
+        u32x4 f[HF];                                     // fragments of the half in use
+        auto read = [&](const int i, const int j) { f[j] = mem[(i % SLOTS * HF + j) * 64 + lane]; };
+        wait_vm<0, true>();                              // from here on only the ring's requests count
+        ask_k(0); ask_v(1); ask_k(2); ask_v(3);
+        wait_vm<LH * 3 + X, false>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        issue(i + SLOTS - 1);
-    };
-    for (int c = c0; c < c_end; ++c) {
-        const int i = 2 * (c - c0);
-        u32x4 pf[NT][PS];
-        step(i, std::true_type{});
-        const bool mine = c < c_my && !((gone >> (c & 31)) & 1u);
-        const bool edge = c * 64 + 63 > from;
-        if (mine) {
+#pragma unroll
+        for (int j = 0; j < HF; ++j) read(0, j);
+        // a chunk that this wave has products for; edge: some of its rows do not see all of it
+        auto work = [&](const int c, const int i, auto is_edge) {
+            constexpr bool edge = decltype(is_edge)::value;
             f32x4 sc[NT][4];
-            const u32x4* kp = lds.ring(i % SLOTS);
-            const uint8_t* ex = (const uint8_t*)lds.scales((i >> 1) % SC);
+            const uint8_t* ex = (const uint8_t*)(mem + SLOTS * HF * 64 + (i >> 1) % SC * 8);
             u32x4 ke{}, ve{};
             if constexpr (L::Q8) { ke = *(const u32x4*)(ex + 16 * (m >> 2)); ve = *(const u32x4*)(ex + 64 + 16 * g); }
 #pragma unroll
@@ -820,30 +843,41 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
                 for (int t = 0; t < NT; ++t) sc[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int hp = 0; hp < HP; ++hp) {
-                    const u32x4 piece = kp[(kt * HP + hp) * 64 + lane];
 #pragma unroll
                     for (int u = 0; u < US; ++u) {
-                        const u32x4 x = kv_operand<A, C>(piece, u, scale);
+                        const u32x4 x = kv_operand<A, C>(f[kt * HP + hp], u, scale);
 #pragma unroll
                         for (int t = 0; t < NT; ++t) mma16<A>(sc[t][kt], x, qf[t][hp * US + u]);
                     }
+                    read(i + 1, kt * HP + hp);
                 }
             }
+            ask_v(i + 5);
             float vs[4][4];
             if constexpr (L::Q8)
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) vs[kt][j] = q8_scale((ve[kt] >> (8 * j)) & 255u);
+            if constexpr (edge) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                if (edge) {
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
                             if (c * 64 + score_key<C>(kt, 4 * g + j) > pos[t]) sc[t][kt][j] = -INFINITY;
+                if constexpr (L::Q8) {                   // (an unwritten scale may be anything)
+                    const int n_keys = s.len - c * 64;
+#pragma unroll
+                    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) if (score_key<C>(kt, 4 * g + j) >= n_keys) vs[kt][j] = 0.f;
                 }
+            }
+            u32x4 pf[NT][PS];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
                 float cm = sc[t][0][0];
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt)
@@ -851,7 +885,8 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
                     for (int j = 0; j < 4; ++j) cm = fmaxf(cm, sc[t][kt][j]);
                 cm = fmaxf(cm, __shfl_xor(cm, 16));
                 cm = fmaxf(cm, __shfl_xor(cm, 32));
-                if (__any(cm > mx[t])) {
+                // The reference of a row's exponents need not be its maximum: it moves only when a weight would pass 2^8
+                if (__any((cm - mx[t]) * a.c2 > 8.f)) {
                     const float mn = fmaxf(mx[t], cm), alpha = mn == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mx[t] - mn) * a.c2);
                     mx[t] = mn;
                     l[t] *= alpha;
@@ -859,71 +894,95 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
                     for (int ht = 0; ht < HT; ++ht) { o[t][ht][0] *= alpha; o[t][ht][1] *= alpha; o[t][ht][2] *= alpha; o[t][ht][3] *= alpha; }
                 }
                 const float off = mx[t] == -INFINITY ? 0.f : -mx[t] * a.c2;
-                float pr[4][4];
+                float sum[2] = {0.f, 0.f};
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
+                for (int kt = 0; kt < 4; ++kt) {
+                    float e[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float e = __builtin_amdgcn_exp2f(fmaf(sc[t][kt][j], a.c2, off));
-                        l[t] += e;
-                        pr[kt][j] = e;
-                        if constexpr (L::Q8) pr[kt][j] = e * vs[kt][j];
-                    }
-                if constexpr (L::Q8)
-                    if (edge) {                          // (an unwritten scale may be anything)
+                    for (int j = 0; j < 4; ++j) { e[j] = __builtin_amdgcn_exp2f(fmaf(sc[t][kt][j], a.c2, off)); sum[j & 1] += e[j]; }
+                    if constexpr (L::Q8)
 #pragma unroll
-                        for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) if (c * 64 + score_key<C>(kt, 4 * g + j) > pos[t]) pr[kt][j] = 0.f;
-                    }
-#pragma unroll
-                for (int x = 0; x < PS; ++x)
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) pf[t][x][y] = BF16::from_f32(pr[2 * x + y / 2][2 * (y & 1)]) | ((uint32_t)BF16::from_f32(pr[2 * x + y / 2][2 * (y & 1) + 1]) << 16);
+                        for (int j = 0; j < 4; ++j) e[j] *= vs[kt][j];
+                    pf[t][kt / 2][kt % 2 * 2] = bf16_pair(e[0], e[1]);      // as V is: see kv_attend_kernel
+                    pf[t][kt / 2][kt % 2 * 2 + 1] = bf16_pair(e[2], e[3]);
+                }
+                l[t] += sum[0] + sum[1];
             }
-        }
-        step(i + 1, std::false_type{});
-        if (mine) {
-            const u32x4* vp = lds.ring((i + 1) % SLOTS);
-            if (!edge) {
-#pragma unroll
-                for (int ht = 0; ht < HT; ++ht)
-#pragma unroll
-                    for (int ks = 0; ks < KST; ++ks) {
-                        const u32x4 piece = vp[(ht * KST + ks) * 64 + lane];
-#pragma unroll
-                        for (int u = 0; u < VS; ++u) {
-                            const u32x4 v = kv_operand<A, C>(piece, u, 1.f);
-#pragma unroll
-                            for (int t = 0; t < NT; ++t) mma16<A>(o[t][ht], v, pf[t][ks * VS + u]);
-                        }
-                    }
-            } else {                                     // keys that a row does not see: see kv_attend_kernel
+            if constexpr (edge) {                        // keys that a row does not see: see kv_attend_kernel
                 const int n_keys = s.len - c * 64;
-                uint32_t hit = 0;
+                if (n_keys < 64) {
 #pragma unroll
-                for (int ht = 0; ht < HT; ++ht)
-#pragma unroll
-                    for (int ks = 0; ks < KST; ++ks) {
-                        u32x4 piece = vp[(ht * KST + ks) * 64 + lane];
+                    for (int ks = 0; ks < KST; ++ks)
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
-                            const uint32_t v = piece[x] & kv_kept<C>(n_keys, ks, g, x);
-                            piece[x] = kv_clean<C>(v);
-                            hit |= v ^ piece[x];
-                        }
+                            const uint32_t keep = kv_kept<C>(n_keys, ks, g, x);
 #pragma unroll
-                        for (int u = 0; u < VS; ++u) {
-                            const u32x4 v = kv_operand<A, C>(piece, u, 1.f);
-#pragma unroll
-                            for (int t = 0; t < NT; ++t) mma16<A>(o[t][ht], v, pf[t][ks * VS + u]);
+                            for (int ht = 0; ht < HT; ++ht) f[ht * KST + ks][x] &= keep;
                         }
-                    }
-                if (__any(hit != 0)) odd = true;
+                }
+                uint32_t hit = 0;
+#pragma unroll
+                for (int j = 0; j < HF; ++j)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) hit |= kv_odd<C>(f[j][x]);
+                if (__any(hit != 0)) {
+                    odd = true;
+#pragma unroll
+                    for (int j = 0; j < HF; ++j)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) f[j][x] = kv_clean<C>(f[j][x]);
+                }
             }
+#pragma unroll
+            for (int ht = 0; ht < HT; ++ht)
+#pragma unroll
+                for (int ks = 0; ks < KST; ++ks) {
+#pragma unroll
+                    for (int u = 0; u < VS; ++u) {
+                        const u32x4 v = kv_operand<A, C>(f[ht * KST + ks], u, 1.f);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) mma16<A>(o[t][ht], v, pf[t][ks * VS + u]);
+                    }
+                    read(i + 2, ht * KST + ks);
+                }
+        };
+        auto turn = [&](const int c, const int i) {      // the chunk's barrier, and the next K
+            if (page_i - page_base >= 62) {              // (once in 62 pages: the ring runs dry for a moment)
+                page_base = page_i;
+                fetch_pages();
+                wait_vm<0, false>();
+            }
+            // asked for before: .. V(i+1) K(i+2) V(i+3) ; the last of them may still be on its way
+            wait_vm<LH, true>();                         // (and this wave has read K(i) into registers)
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            ask_k(i + 4);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        // Chunks that all rows of the workgroup see run in a loop of their own, without masks; those with an edge, or without a page, one by one
+        const int c_main = min(c_end, (base + tile * NT * 64 / a.kv.group + 1) / 64);
+        int c = c0, i = 0;
+        for (;;) {
+            for (; c < c_main && gone == 0; ++c, i += 2) {
+                turn(c, i);
+                work(c, i, std::false_type{});
+            }
+            if (c >= c_end) break;
+            turn(c, i);
+            if (c < c_my && !((gone >> (c & 31)) & 1u)) {
+                work(c, i, std::true_type{});
+            } else {
+                ask_v(i + 5);
+#pragma unroll
+                for (int j = 0; j < HF; ++j) read(i + 2, j);
+            }
+            gone &= ~(1u << (c & 31));
+            ++c; i += 2;
         }
+        if (lost && tid == 0) kv_flag(a.kv, ASD_KV_BAD_PAGE);
+        wait_vm<0, true>();                              // no request may outlive the workgroup's LDS
     }
-    wait_vm<0, true>();                                  // no request may outlive the workgroup's LDS
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         float z = l[t];
@@ -931,22 +990,21 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
         z += __shfl_xor(z, 32);
         const int row = row0 + t * 16 + m, token = row / a.kv.group, head = kvh * a.kv.group + row % a.kv.group;
         if (row >= rows) continue;
+        const size_t at = (size_t)(first + (int64_t)(split * n_tiles + tile) * n_kv + kvh) * (64 * NT) + row - tile * 64 * NT;
+        uint16_t* out = (uint16_t*)a.out + (s.r0 + (int64_t)token) * a.out_stride + head * H;
         if (n_splits == 1) {
             const float inv = z == 0.f ? 0.f : 1.f / z;
 #pragma unroll
             for (int ht = 0; ht < HT; ++ht) {
                 const float v[4] = {o[t][ht][0] * inv, o[t][ht][1] * inv, o[t][ht][2] * inv, o[t][ht][3] * inv};
-                store4<A>((uint16_t*)a.out + (s.r0 + (int64_t)token) * a.out_stride + head * H + ht * 16 + 4 * g, v);
+                store4<A>(out + ht * 16 + 4 * g, v);
             }
         } else {
-            const size_t at = (size_t)(first + (int64_t)(split * n_tiles + tile) * n_kv + kvh) * (64 * NT) + row - tile * 64 * NT;
 #pragma unroll
             for (int ht = 0; ht < HT; ++ht) *(f32x4*)(a.o_part + at * H + ht * 16 + 4 * g) = o[t][ht];
             if (g == 0) { a.ml_part[at * 2] = mx[t]; a.ml_part[at * 2 + 1] = z; }
         }
         if (odd) {                                       // (each lane changes what it has stored)
-            const size_t at = (size_t)(first + (int64_t)(split * n_tiles + tile) * n_kv + kvh) * (64 * NT) + row - tile * 64 * NT;
-            uint16_t* out = (uint16_t*)a.out + (s.r0 + (int64_t)token) * a.out_stride + head * H;
             for (int d = 0; d < H / 4; ++d) {
                 const int dim = d / 4 * 16 + 4 * g + d % 4;
                 const float x = kv_odd_sum<C, H>(a.kv, seq, kvh, max((from + 1) / 64, c0) * 64, min(pos[t], c_end * 64 - 1), dim);
@@ -1046,7 +1104,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(const KvAttendArgs a) {
     E* out = (E*)a.out + (s.r0 + (int64_t)token) * a.out_stride + head * H + d0;
 #pragma unroll
     for (int d = 0; d < DL; d += 2) {
-        if constexpr (sizeof(E) == 2) *(uint32_t*)(out + d) = A::from_f32(acc[d] * inv) | ((uint32_t)A::from_f32(acc[d + 1] * inv) << 16);
+        if constexpr (sizeof(E) == 2) *(uint32_t*)(out + d) = bf16_pair(acc[d] * inv, acc[d + 1] * inv);
         else *(float2*)(out + d) = float2{acc[d] * inv, acc[d + 1] * inv};
     }
 }
