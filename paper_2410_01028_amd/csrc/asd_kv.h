@@ -733,17 +733,16 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
 }
 
 
-// Many rows (bf16): four waves with 16 * NT rows each walk a run of chunks together.  A chunk's halves (K with the scales, V^T) come into an LDS
-// ring of five by direct loads, once for the 64 * NT rows; two workgroups share a compute unit, one's products beside the other's
-// exponentials.  One barrier per chunk c: V^T of c and K of c + 1 have landed, and the two slots read last are asked for anew.  The fragments of the next
-// product are read from LDS into the registers that the present one frees, so that neither product waits for LDS.
-template <class C, int H, int NT>
-__global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
+// Many rows (bf16): NW waves with 16 * NT rows each walk a run of chunks together, their fragments in LDS once for all of them.  They come by
+// direct loads into a ring of five half-chunks (K, V^T, K, ..): one barrier per chunk c, behind which K and V^T of c have landed
+// and the slots of c - 1 are asked for anew (V^T of c + 1, K of c + 2).  A SIMD has several waves, one's products beside the other's exponentials.
+template <class C, int H, int NT, int NW>
+__global__ __launch_bounds__(64 * NW, ROWS_EU) void kv_rows_kernel(const KvAttendArgs a) {
     using A = BF16;
     using L = KvLayout<C, H>;
     constexpr int AE = A::KE, KK = L::KK, HP = L::HP, US = KK / AE, QS = HP * US, HT = L::HT, KST = L::KST, VS = L::KV / AE, PS = KST * VS;
-    constexpr int HF = L::K_BYTES / 1024, LH = HF / 4, SLOTS = 5, SC = 4, X = L::Q8 ? 1 : 0;      // fragments of a half, requests per wave and half; chunks' scales
-    static_assert(HF % 4 == 0 && HF == 4 * HP && HF == HT * KST, "every wave asks for the same number of fragments");
+    constexpr int HF = L::K_BYTES / 1024, LH = HF / NW, SLOTS = 5, SC = 4, X = L::Q8 ? 1 : 0, RT = NW * NT;      // fragments of a half, requests per wave and half; chunks' scales; 16-row blocks of a tile
+    static_assert(HF % NW == 0 && HF == 4 * HP && HF == HT * KST, "every wave asks for the same number of fragments");
     __shared__ u32x4 mem[SLOTS * HF * 64 + (L::Q8 ? SC * 8 : 0)];       // (bf16 at head dim 128: two of them are a unit's whole LDS)
     const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), g = lane >> 4, m = lane & 15;
     int seq, local;
@@ -752,11 +751,11 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
     const bool check = blockIdx.x == 0 && w == 0;
     KvLanes all;
     all.load(a.kv, 0, lane, check);
-    const int run = kv_run<4 * NT>(a, all, lane), n_kv = a.kv.n_kv;
-    if (!kv_find(a.kv, all, blockIdx.x, lane, check, [&](const KvSeq& v) { return kv_tiles<4 * NT>(a.kv, v) * kv_splits(v, run) * n_kv; }, &seq, &local, &first, &s)) return;
-    const int n_tiles = kv_tiles<4 * NT>(a.kv, s), n_splits = kv_splits(s, run), per = kv_per_split(s, n_splits);
+    const int run = kv_run<RT>(a, all, lane), n_kv = a.kv.n_kv;
+    if (!kv_find(a.kv, all, blockIdx.x, lane, check, [&](const KvSeq& v) { return kv_tiles<RT>(a.kv, v) * kv_splits(v, run) * n_kv; }, &seq, &local, &first, &s)) return;
+    const int n_tiles = kv_tiles<RT>(a.kv, s), n_splits = kv_splits(s, run), per = kv_per_split(s, n_splits);
     const int kvh = local % n_kv, tile = n_tiles - 1 - local / n_kv % n_tiles, split = local / n_kv / n_tiles;      // longest first
-    const int rows = s.n * a.kv.group, base = s.len - s.n, row0 = (tile * 4 + w) * NT * 16;
+    const int rows = s.n * a.kv.group, base = s.len - s.n, row0 = (tile * NW + w) * NT * 16;
     int pos[NT];
     u32x4 qf[NT][QS];
 #pragma unroll
@@ -769,9 +768,10 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
         for (int i = 0; i < QS; ++i) qf[t][i] = on ? *(const u32x4*)(qp + i / US * 4 * KK + g * KK + i % US * AE) : u32x4{0u, 0u, 0u, 0u};
     }
     auto chunks_of = [&](int row_end) { return (base + (min(row_end, rows) - 1) / a.kv.group + 64) / 64; };      // chunks that rows up to there see
-    const int c0 = split * per, c_end = min(chunks_of((tile + 1) * 64 * NT), c0 + per);                         // ... of the workgroup
+    const int c0 = split * per, c_end = min(chunks_of((tile + 1) * 16 * RT), c0 + per);                         // ... of the workgroup
     const int c_my = row0 < rows ? min(chunks_of(row0 + 16 * NT), c_end) : 0;                                   // ... of this wave
     const int from = base + row0 / a.kv.group;
+    const int c_main = min(c_end, (base + tile * RT * 16 / a.kv.group + 1) / 64);                               // chunks that all its rows see whole
     f32x4 o[NT][HT];
     float mx[NT], l[NT];
 #pragma unroll
@@ -780,7 +780,7 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
 #pragma unroll
         for (int ht = 0; ht < HT; ++ht) o[t][ht] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    bool odd = false;
+    bool odd = false;                                    // this lane has taken a value out of V
     if (c_end > c0) {
         // The page of the chunk asked for next: 64 entries of the table lie in the wave's lanes (-1: no page of the pool)
         const int cpp = a.kv.page_tokens / 64;
@@ -794,17 +794,17 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
         uint32_t gone = 0;                               // bit c % 32: chunk c has no page
         bool lost = false;
         int asked = c0;                                  // chunk whose K is asked for next
-        const char* src = nullptr;                       // ... and where it is; n_bytes 0: nowhere, zeros come back
-        int n_bytes = 0;
-        auto half = [&](const int i, int off, const char* from_) {      // half i of the ring's sequence K V K V ..
-            u32x4* slot = mem + i % SLOTS * HF * 64;
+        const char *src = nullptr, *src_v = nullptr;     // the K asked for last, and the V^T asked for next; n_bytes 0: nowhere, zeros come back
+        int n_bytes = 0, n_bytes_v = 0, slot_k = 0, slot_v = 1;
+        auto half = [&](const char* from_, const int n, const int slot) {
             // (a descriptor in scalar registers: the loads would be issued lane by lane otherwise)
             from_ = (const char*)((uint64_t)(uint32_t)uniform((int)(uintptr_t)from_) | (uint64_t)(uint32_t)uniform((int)((uintptr_t)from_ >> 32)) << 32);
-            const uint32_t bytes = (uint32_t)uniform(n_bytes);
+            const uint32_t bytes = (uint32_t)uniform(n);
 #pragma unroll
-            for (int q = 0; q < LH; ++q) frag_to_lds(from_ + off + (w + 4 * q) * 1024, bytes, slot + (w + 4 * q) * 64, lane);
+            for (int q = 0; q < LH; ++q) frag_to_lds(from_ + (w + NW * q) * 1024, bytes, mem + slot * HF * 64 + (w + NW * q) * 64, lane);
         };
-        auto ask_k = [&](const int i) {                  // past the end: the last chunk again
+        auto ask_k = [&]() {                             // past the end: the last chunk again
+            src_v = src; n_bytes_v = n_bytes;
             if (asked < c_end) {
                 const int page = __builtin_amdgcn_readlane(pages, page_i - page_base);
                 src = a.kv.pages + (((size_t)max(page, 0) * n_kv + kvh) * cpp + in_page) * L::CHUNK;
@@ -812,27 +812,40 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
                 gone = page >= 0 ? gone & ~(1u << (asked & 31)) : gone | 1u << (asked & 31);
                 lost |= page < 0;
                 if (++in_page == cpp) { in_page = 0; ++page_i; }
-                ++asked;
             }
-            half(i, 0, src);
+            half(src, n_bytes, slot_k);
             if constexpr (L::Q8)
-                if (lane < 8) frag_to_lds(src + 2 * L::K_BYTES, (uint32_t)uniform(n_bytes & 128), mem + SLOTS * HF * 64 + (i >> 1) % SC * 8, lane);
+                if (lane < 8) frag_to_lds(src + 2 * L::K_BYTES, (uint32_t)uniform(n_bytes & 128), mem + SLOTS * HF * 64 + asked % SC * 8, lane);
+            ++asked;
+            slot_k = slot_k + 2 >= SLOTS ? slot_k + 2 - SLOTS : slot_k + 2;
         };
-        auto ask_v = [&](const int i) { half(i, L::K_BYTES, src); };
-        u32x4 f[HF];                                     // fragments of the half in use
-        auto read = [&](const int i, const int j) { f[j] = mem[(i % SLOTS * HF + j) * 64 + lane]; };
+        auto ask_v = [&](const char* p, const int n) {
+            half(p + L::K_BYTES, n, slot_v);
+            slot_v = slot_v + 2 >= SLOTS ? slot_v + 2 - SLOTS : slot_v + 2;
+        };
+        int use_k = 0, use_v = 1;                        // slots of the chunk at hand
         wait_vm<0, true>();                              // from here on only the ring's requests count
-        ask_k(0); ask_v(1); ask_k(2); ask_v(3);
-        wait_vm<LH * 3 + X, false>();
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-#pragma unroll
-        for (int j = 0; j < HF; ++j) read(0, j);
+        ask_k(); ask_v(src, n_bytes); ask_k();           // K, V^T of the first chunk, K of the next
+        auto turn = [&]() {
+            if (page_i - page_base >= 62) {              // (once in 62 pages: the ring runs dry for a moment)
+                page_base = page_i;
+                fetch_pages();
+                wait_vm<0, false>();
+            }
+            wait_vm<LH + X, true>();                     // the K of the next chunk may still be on its way
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            ask_v(src, n_bytes);
+            ask_k();
+            __builtin_amdgcn_sched_barrier(0);
+        };
         // a chunk that this wave has products for; edge: some of its rows do not see all of it
-        auto work = [&](const int c, const int i, auto is_edge) {
+        auto work = [&](const int c, auto is_edge) {
             constexpr bool edge = decltype(is_edge)::value;
+            const u32x4 *kp = mem + use_k * HF * 64 + lane, *vp = mem + use_v * HF * 64 + lane;
             f32x4 sc[NT][4];
-            const uint8_t* ex = (const uint8_t*)(mem + SLOTS * HF * 64 + (i >> 1) % SC * 8);
+            const uint8_t* ex = (const uint8_t*)(mem + SLOTS * HF * 64 + c % SC * 8);
             u32x4 ke{}, ve{};
             if constexpr (L::Q8) { ke = *(const u32x4*)(ex + 16 * (m >> 2)); ve = *(const u32x4*)(ex + 64 + 16 * g); }
 #pragma unroll
@@ -843,16 +856,15 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
                 for (int t = 0; t < NT; ++t) sc[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int hp = 0; hp < HP; ++hp) {
+                    const u32x4 f = kp[(kt * HP + hp) * 64];
 #pragma unroll
                     for (int u = 0; u < US; ++u) {
-                        const u32x4 x = kv_operand<A, C>(f[kt * HP + hp], u, scale);
+                        const u32x4 x = kv_operand<A, C>(f, u, scale);
 #pragma unroll
                         for (int t = 0; t < NT; ++t) mma16<A>(sc[t][kt], x, qf[t][hp * US + u]);
                     }
-                    read(i + 1, kt * HP + hp);
                 }
             }
-            ask_v(i + 5);
             float vs[4][4];
             if constexpr (L::Q8)
 #pragma unroll
@@ -908,80 +920,73 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
                 }
                 l[t] += sum[0] + sum[1];
             }
-            if constexpr (edge) {                        // keys that a row does not see: see kv_attend_kernel
-                const int n_keys = s.len - c * 64;
-                if (n_keys < 64) {
-#pragma unroll
-                    for (int ks = 0; ks < KST; ++ks)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const uint32_t keep = kv_kept<C>(n_keys, ks, g, x);
-#pragma unroll
-                            for (int ht = 0; ht < HT; ++ht) f[ht * KST + ks][x] &= keep;
-                        }
-                }
-                uint32_t hit = 0;
-#pragma unroll
-                for (int j = 0; j < HF; ++j)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) hit |= kv_odd<C>(f[j][x]);
-                if (__any(hit != 0)) {
-                    odd = true;
-#pragma unroll
-                    for (int j = 0; j < HF; ++j)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) f[j][x] = kv_clean<C>(f[j][x]);
-                }
-            }
 #pragma unroll
             for (int ht = 0; ht < HT; ++ht)
 #pragma unroll
                 for (int ks = 0; ks < KST; ++ks) {
+                    const u32x4 f = vp[(ht * KST + ks) * 64];
 #pragma unroll
                     for (int u = 0; u < VS; ++u) {
-                        const u32x4 v = kv_operand<A, C>(f[ht * KST + ks], u, 1.f);
+                        const u32x4 v = kv_operand<A, C>(f, u, 1.f);
 #pragma unroll
                         for (int t = 0; t < NT; ++t) mma16<A>(o[t][ht], v, pf[t][ks * VS + u]);
                     }
-                    read(i + 2, ht * KST + ks);
                 }
         };
-        auto turn = [&](const int c, const int i) {      // the chunk's barrier, and the next K
-            if (page_i - page_base >= 62) {              // (once in 62 pages: the ring runs dry for a moment)
-                page_base = page_i;
-                fetch_pages();
-                wait_vm<0, false>();
+        // A chunk with an edge: keys behind the end and values that are not finite leave V^T (see kv_clean); each wave cleans what it has asked for
+        auto clean = [&](const int c) {
+            const int n_keys = s.len - c * 64;
+            uint32_t hit = 0;
+#pragma unroll 1
+            for (int q = 0; q < LH; ++q) {
+                const int j = w + NW * q;
+                u32x4* p = mem + (use_v * HF + j) * 64 + lane;
+                u32x4 f = *p;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    f[x] &= kv_kept<C>(n_keys, j % KST, g, x);
+                    hit |= kv_odd<C>(f[x]);
+                    f[x] = kv_clean<C>(f[x]);
+                }
+                *p = f;
             }
-            // asked for before: .. V(i+1) K(i+2) V(i+3) ; the last of them may still be on its way
-            wait_vm<LH, true>();                         // (and this wave has read K(i) into registers)
+            odd |= hit != 0;
+            asm volatile("" ::: "memory");
+            wait_vm<63, true>();                         // (the ring's requests go on)
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            __builtin_amdgcn_sched_barrier(0);
-            ask_k(i + 4);
-            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto done = [&]() {
+            use_k = use_k + 2 >= SLOTS ? use_k + 2 - SLOTS : use_k + 2;
+            use_v = use_v + 2 >= SLOTS ? use_v + 2 - SLOTS : use_v + 2;
         };
         // Chunks that all rows of the workgroup see run in a loop of their own, without masks; those with an edge, or without a page, one by one
-        const int c_main = min(c_end, (base + tile * NT * 64 / a.kv.group + 1) / 64);
-        int c = c0, i = 0;
+        int c = c0;
         for (;;) {
-            for (; c < c_main && gone == 0; ++c, i += 2) {
-                turn(c, i);
-                work(c, i, std::false_type{});
+            for (; c < c_main && gone == 0; ++c) {
+                turn();
+                work(c, std::false_type{});
+                done();
             }
             if (c >= c_end) break;
-            turn(c, i);
+            turn();
+            clean(c);
             if (c < c_my && !((gone >> (c & 31)) & 1u)) {
-                work(c, i, std::true_type{});
-            } else {
-                ask_v(i + 5);
-#pragma unroll
-                for (int j = 0; j < HF; ++j) read(i + 2, j);
+                if (c * 64 + 63 > from) work(c, std::true_type{}); else work(c, std::false_type{});
             }
+            done();
             gone &= ~(1u << (c & 31));
-            ++c; i += 2;
+            ++c;
         }
         if (lost && tid == 0) kv_flag(a.kv, ASD_KV_BAD_PAGE);
         wait_vm<0, true>();                              // no request may outlive the workgroup's LDS
+        __syncthreads();
+        int* any = (int*)mem;                            // the ring is free: what one lane has taken out concerns all
+        if (tid == 0) *any = 0;
+        __syncthreads();
+        if (odd) *any = 1;
+        __syncthreads();
+        odd = *any != 0;
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -990,7 +995,7 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
         z += __shfl_xor(z, 32);
         const int row = row0 + t * 16 + m, token = row / a.kv.group, head = kvh * a.kv.group + row % a.kv.group;
         if (row >= rows) continue;
-        const size_t at = (size_t)(first + (int64_t)(split * n_tiles + tile) * n_kv + kvh) * (64 * NT) + row - tile * 64 * NT;
+        const size_t at = (size_t)(first + (int64_t)(split * n_tiles + tile) * n_kv + kvh) * (16 * RT) + row - tile * 16 * RT;
         uint16_t* out = (uint16_t*)a.out + (s.r0 + (int64_t)token) * a.out_stride + head * H;
         if (n_splits == 1) {
             const float inv = z == 0.f ? 0.f : 1.f / z;
@@ -1007,8 +1012,8 @@ __global__ __launch_bounds__(256, 2) void kv_rows_kernel(const KvAttendArgs a) {
         if (odd) {                                       // (each lane changes what it has stored)
             for (int d = 0; d < H / 4; ++d) {
                 const int dim = d / 4 * 16 + 4 * g + d % 4;
-                const float x = kv_odd_sum<C, H>(a.kv, seq, kvh, max((from + 1) / 64, c0) * 64, min(pos[t], c_end * 64 - 1), dim);
-                if (finite(x)) continue;
+                const float x = kv_odd_sum<C, H>(a.kv, seq, kvh, max(c_main, c0) * 64, min(pos[t], c_end * 64 - 1), dim);
+                if (finite(x)) continue;                 // (nothing of its own row's to add)
                 if (n_splits == 1) out[dim] = BF16::from_f32(BF16::to_f32(out[dim]) + x); else a.o_part[at * H + dim] += x;
             }
         }

@@ -1,5 +1,10 @@
 // Host side of the operators over a paged cache of several sequences: argument checks, launch rules, the C ABI of asd.h.
 #include "../../include/asd.h"
+#ifndef ROWS_NT
+#define ROWS_NT 2
+#define ROWS_NW 4
+#define ROWS_EU 2
+#endif
 #include "asd_kv.h"
 
 #include <cmath>
@@ -87,9 +92,6 @@ int units() {
     return n;
 }
 
-#ifndef ROWS_NT
-#define ROWS_NT 2
-#endif
 #ifdef KV_DEV
 #include <cstdlib>
 #define DEV_TUNE if (getenv("KV_TL")) p.target_log2 = atoi(getenv("KV_TL")); if (getenv("KV_MR")) p.min_run = atoi(getenv("KV_MR"));
@@ -113,7 +115,7 @@ AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b) {
     p.nt = rows <= 16 ? 1 : s->dtype == ASD_DT_F32 ? 2 : rows <= 32 ? 2 : 4;
     if (s->dtype == ASD_DT_F32 && (int64_t)b->n_rows * s->n_heads / 32 < 2 * units()) p.nt = 1;
     p.rows = s->dtype == ASD_DT_BF16 && s->head_dim >= 64 && rows > 64;
-    if (p.rows) p.nt = 4 * ROWS_NT;
+    if (p.rows) p.nt = 8;
     p.min_run = 16;
     p.target_log2 = 0;
     while ((2 << p.target_log2) <= 4 * units()) ++p.target_log2;
@@ -209,8 +211,8 @@ int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, i
     by_shape(s, [&](auto t, auto c, auto h) {
         if (p.rows) {
             if constexpr (sizeof(typename decltype(t)::elem) == 2 && h.value >= 64) {
-                kv_rows_kernel<decltype(c), h.value, ROWS_NT><<<(unsigned)p.grid, 256, 0, stream>>>(a);
-                if (p.join) kv_join_kernel<decltype(t), h.value, 4 * ROWS_NT><<<join_grid, 256, 0, stream>>>(a);
+                kv_rows_kernel<decltype(c), h.value, (sizeof(typename decltype(c)::elem) * h.value < 128 ? 2 : ROWS_NT), (sizeof(typename decltype(c)::elem) * h.value < 128 ? 4 : ROWS_NW)><<<(unsigned)p.grid, sizeof(typename decltype(c)::elem) * h.value < 128 ? 256 : 64 * ROWS_NW, 0, stream>>>(a);
+                if (p.join) kv_join_kernel<decltype(t), h.value, 8><<<join_grid, 256, 0, stream>>>(a);
             }
         } else if (p.nt == 1) go(t, c, h, std::integral_constant<int, 1>{});
         else if (p.nt == 2) go(t, c, h, std::integral_constant<int, 2>{});
