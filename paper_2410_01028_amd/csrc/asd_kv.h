@@ -136,6 +136,20 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
 }
 
+// maximum and sum over the four lane groups (every lane gets them): exchanges of rows and halves in the vector unit, no LDS round trip
+__device__ __forceinline__ float groups_max(float x) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float groups_sum(float x) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // A matrix-core operand register of activation type A out of step u of a piece of cache type C (codes: times `scale`)
 template <class A, class C> __device__ __forceinline__ u32x4 kv_operand(const u32x4& piece, int u, float scale) {
     if constexpr (sizeof(typename C::elem) > 1) {
@@ -608,8 +622,7 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
             for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) cm = fmaxf(cm, sc[t][kt][j]);
-            cm = fmaxf(cm, __shfl_xor(cm, 16));
-            cm = fmaxf(cm, __shfl_xor(cm, 32));
+            cm = groups_max(cm);
             const float mn = fmaxf(mx[t], cm), ref = mn == -INFINITY ? 0.f : mn;      // nothing seen yet: all weights are 0
             const float alpha = __builtin_amdgcn_exp2f((mx[t] - ref) * a.c2);
             mx[t] = mn;
@@ -694,8 +707,7 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         if (t) __syncthreads();
-        l[t] += __shfl_xor(l[t], 16);
-        l[t] += __shfl_xor(l[t], 32);
+        l[t] = groups_sum(l[t]);
         if (g == 0) { sml[w][m][0] = mx[t]; sml[w][m][1] = l[t]; }
 #pragma unroll
         for (int ht = 0; ht < HT; ++ht) *(f32x4*)&so[w][m][ht * 16 + 4 * g] = o[t][ht];
@@ -848,22 +860,29 @@ __global__ __launch_bounds__(64 * NW, ROWS_EU) void kv_rows_kernel(const KvAtten
             const uint8_t* ex = (const uint8_t*)(mem + SLOTS * HF * 64 + c % SC * 8);
             u32x4 ke{}, ve{};
             if constexpr (L::Q8) { ke = *(const u32x4*)(ex + 16 * (m >> 2)); ve = *(const u32x4*)(ex + 64 + 16 * g); }
+            // The four score tiles side by side, so that no product waits for the one before it, and the fragments of a step
+            // are read while the step before it runs; so too the output tiles below, two at a time (the fences keep that order)
+            u32x4 f[2][4];
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt) {
-                float scale = 1.f;
-                if constexpr (L::Q8) scale = q8_scale((ke[kt] >> (8 * (m & 3))) & 255u);
+            for (int kt = 0; kt < 4; ++kt) f[0][kt] = kp[kt * HP * 64];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) sc[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int hp = 0; hp < HP; ++hp) {
 #pragma unroll
-                for (int hp = 0; hp < HP; ++hp) {
-                    const u32x4 f = kp[(kt * HP + hp) * 64];
+                for (int kt = 0; kt < 4; ++kt) f[(hp + 1) & 1][kt] = hp + 1 < HP ? kp[(kt * HP + hp + 1) * 64] : vp[kt * 64];
 #pragma unroll
-                    for (int u = 0; u < US; ++u) {
-                        const u32x4 x = kv_operand<A, C>(f, u, scale);
+                for (int u = 0; u < US; ++u)
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) mma16<A>(sc[t][kt], x, qf[t][hp * US + u]);
+                    for (int kt = 0; kt < 4; ++kt) {
+                        float scale = 1.f;
+                        if constexpr (L::Q8) scale = q8_scale((ke[kt] >> (8 * (m & 3))) & 255u);
+                        const u32x4 x = kv_operand<A, C>(f[hp & 1][kt], u, scale);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            if (hp == 0 && u == 0) sc[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+                            mma16<A>(sc[t][kt], x, qf[t][hp * US + u]);
+                        }
                     }
-                }
+                __builtin_amdgcn_sched_barrier(0);
             }
             float vs[4][4];
             if constexpr (L::Q8)
@@ -895,8 +914,7 @@ __global__ __launch_bounds__(64 * NW, ROWS_EU) void kv_rows_kernel(const KvAtten
                 for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) cm = fmaxf(cm, sc[t][kt][j]);
-                cm = fmaxf(cm, __shfl_xor(cm, 16));
-                cm = fmaxf(cm, __shfl_xor(cm, 32));
+                cm = groups_max(cm);
                 // The reference of a row's exponents need not be its maximum: it moves only when a weight would pass 2^8
                 if (__any((cm - mx[t]) * a.c2 > 8.f)) {
                     const float mn = fmaxf(mx[t], cm), alpha = mn == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mx[t] - mn) * a.c2);
@@ -920,18 +938,26 @@ __global__ __launch_bounds__(64 * NW, ROWS_EU) void kv_rows_kernel(const KvAtten
                 }
                 l[t] += sum[0] + sum[1];
             }
+            constexpr int HG = 4 / KST;                  // output tiles of a step
 #pragma unroll
-            for (int ht = 0; ht < HT; ++ht)
+            for (int q = 0; q < HF / 4; ++q) {
+                u32x4 (&now)[4] = f[(HP + q) & 1];
+                if (q + 1 < HF / 4) {
 #pragma unroll
-                for (int ks = 0; ks < KST; ++ks) {
-                    const u32x4 f = vp[(ht * KST + ks) * 64];
-#pragma unroll
-                    for (int u = 0; u < VS; ++u) {
-                        const u32x4 v = kv_operand<A, C>(f, u, 1.f);
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) mma16<A>(o[t][ht], v, pf[t][ks * VS + u]);
-                    }
+                    for (int j = 0; j < 4; ++j) f[(HP + q + 1) & 1][j] = vp[(q * 4 + 4 + j) * 64];
                 }
+#pragma unroll
+                for (int ks = 0; ks < KST; ++ks)
+#pragma unroll
+                    for (int u = 0; u < VS; ++u)
+#pragma unroll
+                        for (int h = 0; h < HG; ++h) {
+                            const u32x4 v = kv_operand<A, C>(now[h * KST + ks], u, 1.f);
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) mma16<A>(o[t][q * HG + h], v, pf[t][ks * VS + u]);
+                        }
+                __builtin_amdgcn_sched_barrier(0);
+            }
         };
         // A chunk with an edge: keys behind the end and values that are not finite leave V^T (see kv_clean); each wave cleans what it has asked for
         auto clean = [&](const int c) {
@@ -990,9 +1016,7 @@ __global__ __launch_bounds__(64 * NW, ROWS_EU) void kv_rows_kernel(const KvAtten
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        float z = l[t];
-        z += __shfl_xor(z, 16);
-        z += __shfl_xor(z, 32);
+        const float z = groups_sum(l[t]);
         const int row = row0 + t * 16 + m, token = row / a.kv.group, head = kvh * a.kv.group + row % a.kv.group;
         if (row >= rows) continue;
         const size_t at = (size_t)(first + (int64_t)(split * n_tiles + tile) * n_kv + kvh) * (16 * RT) + row - tile * 16 * RT;
