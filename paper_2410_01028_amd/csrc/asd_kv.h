@@ -747,7 +747,7 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
 
 // Many rows (bf16): NW waves with 16 * NT rows each walk a run of chunks together, their fragments in LDS once for all of them.  They come by
 // direct loads into a ring of five half-chunks (K, V^T, K, ..): one barrier per chunk c, behind which K and V^T of c have landed
-// and the slots of c - 1 are asked for anew (V^T of c + 1, K of c + 2).  A SIMD has several waves, one's products beside the other's exponentials.
+// and the slots of c - 1 may be asked for anew (V^T of c + 1, K of c + 2).  A SIMD has several waves, one's products beside the other's exponentials.
 template <class C, int H, int NT, int NW>
 __global__ __launch_bounds__(64 * NW, ROWS_EU) void kv_rows_kernel(const KvAttendArgs a) {
     using A = BF16;
@@ -806,8 +806,8 @@ __global__ __launch_bounds__(64 * NW, ROWS_EU) void kv_rows_kernel(const KvAtten
         uint32_t gone = 0;                               // bit c % 32: chunk c has no page
         bool lost = false;
         int asked = c0;                                  // chunk whose K is asked for next
-        const char *src = nullptr, *src_v = nullptr;     // the K asked for last, and the V^T asked for next; n_bytes 0: nowhere, zeros come back
-        int n_bytes = 0, n_bytes_v = 0, slot_k = 0, slot_v = 1;
+        const char* src = nullptr;                       // the chunk whose K was asked for last; n_bytes 0: nowhere, zeros come back
+        int n_bytes = 0, slot_k = 0, slot_v = 1;
         auto half = [&](const char* from_, const int n, const int slot) {
             // (a descriptor in scalar registers: the loads would be issued lane by lane otherwise)
             from_ = (const char*)((uint64_t)(uint32_t)uniform((int)(uintptr_t)from_) | (uint64_t)(uint32_t)uniform((int)((uintptr_t)from_ >> 32)) << 32);
@@ -816,7 +816,6 @@ __global__ __launch_bounds__(64 * NW, ROWS_EU) void kv_rows_kernel(const KvAtten
             for (int q = 0; q < LH; ++q) frag_to_lds(from_ + (w + NW * q) * 1024, bytes, mem + slot * HF * 64 + (w + NW * q) * 64, lane);
         };
         auto ask_k = [&]() {                             // past the end: the last chunk again
-            src_v = src; n_bytes_v = n_bytes;
             if (asked < c_end) {
                 const int page = __builtin_amdgcn_readlane(pages, page_i - page_base);
                 src = a.kv.pages + (((size_t)max(page, 0) * n_kv + kvh) * cpp + in_page) * L::CHUNK;
@@ -848,10 +847,8 @@ __global__ __launch_bounds__(64 * NW, ROWS_EU) void kv_rows_kernel(const KvAtten
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
-            ask_v(src, n_bytes);
-            ask_k();
-            __builtin_amdgcn_sched_barrier(0);
         };
+        auto ask = [&]() { ask_v(src, n_bytes); ask_k(); };      // V^T of the next chunk, K of the one behind it
         // a chunk that this wave has products for; edge: some of its rows do not see all of it
         auto work = [&](const int c, auto is_edge) {
             constexpr bool edge = decltype(is_edge)::value;
@@ -863,6 +860,7 @@ __global__ __launch_bounds__(64 * NW, ROWS_EU) void kv_rows_kernel(const KvAtten
             // The four score tiles side by side, so that no product waits for the one before it, and the fragments of a step
             // are read while the step before it runs; so too the output tiles below, two at a time (the fences keep that order)
             u32x4 f[2][4];
+            __builtin_amdgcn_s_setprio(1);               // products ahead of another wave's exponentials
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) f[0][kt] = kp[kt * HP * 64];
 #pragma unroll
@@ -884,6 +882,8 @@ __global__ __launch_bounds__(64 * NW, ROWS_EU) void kv_rows_kernel(const KvAtten
                     }
                 __builtin_amdgcn_sched_barrier(0);
             }
+            __builtin_amdgcn_s_setprio(0);
+            ask();
             float vs[4][4];
             if constexpr (L::Q8)
 #pragma unroll
@@ -938,6 +938,7 @@ __global__ __launch_bounds__(64 * NW, ROWS_EU) void kv_rows_kernel(const KvAtten
                 }
                 l[t] += sum[0] + sum[1];
             }
+            __builtin_amdgcn_s_setprio(1);
             constexpr int HG = 4 / KST;                  // output tiles of a step
 #pragma unroll
             for (int q = 0; q < HF / 4; ++q) {
@@ -958,6 +959,7 @@ __global__ __launch_bounds__(64 * NW, ROWS_EU) void kv_rows_kernel(const KvAtten
                         }
                 __builtin_amdgcn_sched_barrier(0);
             }
+            __builtin_amdgcn_s_setprio(0);
         };
         // A chunk with an edge: keys behind the end and values that are not finite leave V^T (see kv_clean); each wave cleans what it has asked for
         auto clean = [&](const int c) {
@@ -997,9 +999,7 @@ __global__ __launch_bounds__(64 * NW, ROWS_EU) void kv_rows_kernel(const KvAtten
             if (c >= c_end) break;
             turn();
             clean(c);
-            if (c < c_my && !((gone >> (c & 31)) & 1u)) {
-                if (c * 64 + 63 > from) work(c, std::true_type{}); else work(c, std::false_type{});
-            }
+            if (c < c_my && !((gone >> (c & 31)) & 1u)) work(c, std::true_type{}); else ask();
             done();
             gone &= ~(1u << (c & 31));
             ++c;
