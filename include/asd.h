@@ -439,7 +439,7 @@ size_t asd_kv_page_bytes(const asd_kv_shape* s);
 /*
  * New rows: queries and keys are normalised per head (x / sqrt(mean x^2 + eps) * gain, where a gain [head_dim] fp32 is given)
  * and rotated, in fp32, and rounded once: queries into q_out, keys and (unchanged) values into the pages.  The first rot_dim
- * dims of a head turn (0: none; a multiple of 8): pairs (j, j + rot_dim/2), or (2j, 2j+1) with interleaved != 0, by the angle
+ * dims of a head turn (0: none; a multiple of 16, for fp32 rows of 8): pairs (j, j + rot_dim/2), or (2j, 2j+1) with interleaved != 0, by the angle
  * whose cosine and sine are rope[(position * rot_dim/2 + j) * 2 ..] (fp32 [rope_positions][rot_dim/2][2]; asd_rope_table makes
  * such a table).  Strides are in elements from row to row, heads lie packed within a row [heads][head_dim]; pointers
  * and strides are multiples of 16 bytes.  q and q_out may be NULL (both: keys and values only) and may be the same buffer.

@@ -9,6 +9,7 @@
 // multiplies is the stored value itself; a floating-point code loses nothing to a scale that is up to 2x too large.
 #pragma once
 #include "asd_common.h"
+#include <type_traits>
 
 // e4m3 codes (cache only); 16 to a lane's piece
 struct FP8 {
@@ -120,14 +121,10 @@ __device__ __forceinline__ int q8_exponent(float top) {
 }
 __device__ __forceinline__ float q8_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
-// four values as codes; what is not finite becomes the code of NaN (the format has no infinity)
-__device__ __forceinline__ uint32_t q8_pack(const float (&v)[4], float inv) {
-    float x[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = finite(v[j]) ? v[j] * inv : __uint_as_float(0x7fc00000u);
-    int p = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
-    p = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], p, true);
-    return (uint32_t)p;
+// four values as codes (the format has no infinity: the caller has made NaN of what is not finite)
+__device__ __forceinline__ uint32_t q8_pack(float a, float b, float c, float d) {
+    const int p = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, p, true);
 }
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
@@ -168,22 +165,14 @@ template <class A, class C> __device__ __forceinline__ u32x4 kv_operand(const u3
     }
 }
 // four consecutive elements of a row
-template <class T> __device__ __forceinline__ void load4(const typename T::elem* p, float (&v)[4]);
-template <> __device__ __forceinline__ void load4<F32>(const float* p, float (&v)[4]) {
-    const float4 x = *(const float4*)p;
-    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-}
-template <> __device__ __forceinline__ void load4<BF16>(const uint16_t* p, float (&v)[4]) {
-    const uint2 x = *(const uint2*)p;
-    v[0] = __uint_as_float(x.x << 16); v[1] = __uint_as_float(x.x & 0xffff0000u);
-    v[2] = __uint_as_float(x.y << 16); v[3] = __uint_as_float(x.y & 0xffff0000u);
-}
 template <class T> __device__ __forceinline__ void store4(typename T::elem* p, const float (&v)[4]) {
     if constexpr (sizeof(typename T::elem) == 4) *(float4*)p = float4{v[0], v[1], v[2], v[3]};
     else *(uint2*)p = uint2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
 }
 
 // ---------------------------------------------------------------- new rows into the cache
+// (token, head) pairs that a workgroup of kv_append_kernel holds: four heads of a tile, but no more than 36 KiB
+__host__ __device__ constexpr int APPEND_SLOTS(int tok, int row_bytes) { return 4 * tok * row_bytes <= 32768 ? 4 * tok : 32768 / row_bytes > tok ? 32768 / row_bytes : tok; }
 struct KvAppendArgs {
     KvArgs kv;
     const void *q, *k, *v;
@@ -191,154 +180,226 @@ struct KvAppendArgs {
     int64_t q_stride, k_stride, v_stride, out_stride;
     const float *q_gain, *k_gain, *rope;
     float eps;
-    int32_t rope_positions, rot, interleaved;
-    int32_t kv_heads_per, q_heads_per, kv_blocks;      // heads of a workgroup; grid rows 0 .. kv_blocks-1 take K and V, the others q
+    int32_t rope_positions, rot;
+    int32_t kv_heads_per, q_heads_per, kv_blocks, blocks;      // heads of a workgroup; of a tile's `blocks` workgroups kv_blocks take K and V, the others q
 };
 
-// A head's vector lies in H / 8 lanes, two units of four dims each, chosen so that both partners of every rotated pair are
-// in one lane: neighbours (interleaved), or dims 4p .. 4p+3 and those rot/2 further on (half layout), the dims behind the
+// A head's vector lies in H / 2DU lanes, two units of 16 bytes (DU dims) each, chosen so that both partners of every rotated pair
+// are in one lane: neighbours (interleaved), or dims p * DU .. and those rot/2 further on (half layout), the dims behind the
 // rotated part after them.  The norm's sum of squares runs over the lanes by shuffles.
-template <class T, int H> struct HeadVec {
-    float x[2][4];
-    int d[2];                                          // first dims of the units
-    __device__ __forceinline__ void place(int p, int rot, bool inter) {
-        const bool pair = !inter && 8 * p < rot;
-        d[0] = pair ? 4 * p : 8 * p;
-        d[1] = pair ? rot / 2 + 4 * p : 8 * p + 4;
+template <class T, int H, bool INTER> struct HeadVec {
+    static constexpr int DU = 16 / (int)sizeof(typename T::elem), LPV = H / (2 * DU);
+    float x[2][DU];
+    // first dims of lane p's units
+    static __device__ __forceinline__ void place(int p, int rot, int (&d)[2]) {
+        const bool pair = !INTER && 2 * DU * p < rot;
+        d[0] = pair ? DU * p : 2 * DU * p;
+        d[1] = pair ? rot / 2 + DU * p : 2 * DU * p + DU;
     }
-    __device__ __forceinline__ void load(const typename T::elem* row) { load4<T>(row + d[0], x[0]); load4<T>(row + d[1], x[1]); }
-    __device__ __forceinline__ void normalise(const float* gain, float eps) {
+    __device__ __forceinline__ void load(const typename T::elem* row, const int (&d)[2]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const u32x4 r = *(const u32x4*)(row + d[i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (DU == 4) x[i][j] = __uint_as_float(r[j]);
+                else { x[i][2 * j] = __uint_as_float(r[j] << 16); x[i][2 * j + 1] = __uint_as_float(r[j] & 0xffff0000u); }
+            }
+        }
+    }
+    static __device__ __forceinline__ u32x4 pack(const float (&v)[DU]) {
+        u32x4 r;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (DU == 4) r[j] = __float_as_uint(v[j]);
+            else r[j] = bf16_pair(v[2 * j], v[2 * j + 1]);
+        }
+        return r;
+    }
+    __device__ __forceinline__ void normalise(const float* gain, float eps, const int (&d)[2]) {
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s += x[i][j] * x[i][j];
+            for (int j = 0; j < DU; ++j) s += x[i][j] * x[i][j];
 #pragma unroll
-        for (int o = 1; o < H / 8; o <<= 1) s += __shfl_xor(s, o);
+        for (int o = 1; o < LPV; o <<= 1) s += __shfl_xor(s, o);
         const float r = 1.f / sqrtf(s * (1.f / H) + eps);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float4 g = *(const float4*)(gain + d[i]);
-            x[i][0] *= r * g.x; x[i][1] *= r * g.y; x[i][2] *= r * g.z; x[i][3] *= r * g.w;
-        }
-    }
-    // cs: (cos, sin) of the position's angles 4p .. 4p+3
-    __device__ __forceinline__ void rotate(const float* cs, bool inter) {
-        const float4 t0 = ((const float4*)cs)[0], t1 = ((const float4*)cs)[1];
-        const float c[4] = {t0.x, t0.z, t1.x, t1.z}, s[4] = {t0.y, t0.w, t1.y, t1.w};
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float& a = inter ? x[j >> 1][(j & 1) * 2] : x[0][j];
-            float& b = inter ? x[j >> 1][(j & 1) * 2 + 1] : x[1][j];
-            const float a1 = a * c[j] - b * s[j], b1 = b * c[j] + a * s[j];
+            for (int j = 0; j < DU; j += 4) {
+                const float4 g = *(const float4*)(gain + d[i] + j);
+                x[i][j] *= r * g.x; x[i][j + 1] *= r * g.y; x[i][j + 2] *= r * g.z; x[i][j + 3] *= r * g.w;
+            }
+    }
+    // cs: (cos, sin) of the angles of the lane's DU pairs
+    __device__ __forceinline__ void rotate(const float4 (&cs)[DU / 2]) {
+        auto turn = [&](float& a, float& b, int j) {
+            const float c = j & 1 ? cs[j / 2].z : cs[j / 2].x, s = j & 1 ? cs[j / 2].w : cs[j / 2].y;
+            const float a1 = a * c - b * s, b1 = b * c + a * s;
             a = a1; b = b1;
+        };
+#pragma unroll
+        for (int j = 0; j < DU; ++j) {
+            if constexpr (INTER) turn(x[2 * j / DU][2 * j % DU], x[2 * j / DU][2 * j % DU + 1], j);
+            else turn(x[0][j], x[1][j], j);
         }
     }
 };
 
-// A workgroup takes up to 16 tokens of one sequence (a tile at positions 16t .. 16t+15, so that a V^T piece belongs to one
-// workgroup) and some heads.  Bound by memory: every row is read once, in 8- or 16-byte pieces that fill their lines, and held
-// in registers from the load to the store.  V goes through LDS to be transposed; a piece all of whose keys are new is
-// written whole, one at the edge of the new rows element by element, so that what the cache holds beside them stays.
-template <class T, class C, int H>
+// A workgroup takes up to TOK tokens of one sequence (a tile at positions TOK * t ..) and some heads.  Bound by memory: every row is read
+// once, 16 bytes a lane, four heads of a token in flight (their angles are read once); what the vector unit does per value is kept short, and
+// values that are not finite are looked for by one comparison of the largest magnitude.  The cache's elements go through LDS, K row by
+// row and V to be transposed, so that they leave in the layout's own 16-byte pieces, whole lines for whole chunks.  A V^T piece some of whose
+// keys are not new is written element by element, so that what the cache holds beside the new rows stays.
+// (Neighbours turn in a kernel of their own: an array whose elements two branches pair differently stays in memory.)
+template <class T, class C, int H, int TOK, bool INTER>
 __global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
     using L = KvLayout<C, H>;
     using E = typename T::elem;
-    constexpr int LPV = H / 8, VPP = 256 / LPV;        // lanes of a vector, vectors of a pass
-    __shared__ __align__(16) typename C::elem vt[16][H];
+    using CE = typename C::elem;
+    using V = HeadVec<T, H, INTER>;
+    constexpr int DU = V::DU, LPV = V::LPV, VPP = 256 / LPV, U = 4;       // dims of a unit, lanes of a vector; vectors of a pass, heads in flight
+    constexpr int RS = H + 16 / (int)sizeof(CE);                          // an LDS row, 16 bytes longer: its pieces fall on different banks
+    constexpr int SLOTS = APPEND_SLOTS(TOK, H * sizeof(CE));              // (token, head) pairs of a workgroup
+    __shared__ __align__(16) CE rows[SLOTS][RS];
+    __shared__ uint8_t exps[SLOTS];
     const int tid = threadIdx.x, lane = tid & 63;
     int seq, tile;
     int64_t first;
     KvSeq s;
-    auto tiles = [](const KvSeq& v) { const int p0 = max(v.len - v.n, 0); return v.n > 0 && v.len > 0 ? (v.len + 15) / 16 - p0 / 16 : 0; };
-    const bool check = blockIdx.x == 0 && blockIdx.y == 0 && tid < 64;
+    auto tiles = [](const KvSeq& v) { return v.n > 0 && v.len > 0 ? (v.len + TOK - 1) / TOK - max(v.len - v.n, 0) / TOK : 0; };
+    // a tile's workgroups side by side: those that run at a time read whole rows, not the same part of many
+    const int item = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks;
+    const bool check = blockIdx.x == 0 && tid < 64;
     KvLanes all;
     all.load(a.kv, 0, lane, check);
-    if (!kv_find(a.kv, all, blockIdx.x, lane, check, tiles, &seq, &tile, &first, &s)) return;
+    if (!kv_find(a.kv, all, item, lane, check, tiles, &seq, &tile, &first, &s)) return;
     const int base = s.len - s.n;                      // position of row 0 (negative: rows in front have no place)
-    const int t16 = max(base, 0) / 16 + tile;
-    const int lo = max(max(base, 0), 16 * t16), hi = min(s.len, 16 * t16 + 16), nt = hi - lo;
-    const bool inter = a.interleaved != 0;
+    const int t0 = (max(base, 0) / TOK + tile) * TOK;
+    const int lo = max(max(base, 0), t0), nt = min(s.len, t0 + TOK) - lo;
     const int vec = tid / LPV, p = tid % LPV;
-    auto angles = [&](int pos) {
-        if (pos >= a.rope_positions) kv_flag(a.kv, ASD_KV_BAD_POS);
-        return a.rope + ((size_t)min(pos, a.rope_positions - 1) * (a.rot / 2) + 4 * p) * 2;
-    };
-    if ((int)blockIdx.y >= a.kv_blocks) {              // queries
-        const int h0 = ((int)blockIdx.y - a.kv_blocks) * a.q_heads_per, nh = min(a.q_heads_per, a.kv.n_h - h0);
-        for (int i = vec; i < nh * nt; i += VPP) {     // (the lanes of a vector take the same turns)
-            const int head = h0 + i % nh, pos = lo + i / nh;
-            const int64_t row = s.r0 + pos - base;
-            HeadVec<T, H> x;
-            x.place(p, a.rot, inter);
-            x.load((const E*)a.q + row * a.q_stride + head * H);
-            if (a.q_gain) x.normalise(a.q_gain, a.eps);
-            if (8 * p < a.rot) x.rotate(angles(pos), inter);
-            E* out = (E*)a.q_out + row * a.out_stride + head * H;
-            store4<T>(out + x.d[0], x.x[0]);
-            store4<T>(out + x.d[1], x.x[1]);
+    int d[2];
+    V::place(p, a.rot, d);
+    // heads h0 .. h0 + nh - 1 of the tile's rows of x, prepared, into sink(vector, token of the tile, head of the workgroup)
+    auto each = [&](const void* x, int64_t stride, int h0, int nh, bool turn, const float* gain, auto sink) {
+        const int uh = nt * nh > VPP ? U : 1, groups = (nh + uh - 1) / uh;      // heads of a lane's turn: one where they would leave lanes idle
+        for (int i = vec; i < nt * groups; i += VPP) {                           // (the lanes of a vector take the same turns)
+            const int token = groups == 1 ? i : i / groups, g0 = groups == 1 ? 0 : i % groups * uh, left = min(nh - g0, uh), pos = lo + token;
+            const E* row = (const E*)x + (s.r0 + (int64_t)(pos - base)) * stride + (h0 + g0) * H;
+            V v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u].load(row + min(u, left - 1) * H, d);
+            float4 cs[DU / 2];
+            turn = turn && 2 * DU * p < a.rot;
+            if (turn) {
+                if (pos >= a.rope_positions) kv_flag(a.kv, ASD_KV_BAD_POS);
+                const float4* at = (const float4*)(a.rope + ((size_t)min(pos, a.rope_positions - 1) * (a.rot / 2) + DU * p) * 2);
+#pragma unroll
+                for (int j = 0; j < DU / 2; ++j) cs[j] = at[j];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (gain) v[u].normalise(gain, a.eps, d);
+                if (turn) v[u].rotate(cs);
+                if (u < left) sink(v[u], token, g0 + u);
+            }
         }
+    };
+    if (block >= a.kv_blocks) {                        // queries
+        const int h0 = (block - a.kv_blocks) * a.q_heads_per;
+        each(a.q, a.q_stride, h0, min(a.q_heads_per, a.kv.n_h - h0), true, a.q_gain, [&](const V& v, int token, int head) {
+            E* out = (E*)a.q_out + (s.r0 + (int64_t)(lo + token - base)) * a.out_stride + (h0 + head) * H;
+            *(u32x4*)(out + d[0]) = V::pack(v.x[0]);
+            *(u32x4*)(out + d[1]) = V::pack(v.x[1]);
+        });
         return;
     }
-    char* chunk0 = (char*)kv_chunk<C, H>(a.kv, seq, t16 / 4, 0);
+    char* chunk0 = (char*)kv_chunk<C, H>(a.kv, seq, t0 / 64, 0);
     if (!chunk0) { if (tid == 0) kv_flag(a.kv, ASD_KV_BAD_PAGE); return; }
     const size_t head_bytes = (size_t)(a.kv.page_tokens / 64) * L::CHUNK;
-    const int h0 = blockIdx.y * a.kv_heads_per, nh = min(a.kv_heads_per, a.kv.n_kv - h0);
-    const int slots = nh * nt;                         // at most 16
-    for (int i = vec; i < 2 * slots; i += VPP) {       // K of all slots, then V
-        const bool isv = i >= slots;
-        const int slot = isv ? i - slots : i, head = h0 + slot / nt, pos = lo + slot % nt, key = pos & 63;
-        const int64_t row = s.r0 + pos - base;
-        HeadVec<T, H> x;
-        x.place(p, a.rot, inter);
-        x.load(isv ? (const E*)a.v + row * a.v_stride + head * H : (const E*)a.k + row * a.k_stride + head * H);
-        if (!isv) {
-            if (a.k_gain) x.normalise(a.k_gain, a.eps);
-            if (8 * p < a.rot) x.rotate(angles(pos), inter);
-        }
-        char* chunk = chunk0 + head * head_bytes;
+    const int h0 = block * a.kv_heads_per, nh = min(a.kv_heads_per, a.kv.n_kv - h0);
+    chunk0 += h0 * head_bytes;
+    const int k0 = lo & 63, k1 = k0 + nt;              // the chunk's new keys; a pair's slot: (key - k0) * nh + head
+    auto keep = [&](const V& v, int token, int head) {
+        const int slot = token * nh + head;
+        CE* row = rows[slot];
         if constexpr (L::Q8) {
-            float top = 0.f;
+            uint32_t top = 0;                          // largest magnitude, as its bits
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) top = fmaxf(top, finite(x.x[u][j]) ? fabsf(x.x[u][j]) : 0.f);
+                for (int j = 0; j < DU; ++j) top = max(top, __float_as_uint(v.x[i][j]) & 0x7fffffffu);
 #pragma unroll
-            for (int o = 1; o < LPV; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-            const int e = q8_exponent(top);
-            const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-            const uint32_t c0 = q8_pack(x.x[0], inv), c1 = q8_pack(x.x[1], inv);
-            if (isv) {
-                *(uint32_t*)&vt[slot][x.d[0]] = c0; *(uint32_t*)&vt[slot][x.d[1]] = c1;
-                if (p == 0) *(uint8_t*)(chunk + 2 * L::K_BYTES + 64 + key) = (uint8_t)(e + 127);
-            } else {
-                *(uint32_t*)(chunk + L::k_off(key, x.d[0])) = c0; *(uint32_t*)(chunk + L::k_off(key, x.d[1])) = c1;
-                if (p == 0) *(uint8_t*)(chunk + 2 * L::K_BYTES + key) = (uint8_t)(e + 127);
+            for (int o = 1; o < LPV; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+            float y[2][DU];
+            const bool odd = top >= 0x7f800000u;       // something is not finite: it becomes NaN, and the scale comes from the rest
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < DU; ++j) y[i][j] = v.x[i][j];
+            if (odd) {
+                top = 0;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < DU; ++j) {
+                        if (finite(y[i][j])) top = max(top, __float_as_uint(y[i][j]) & 0x7fffffffu);
+                        else y[i][j] = __uint_as_float(0x7fc00000u);
+                    }
+#pragma unroll
+                for (int o = 1; o < LPV; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
             }
-        } else {
+            const int e = q8_exponent(__uint_as_float(top));
+            const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-                store4<C>(isv ? &vt[slot][x.d[u]] : (typename C::elem*)(chunk + L::k_off(key, x.d[u])), x.x[u]);
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < DU; j += 4) *(uint32_t*)(row + d[i] + j) = q8_pack(y[i][j] * inv, y[i][j + 1] * inv, y[i][j + 2] * inv, y[i][j + 3] * inv);
+            if (p == 0) exps[slot] = (uint8_t)(e + 127);
+        } else {
+            *(u32x4*)(row + d[0]) = V::pack(v.x[0]);
+            *(u32x4*)(row + d[1]) = V::pack(v.x[1]);
         }
-    }
+    };
+    auto write_exps = [&](int at) {
+        if constexpr (L::Q8)
+            for (int i = tid; i < nh * nt; i += 256) *(uint8_t*)(chunk0 + i % nh * head_bytes + 2 * L::K_BYTES + at + k0 + i / nh) = exps[i];
+    };
+    each(a.k, a.k_stride, h0, nh, true, a.k_gain, keep);
     __syncthreads();
-    constexpr int KV = L::KV, PPT = 16 / KV;           // V^T pieces of a dim in the tile
-    for (int i = tid; i < nh * H * PPT; i += 256) {
-        const int dim = i % H, pc = i / H % PPT, hd = i / (H * PPT);
-        const int k0 = 16 * t16 + pc * KV;             // first position of the piece
-        const int b = max(lo, k0), e = min(hi, k0 + KV);
-        if (b >= e) continue;
-        typename C::elem* dst = (typename C::elem*)(chunk0 + (h0 + hd) * head_bytes + L::v_off(k0 & 63, dim));
-        if (e - b == KV) {
-            u32x4 r;
-            typename C::elem* t = (typename C::elem*)&r;
-#pragma unroll
-            for (int j = 0; j < KV; ++j) t[j] = vt[hd * nt + k0 - lo + j][dim];
-            *(u32x4*)dst = r;
-        } else {
-            for (int j = b; j < e; ++j) dst[j - k0] = vt[hd * nt + j - lo][dim];
+    constexpr int KP = 4 * L::HP * 64, VP = L::HT * L::KST * 64, KV = L::KV;      // pieces of a chunk, in the order in which they lie
+    for (int hd = 0; hd < nh; ++hd)
+        for (int q = tid; q < KP; q += 256) {
+            const int l = q & 63, key = score_key<C>(q / 64 / L::HP, l & 15);
+            if (key < k0 || key >= k1) continue;
+            const CE* src = &rows[(key - k0) * nh + hd][q / 64 % L::HP * 4 * L::KK + (l >> 4) * L::KK];
+            CE* dst = (CE*)(chunk0 + hd * head_bytes) + (size_t)q * L::KK;
+            if constexpr (L::KK * sizeof(CE) == 16) *(u32x4*)dst = *(const u32x4*)src;
+            else *(uint2*)dst = *(const uint2*)src;
         }
-    }
+    write_exps(0);
+    __syncthreads();
+    each(a.v, a.v_stride, h0, nh, false, nullptr, keep);
+    __syncthreads();
+    for (int hd = 0; hd < nh; ++hd)
+        for (int q = tid; q < VP; q += 256) {
+            const int l = q & 63, dim = q / 64 / L::KST * 16 + (l & 15), first_key = q / 64 % L::KST * 4 * KV + (l >> 4) * KV;
+            const int b = max(k0, first_key), e = min(k1, first_key + KV);
+            if (b >= e) continue;
+            CE* dst = (CE*)(chunk0 + hd * head_bytes + L::K_BYTES) + (size_t)q * KV;
+            if (e - b == KV) {
+                u32x4 r;
+                CE* t = (CE*)&r;
+#pragma unroll
+                for (int j = 0; j < KV; ++j) t[j] = rows[(first_key + j - k0) * nh + hd][dim];
+                *(u32x4*)dst = r;
+            } else {
+                for (int j = b; j < e; ++j) dst[j - first_key] = rows[(j - k0) * nh + hd][dim];
+            }
+        }
+    write_exps(64);
 }
 
 // ---------------------------------------------------------------- rows out of the cache

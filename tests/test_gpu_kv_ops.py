@@ -74,7 +74,7 @@ LENS = [(1, 1), (3, 3), (0, 9), (16, 80), (17, 64), (5, 131), (70, 70), (1, 200)
 
 
 @pytest.mark.parametrize("dtype,kv", COMBOS)
-@pytest.mark.parametrize("h,heads,kv_heads,rot,inter,norm", [(128, 8, 2, 128, False, True), (128, 3, 3, 64, True, False), (64, 10, 5, 24, False, False),
+@pytest.mark.parametrize("h,heads,kv_heads,rot,inter,norm", [(128, 8, 2, 128, False, True), (128, 3, 3, 64, True, False), (64, 10, 5, 48, False, False),
                                                              (64, 4, 4, 64, True, True), (32, 6, 2, 16, False, True), (32, 1, 1, 0, False, False)])
 def test_append_and_read(dtype, kv, h, heads, kv_heads, rot, inter, norm):
     p = Pool(dtype, kv, heads, kv_heads, h, 64, LENS, seed=h + rot)

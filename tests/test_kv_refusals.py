@@ -54,7 +54,7 @@ def test_batches(kw, text):
 
 @pytest.mark.parametrize("name,kw", [("append", dict(k=None)), ("append", dict(v=None)), ("append", dict(out=None)), ("append", dict(q=None)), ("append", dict(prep=None)),
                                      ("append", dict(k=P + 8)), ("append", dict(ks=127)), ("append", dict(ks=64)), ("append", dict(qs=504)), ("append", dict(os=-512)),
-                                     ("append", dict(prep=asd.KvPrep(None, None, 0, P, 10, 12, 0))), ("append", dict(prep=asd.KvPrep(None, None, 0, P, 10, 72, 0))),
+                                     ("append", dict(prep=asd.KvPrep(None, None, 0, P, 10, 12, 0))), ("append", dict(prep=asd.KvPrep(None, None, 0, P, 10, 72, 0))), ("append", dict(prep=asd.KvPrep(None, None, 0, P, 10, 24, 0))),
                                      ("append", dict(prep=asd.KvPrep(None, None, 0, None, 10, 64, 0))), ("append", dict(prep=asd.KvPrep(None, None, 0, P, 0, 64, 0))),
                                      ("append", dict(prep=asd.KvPrep(P + 4, None, 0, P, 10, 64, 0))), ("append", dict(prep=asd.KvPrep(P, P, -1.0, P, 10, 64, 0))),
                                      ("append", dict(prep=asd.KvPrep(P, P, float("nan"), P, 10, 64, 0))),
