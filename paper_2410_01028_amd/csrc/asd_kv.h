@@ -181,7 +181,7 @@ struct KvAppendArgs {
     const float *q_gain, *k_gain, *rope;
     float eps;
     int32_t rope_positions, rot;
-    int32_t kv_heads_per, q_heads_per, kv_blocks, blocks;      // heads of a workgroup; of a tile's `blocks` workgroups kv_blocks take K and V, the others q
+    int32_t kv_heads_per, q_heads_per, kv_blocks, blocks;      // heads of a workgroup; of a tile's `blocks` workgroups kv_blocks take K, as many V, the others q
 };
 
 // A head's vector lies in H / 2DU lanes, two units of 16 bytes (DU dims) each, chosen so that both partners of every rotated pair
@@ -307,8 +307,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
             }
         }
     };
-    if (block >= a.kv_blocks) {                        // queries
-        const int h0 = (block - a.kv_blocks) * a.q_heads_per;
+    if (block >= 2 * a.kv_blocks) {                    // queries
+        const int h0 = (block - 2 * a.kv_blocks) * a.q_heads_per;
         each(a.q, a.q_stride, h0, min(a.q_heads_per, a.kv.n_h - h0), true, a.q_gain, [&](const V& v, int token, int head) {
             E* out = (E*)a.q_out + (s.r0 + (int64_t)(lo + token - base)) * a.out_stride + (h0 + head) * H;
             *(u32x4*)(out + d[0]) = V::pack(v.x[0]);
@@ -316,11 +316,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
         });
         return;
     }
-    char* chunk0 = (char*)kv_chunk<C, H>(a.kv, seq, t0 / 64, 0);
-    if (!chunk0) { if (tid == 0) kv_flag(a.kv, ASD_KV_BAD_PAGE); return; }
-    const size_t head_bytes = (size_t)(a.kv.page_tokens / 64) * L::CHUNK;
-    const int h0 = block * a.kv_heads_per, nh = min(a.kv_heads_per, a.kv.n_kv - h0);
-    chunk0 += h0 * head_bytes;
+    const bool isv = block >= a.kv_blocks;
+    const int h0 = (isv ? block - a.kv_blocks : block) * a.kv_heads_per, nh = min(a.kv_heads_per, a.kv.n_kv - h0);
     const int k0 = lo & 63, k1 = k0 + nt;              // the chunk's new keys; a pair's slot: (key - k0) * nh + head
     auto keep = [&](const V& v, int token, int head) {
         const int slot = token * nh + head;
@@ -363,14 +360,16 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
             *(u32x4*)(row + d[1]) = V::pack(v.x[1]);
         }
     };
-    auto write_exps = [&](int at) {
-        if constexpr (L::Q8)
-            for (int i = tid; i < nh * nt; i += 256) *(uint8_t*)(chunk0 + i % nh * head_bytes + 2 * L::K_BYTES + at + k0 + i / nh) = exps[i];
-    };
-    each(a.k, a.k_stride, h0, nh, true, a.k_gain, keep);
+    if (isv) each(a.v, a.v_stride, h0, nh, false, nullptr, keep);
+    else each(a.k, a.k_stride, h0, nh, true, a.k_gain, keep);
+    char* chunk0 = (char*)kv_chunk<C, H>(a.kv, seq, t0 / 64, h0);
+    if (!chunk0) { if (tid == 0) kv_flag(a.kv, ASD_KV_BAD_PAGE); return; }
+    const size_t head_bytes = (size_t)(a.kv.page_tokens / 64) * L::CHUNK;
     __syncthreads();
+    if constexpr (L::Q8)
+        for (int i = tid; i < nh * nt; i += 256) *(uint8_t*)(chunk0 + i % nh * head_bytes + 2 * L::K_BYTES + 64 * isv + k0 + i / nh) = exps[i];
     constexpr int KP = 4 * L::HP * 64, VP = L::HT * L::KST * 64, KV = L::KV;      // pieces of a chunk, in the order in which they lie
-    for (int hd = 0; hd < nh; ++hd)
+    for (int hd = 0; hd < nh && !isv; ++hd)
         for (int q = tid; q < KP; q += 256) {
             const int l = q & 63, key = score_key<C>(q / 64 / L::HP, l & 15);
             if (key < k0 || key >= k1) continue;
@@ -379,11 +378,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
             if constexpr (L::KK * sizeof(CE) == 16) *(u32x4*)dst = *(const u32x4*)src;
             else *(uint2*)dst = *(const uint2*)src;
         }
-    write_exps(0);
-    __syncthreads();
-    each(a.v, a.v_stride, h0, nh, false, nullptr, keep);
-    __syncthreads();
-    for (int hd = 0; hd < nh; ++hd)
+    for (int hd = 0; hd < nh && isv; ++hd)
         for (int q = tid; q < VP; q += 256) {
             const int l = q & 63, dim = q / 64 / L::KST * 16 + (l & 15), first_key = q / 64 % L::KST * 4 * KV + (l >> 4) * KV;
             const int b = max(k0, first_key), e = min(k1, first_key + KV);
@@ -399,7 +394,6 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
                 for (int j = b; j < e; ++j) dst[j - first_key] = rows[(j - k0) * nh + hd][dim];
             }
         }
-    write_exps(64);
 }
 
 // ---------------------------------------------------------------- rows out of the cache

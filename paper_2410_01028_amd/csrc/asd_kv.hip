@@ -179,7 +179,7 @@ int asd_kv_append(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_pre
     const int q_blocks = q ? (s->n_heads + a.q_heads_per - 1) / a.q_heads_per : 0;
     // tiles at positions divisible by tok: rows / tok and two more at a sequence's ends, but no more than it has rows
     const int64_t loose = b->n_rows / tok + 2 * seqs;
-    a.blocks = a.kv_blocks + q_blocks;
+    a.blocks = 2 * a.kv_blocks + q_blocks;
     const int64_t grid = (loose < b->n_rows ? loose : b->n_rows) * a.blocks;
     if (grid >= (int64_t)1 << 31) return refuse(ASD_E_INVAL, "asd_kv_append: the batch is too large");
     by_shape(s, [&](auto t, auto c, auto h) {
