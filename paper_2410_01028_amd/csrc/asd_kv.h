@@ -369,6 +369,23 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
     if constexpr (L::Q8)
         for (int i = tid; i < nh * nt; i += 256) *(uint8_t*)(chunk0 + i % nh * head_bytes + 2 * L::K_BYTES + 64 * isv + k0 + i / nh) = exps[i];
     constexpr int KP = 4 * L::HP * 64, VP = L::HT * L::KST * 64, KV = L::KV;      // pieces of a chunk, in the order in which they lie
+    if (TOK == 16 && !isv) {                           // few keys: by rows
+        constexpr int PR = H / L::KK;                  // pieces of a row
+        for (int i = tid; i < nh * nt * PR; i += 256) {
+            const int slot = i / PR, dim = i % PR * L::KK, key = k0 + slot / nh;
+            CE* dst = (CE*)(chunk0 + slot % nh * head_bytes + L::k_off(key, dim));
+            if constexpr (L::KK * sizeof(CE) == 16) *(u32x4*)dst = *(const u32x4*)&rows[slot][dim];
+            else *(uint2*)dst = *(const uint2*)&rows[slot][dim];
+        }
+        return;
+    }
+    if (TOK == 16 && nt < KV) {                        // ... and elements
+        for (int i = tid; i < nh * nt * H; i += 256) {
+            const int slot = i / H, dim = i % H, key = k0 + slot / nh;
+            *(CE*)(chunk0 + slot % nh * head_bytes + L::v_off(key, dim)) = rows[slot][dim];
+        }
+        return;
+    }
     for (int hd = 0; hd < nh && !isv; ++hd)
         for (int q = tid; q < KP; q += 256) {
             const int l = q & 63, key = score_key<C>(q / 64 / L::HP, l & 15);
@@ -486,12 +503,12 @@ struct KvAttendArgs {
     int64_t q_stride, out_stride;
     float c2;                       // scale * log2(e)
     float *o_part, *ml_part;        // [item][rows of a tile][H] unnormalised sums; [item][rows][2] (maximum, sum)
-    int32_t target_log2;            // work items to cut the batch into
+    int32_t target;                 // work items to cut the batch into
     int32_t min_run;                // chunks that are worth a run
     int32_t cut;                    // 0: every tile's keys stay together
 };
 // How a batch is cut.  The rows of a sequence and KV head are its new tokens x the heads of the group; a tile is 16 * NT of
-// them.  With `cut`, all tiles' key ranges are cut into runs of `run` chunks, the same for every sequence, so that about 2^target_log2 items come out
+// them.  With `cut`, all tiles' key ranges are cut into runs of `run` chunks, the same for every sequence, so that about `target` items come out
 // whatever the lengths are: one long conversation among short ones is spread over the card.
 template <int NT> __device__ __forceinline__ int kv_tiles(const KvArgs& a, const KvSeq& v) { return (int)(((int64_t)v.n * a.group + 16 * NT - 1) / (16 * NT)); }
 template <int NT> __device__ __forceinline__ int kv_run(const KvAttendArgs& a, const KvLanes& all, int lane) {
@@ -503,8 +520,8 @@ template <int NT> __device__ __forceinline__ int kv_run(const KvAttendArgs& a, c
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);
     }
-    const int64_t run = ((t * a.kv.n_kv - 1) >> a.target_log2) + 1;
-    return uniform((int)min(max(run, (int64_t)a.min_run), (int64_t)1 << 28));
+    const int run = (int)fminf((float)(t * a.kv.n_kv) / (float)a.target, 1e8f) + 1;
+    return uniform(max(run, a.min_run));
 }
 // runs of a sequence, of equal length: its chunks / run, to the nearest
 __device__ __forceinline__ int kv_splits(const KvSeq& v, int run) { return max(1, (int)(((int64_t)(v.len + 63) / 64 + run / 2) / run)); }

@@ -94,7 +94,7 @@ int units() {
 
 #ifdef KV_DEV
 #include <cstdlib>
-#define DEV_TUNE if (getenv("KV_TL")) p.target_log2 = atoi(getenv("KV_TL")); if (getenv("KV_MR")) p.min_run = atoi(getenv("KV_MR"));
+#define DEV_TUNE if (getenv("KV_TL")) p.target = atoi(getenv("KV_TL")); if (getenv("KV_MR")) p.min_run = atoi(getenv("KV_MR"));
 #else
 #define DEV_TUNE
 #endif
@@ -102,7 +102,7 @@ int units() {
 struct AttendPlan {
     int nt;                        // 16-row column blocks of a tile
     bool rows;                     // kv_rows_kernel
-    int32_t target_log2, max_tiles, min_run;
+    int32_t target, max_tiles, min_run;
     int64_t grid;                  // most work items
     bool join;                     // some sequence's keys may be cut
     size_t o_bytes, bytes;
@@ -117,15 +117,13 @@ AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b) {
     p.rows = s->dtype == ASD_DT_BF16 && s->head_dim >= 64 && rows > 64;
     if (p.rows) p.nt = 8;
     p.min_run = 16;
-    p.target_log2 = 0;
-    while ((2 << p.target_log2) <= 4 * units()) ++p.target_log2;
+    p.target = 4 * units();
     p.max_tiles = (int32_t)((int64_t)b->n_rows * group / (16 * p.nt) + (b->n_seqs < b->n_rows ? b->n_seqs : b->n_rows));
     const int64_t whole = (int64_t)p.max_tiles * s->n_kv_heads;
     // No cut where the tiles alone are work enough for every compute unit, or the keys are too few
-    auto target = [&] { return (int64_t)1 << p.target_log2; };
     DEV_TUNE
-    p.join = (chunks + p.min_run / 2) / p.min_run > 1 && !(p.rows && whole >= target());
-    p.grid = p.join ? whole + target() : whole;
+    p.join = (chunks + p.min_run / 2) / p.min_run > 1 && !(p.rows && whole >= p.target);
+    p.grid = p.join ? whole + p.target : whole;
     if (p.join && whole * ((chunks + p.min_run / 2) / p.min_run) < p.grid) p.grid = whole * ((chunks + p.min_run / 2) / p.min_run);
     if (p.join) {
         p.o_bytes = ((size_t)p.grid * 16 * p.nt * s->head_dim * 4 + 255) / 256 * 256;
@@ -213,7 +211,7 @@ int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, i
     a.q = q; a.out = out; a.q_stride = q_stride; a.out_stride = out_stride;
     a.c2 = (float)((double)scale * 1.4426950408889634074);
     a.o_part = (float*)workspace; a.ml_part = (float*)((char*)workspace + p.o_bytes);
-    a.target_log2 = p.target_log2; a.cut = p.join; a.min_run = p.min_run;
+    a.target = p.target; a.cut = p.join; a.min_run = p.min_run;
     const hipStream_t stream = (hipStream_t)hip_stream;
     const dim3 join_grid((unsigned)((int64_t)p.max_tiles * s->n_kv_heads), p.nt);
     auto go = [&](auto t, auto c, auto h, auto nt) {
