@@ -469,6 +469,16 @@ int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, i
 int asd_kv_read(const asd_kv_shape* s, const asd_kv_batch* b, void* k_out, int64_t k_stride, void* v_out, int64_t v_stride, void* hip_stream);
 
 /*
+ * An engine's own cache as such pages: fills the shape and, in the batch, one layer's pages, the engine's page table and its one
+ * sequence's capacity; row_start, kv_len, n_rows and max_new are the caller's (the engine's sequence is n_seqs = 1).  With it a
+ * sequence is taken out of an engine (asd_kv_read) into other pages, of 8 bits say, and put back later (asd_kv_append without norm and
+ * rotation, then asd_set_kv_len, after which the next pass starts at position n; asd_decode with mask_mode 0 or 2 needs a prompt pass of its own
+ * first, as its averages are not kept).  Work on the engine's pages belongs on the engine's stream.
+ */
+int asd_kv_view(asd_engine* e, int32_t layer, asd_kv_shape* s, asd_kv_batch* b);
+int asd_set_kv_len(asd_engine* e, int32_t n);
+
+/*
  * Rotary table [positions][rot_dim/2][cos, sin] in fp32, computed in double: angle = position * f_j, f_j = theta^(-2j / rot_dim),
  * changed by `kind` for contexts longer than the trained one (factor >= 1; r = trained * f_j / 2 pi is the number of turns over it):
  *   ASD_ROPE_PLAIN   f_j as it is

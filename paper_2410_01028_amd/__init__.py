@@ -154,6 +154,8 @@ def _kv_lib():
         L.asd_kv_attend.argtypes = [shape, batch, vp, i64, vp, i64, ctypes.c_float, vp, sz, vp]
         L.asd_kv_read.argtypes = [shape, batch, vp, i64, vp, i64, vp]
         L.asd_rope_table.argtypes = [ctypes.POINTER(Rope), i32, vp, vp]
+        L.asd_kv_view.argtypes = [vp, i32, shape, batch]
+        L.asd_set_kv_len.argtypes = [vp, i32]
         _kv_ready = True
     return L
 
@@ -292,6 +294,47 @@ class Engine:
         v = np.empty_like(k)
         self._ck(lib().asd_get_kv(self._h, layer, pos0, n, k.ctypes.data, v.ctypes.data))
         return k, v
+
+    def kv_cache(self, layer: int):
+        """(KVCache over the engine's own pages of one layer, its page table [1, pages]): asd_kv_view.  Work on them belongs on
+        the engine's stream, and they live as long as the engine."""
+        s, b = KvShape(), KvBatch()
+        self._ck(_kv_lib().asd_kv_view(self._h, layer, s, b))
+        each = kv_page_bytes(s.n_heads, s.n_kv_heads, s.head_dim, s.page_tokens, s.dtype, s.kv_dtype)
+        part = lambda at, n: self.arena[at - self.arena.data_ptr():][:n]
+        table = part(b.page_table, 4 * b.n_pages).view(self._torch.int32).view(1, b.n_pages)
+        return KVCache(part(b.pages, each * b.n_pages), s.n_heads, s.n_kv_heads, s.head_dim, s.page_tokens, s.dtype, s.kv_dtype), table
+
+    def park(self, caches, page_table) -> int:
+        """Copy the engine's sequence (positions 0 .. kv_len-1) into other pages, one KVCache per layer, 8-bit ones say, with the page table
+        [1, pages] of its place there (int32, on the device); returns its length.  Enqueued on the engine's stream, behind the current one's work."""
+        n = self.kv_len
+        if n:
+            self._move(n, [self.kv_cache(l) for l in range(self.cfg.n_layers)], [(c, page_table) for c in caches])
+        return n
+
+    def resume(self, caches, page_table, n: int):
+        """Put a sequence of n tokens that park() has copied back into the engine: the next pass starts at position n."""
+        if n < 0 or n > self.cfg.max_seq:
+            raise AsdError(E_INVAL, f"length {n} outside the cache capacity {self.cfg.max_seq}")
+        if n:
+            self._move(n, [(c, page_table) for c in caches], [self.kv_cache(l) for l in range(self.cfg.n_layers)])
+        self._ck(_kv_lib().asd_set_kv_len(self._h, n))
+
+    def _move(self, n: int, source, target):
+        """Rows 0 .. n-1 of every layer out of `source` into `target`: (KVCache, page table) pairs."""
+        if len(source) != self.cfg.n_layers or len(target) != self.cfg.n_layers:
+            raise AsdError(E_INVAL, f"one cache for each of the {self.cfg.n_layers} layers")
+        torch = self._torch
+        self.stream.wait_stream(torch.cuda.current_stream(self.device))
+        with torch.cuda.stream(self.stream):
+            rows, length = torch.tensor([0, n], dtype=torch.int32, device=self.device), torch.tensor([n], dtype=torch.int32, device=self.device)
+            for (a, a_table), (b, b_table) in zip(source, target):
+                both = [KVBatch(t, rows, length, n, n, n) for t in (a_table, b_table)]
+                k, v = a.read(both[0])
+                b.append(both[1], None, k, v)
+                for batch in both:
+                    batch.check()
 
     def reset(self):
         self._ck(lib().asd_reset(self._h))

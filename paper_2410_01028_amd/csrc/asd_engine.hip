@@ -1496,6 +1496,28 @@ int asd_get_kv(asd_engine* e, int32_t layer, int32_t pos0, int32_t n, float* k_o
     return ASD_OK;
 }
 
+int asd_kv_view(asd_engine* e, int32_t layer, asd_kv_shape* s, asd_kv_batch* b) {
+    if (!e) return ASD_E_INVAL;
+    if (!s || !b) return fail(e, ASD_E_INVAL, "shape and batch must be given");
+    if (layer < 0 || layer >= e->c.n_layers) return fail(e, ASD_E_INVAL, "layer %d out of range", layer);
+    *s = asd_kv_shape{e->c.n_heads, e->c.n_kv_heads, e->c.head_dim, e->c.page_tokens, e->c.dtype, e->c.dtype};
+    *b = asd_kv_batch{};
+    b->pages = e->kv + (size_t)layer * e->kv_layer_bytes;
+    b->page_table = e->page_table;
+    b->n_pages = b->table_stride = e->n_pages;
+    b->n_seqs = 1;
+    b->max_len = capacity(e);
+    return ASD_OK;
+}
+
+int asd_set_kv_len(asd_engine* e, int32_t n) {
+    if (!e) return ASD_E_INVAL;
+    if (n < 0 || n > capacity(e)) return fail(e, ASD_E_INVAL, "length %d outside the cache capacity %d", n, capacity(e));
+    e->kv_len = n;
+    e->acs_valid = false;               // (the averages belong to the prompt that was in the cache)
+    return ASD_OK;
+}
+
 // host copy of the input generator's stream key and constants (pure integer / one sqrt / one pow)
 static uint64_t h_mix64(uint64_t z) {
     z ^= z >> 30; z *= 0xBF58476D1CE4E5B9ULL;

@@ -198,24 +198,122 @@ def test_attend(dtype, kv, lens, h, heads, kv_heads, page):
 
 
 @pytest.mark.parametrize("dtype,kv", COMBOS)
-def test_values_that_are_not_finite_stay_where_they_are_seen(dtype, kv):
-    """Infinities and NaN in V and NaN in K at keys that some rows of the call do not see."""
-    lens = [(40, 100), (6, 6), (90, 130)]
-    p = Pool(dtype, kv, 4, 2, 64, 64, lens, seed=1)
-    total, news = [b for _, b in lens], [a for a, _ in lens]
-    k, v = p.normal(sum(total), 2, 64), p.normal(sum(total), 2, 64)
+@pytest.mark.parametrize("news", [(40, 6, 90), (5, 3, 4), (1, 6, 1)], ids=["many rows", "drafts", "tokens"])
+@pytest.mark.parametrize("h", [64, 128])
+def test_values_that_are_not_finite_stay_where_they_are_seen(dtype, kv, news, h):
+    """Infinities and NaN in V and NaN in K at keys that some rows of the call do not see, and in chunks that all rows see."""
+    total = [100, 6, 130]
+    p = Pool(dtype, kv, 4, 2, h, 64, list(zip(news, total)), seed=1)
+    k, v = p.normal(sum(total), 2, h), p.normal(sum(total), 2, h)
     v[70, 0, 3], v[95, 0, 7], v[95, 1, 9], v[97, 0, 7], v[103, 1, 60], v[220, 0, 33] = math.inf, math.inf, math.nan, -math.inf, -math.inf, math.nan
+    v[110, 1, 2], v[233, 1, 5] = math.inf, -math.inf
     k[104, 0, 5] = math.nan
     whole = p.batch(total, total)
     p.cache.append(whole, None, k, v)
     k, v = (torch.split(x, total) for x in p.cache.read(whole))
     b = p.batch(news, total)
-    q = p.normal(sum(news), 4, 64)
+    q = p.normal(sum(news), 4, h)
     out = p.cache.attend(b, q)
     b.check()
-    assert bool(out[40 + 4:40 + 6, :2].isnan().all()) and bool(out[40 + 4:40 + 6, 2:, :60].isfinite().all())      # the K of key 4, its own KV head
-    check_attend(p, [40], total[:1], q[:40], out[:40], k[:1], v[:1], 0.125)
-    check_attend(p, [90], total[2:], q[46:], out[46:], k[2:], v[2:], 0.125)
+    one, two = news[0], news[0] + news[1]
+    assert bool(out[two - 2:two, :2].isnan().all()) and bool(out[two - 2:two, 2:, :60].isfinite().all())      # the K of key 4, its own KV head
+    check_attend(p, [one], total[:1], q[:one], out[:one], k[:1], v[:1], h ** -0.5)
+    check_attend(p, [news[2]], total[2:], q[two:], out[two:], k[2:], v[2:], h ** -0.5)
+
+
+@pytest.mark.parametrize("kv", ["fp8", "bf16"])
+def test_long_and_lopsided_batches(kv):
+    """One long sequence among short ones: its keys are cut into runs and joined, for a token, a few rows and a chunk of many."""
+    for news, total in (((1, 1, 1, 1), (20000, 40, 1, 700)), ((6, 0, 2, 6), (9000, 40, 2, 7000)), ((150, 1, 90, 3), (6000, 40, 90, 2100))):
+        p = Pool("bf16", kv, 8, 2, 128, 256, list(zip(news, total)), seed=3)
+        k, v = p.fill()
+        b = p.batch(news, total)
+        q = p.normal(sum(news), 8, 128, scale=2.0)
+        out = p.cache.attend(b, q)
+        b.check()
+        check_attend(p, news, total, q, out, k, v, 128 ** -0.5)
+
+
+def test_many_sequences():
+    """More sequences than a wave looks at at a time, some without new rows."""
+    lens = [(i % 3, 1 + (i * 37) % 150 + i % 3) for i in range(333)]
+    p = Pool("bf16", "fp8", 4, 2, 64, 64, lens, seed=6)
+    k, v = p.fill()
+    news, total = [a for a, _ in lens], [b for _, b in lens]
+    b = p.batch(news, total)
+    q, kn, vn = p.normal(sum(news), 4, 64), p.normal(sum(news), 2, 64), p.normal(sum(news), 2, 64)
+    turned = p.cache.append(b, q, kn, vn)
+    assert torch.equal(turned, q)
+    whole = p.batch(total, total)
+    k, v = (torch.split(x, total) for x in p.cache.read(whole))
+    out = p.cache.attend(b, q)
+    b.check(), whole.check()
+    check_attend(p, news, total, q, out, k, v, 0.125)
+
+
+def test_pages_far_apart():
+    """Offsets past 2^32 bytes: a pool of more than 8 GiB, the sequence's pages at its ends."""
+    args = (8, 8, 128, 256, asd.DT_BF16, asd.DT_BF16)
+    each = asd.kv_page_bytes(*args)
+    n = 9 * 2 ** 30 // each
+    pages = torch.empty(n * each, dtype=torch.uint8, device=DEV)
+    cache = asd.KVCache(pages, *args)
+    g = torch.Generator(DEV).manual_seed(0)
+    k, v, q = (torch.randn(600, 8, 128, generator=g, device=DEV).bfloat16() for _ in range(3))
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)      # noqa: E731
+    whole = asd.KVBatch(i32([[n - 1, 0, n - 2]]), i32([0, 600]), i32([600]), 600, 600, 600)
+    turned = cache.append(whole, q, k, v)
+    rk, rv = cache.read(whole)
+    assert torch.equal(turned, q) and torch.equal(rk, k) and torch.equal(rv, v)
+    out = cache.attend(whole, q)
+    few = asd.KVBatch(whole.page_table, i32([0, 2]), whole.kv_len, 2, 2, 600)
+    out2 = cache.attend(few, q[598:])
+    whole.check(), few.check()
+    want, size, big = attention(q, k, v, 0, 128 ** -0.5)
+    e = 2 * 128 * 2.0 ** -24 * big[..., None] + 2.0 ** -20 + 600 * 2.0 ** -24 + 2.0 ** -8
+    close(out, want, size * e + (want.abs() + size * e) * 2.0 ** -8, "rows")
+    close(out2, want[598:], (size * e + (want.abs() + size * e) * 2.0 ** -8)[598:], "few")
+
+
+def test_in_place_and_aligned_slices():
+    """Queries prepared in place; rows with strides; pages that are a slice of a larger buffer."""
+    args = (4, 2, 64, 64, asd.DT_BF16, asd.DT_FP8)
+    each = asd.kv_page_bytes(*args)
+    buffer = torch.zeros(16 + 3 * each, dtype=torch.uint8, device=DEV)
+    cache = asd.KVCache(buffer[16:], *args)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)      # noqa: E731
+    b = asd.KVBatch(i32([[2, 0]]), i32([0, 70]), i32([70]), 70, 70, 128)
+    fused = torch.randn(70, 10, 64, device=DEV).bfloat16()
+    q, k, v = fused[:, :4], fused[:, 4:6], fused[:, 6:8]
+    table, gain = asd.rope_table(64, 70), torch.full((64,), 1.5, device=DEV)
+    apart = cache.append(b, q.clone(), k, v, rope=table, rot_dim=64, q_gain=gain)
+    rest = fused[:, 4:].clone()
+    assert cache.append(b, q, k, v, q_out=q, rope=table, rot_dim=64, q_gain=gain) is q
+    assert torch.equal(q, apart) and torch.equal(fused[:, 4:], rest) and bool((buffer[:16] == 0).all())
+    b.check()
+
+
+def test_refusals_of_the_binding():
+    p = Pool("bf16", "fp8", 4, 2, 64, 64, [(2, 10)])
+    p.fill()
+    b = p.batch([2], [10])
+    q, k = p.normal(2, 4, 64), p.normal(2, 2, 64)
+    for bad in (q.float(), q[:1], q[:, :3], q.transpose(0, 1), q.cpu(), p.normal(2, 4, 128)[..., ::2], p.normal(2, 8, 64)[:, ::2]):
+        with pytest.raises(asd.AsdError):
+            p.cache.attend(b, bad)
+    with pytest.raises(asd.AsdError):
+        p.cache.attend(b, q, workspace=torch.empty(4, dtype=torch.uint8))
+    with pytest.raises(asd.AsdError):
+        p.cache.append(b, None, k, k, q_out=q)
+    for kw in (dict(rope=torch.zeros(10, 32, 2, device=DEV).double(), rot_dim=64), dict(rope=torch.zeros(10, 16, 2, device=DEV), rot_dim=64), dict(rot_dim=64),
+               dict(q_gain=torch.ones(32, device=DEV)), dict(k_gain=torch.ones(64))):
+        with pytest.raises(asd.AsdError):
+            p.cache.append(b, q, k, k, **kw)
+    for bad in ((p.d_table.long(), b.row_start, b.kv_len), (p.d_table, b.row_start[:1], b.kv_len), (p.d_table, b.row_start, b.kv_len.cpu()), (p.table, b.row_start.cpu(), b.kv_len.cpu())):
+        with pytest.raises(asd.AsdError):
+            asd.KVBatch(*bad, n_rows=2, max_new=2, max_len=10)
+    with pytest.raises(asd.AsdError):
+        asd.KVCache(p.pages.view(-1)[:-1], 4, 2, 64, 64)
 
 
 def test_rows_without_keys_are_zero():

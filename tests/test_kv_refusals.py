@@ -84,3 +84,9 @@ def test_rope_tables(kw):
     ok = asd.Rope(0, 64, 1e4, 2.0, 1.0, 4.0, 4096.0, 1.0)
     for positions, table in ((0, P), (1 << 25, P), (10, None), (10, P + 4)):
         assert asd._kv_lib().asd_rope_table(ok, positions, table, None) == asd.E_INVAL
+
+
+def test_engine_calls_without_an_engine():
+    L = asd._kv_lib()
+    assert L.asd_kv_view(None, 0, asd.KvShape(), asd.KvBatch()) == asd.E_INVAL
+    assert L.asd_set_kv_len(None, 0) == asd.E_INVAL
