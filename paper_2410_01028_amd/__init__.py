@@ -145,14 +145,15 @@ def _kv_lib():
     L = lib()
     if not _kv_ready:
         vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
-        shape, batch, prep = ctypes.POINTER(KvShape), ctypes.POINTER(KvBatch), ctypes.POINTER(KvPrep)
+        shape, batch = ctypes.POINTER(KvShape), ctypes.POINTER(KvBatch)
         L.asd_kv_page_bytes.restype = sz
         L.asd_kv_page_bytes.argtypes = [shape]
-        L.asd_kv_append.argtypes = [shape, batch, prep, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+        # (structures by address: a pointer object per call costs as much as the rest of the marshalling)
+        L.asd_kv_append.argtypes = [vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp]
         L.asd_kv_attend_workspace.restype = sz
-        L.asd_kv_attend_workspace.argtypes = [shape, batch]
-        L.asd_kv_attend.argtypes = [shape, batch, vp, i64, vp, i64, ctypes.c_float, vp, sz, vp]
-        L.asd_kv_read.argtypes = [shape, batch, vp, i64, vp, i64, vp]
+        L.asd_kv_attend_workspace.argtypes = [vp, vp]
+        L.asd_kv_attend.argtypes = [vp, vp, vp, i64, vp, i64, ctypes.c_float, vp, sz, vp]
+        L.asd_kv_read.argtypes = [vp, vp, vp, i64, vp, i64, vp]
         L.asd_rope_table.argtypes = [ctypes.POINTER(Rope), i32, vp, vp]
         L.asd_kv_view.argtypes = [vp, i32, shape, batch]
         L.asd_set_kv_len.argtypes = [vp, i32]
@@ -539,22 +540,26 @@ class KVCache:
         self.n_heads, self.n_kv_heads, self.head_dim = n_heads, n_kv_heads, head_dim
         self.torch_dtype = torch.bfloat16 if dtype == DT_BF16 else torch.float32
         self._shape = KvShape(n_heads, n_kv_heads, head_dim, page_tokens, dtype, kv_dtype)
-        self._torch, self._lib, self._scale = torch, _kv_lib(), head_dim ** -0.5
-        self._key = (n_heads, n_kv_heads, head_dim, page_tokens, dtype, kv_dtype)
-        self._pool = pages.data_ptr()
+        self._torch, self._lib, self._scale, self._index = torch, _kv_lib(), head_dim ** -0.5, pages.device.index
+        self._key, self._s = (n_heads, n_kv_heads, head_dim, page_tokens, dtype, kv_dtype), ctypes.addressof(self._shape)
+        self._last = (None, None, 0)                    # the batch of the last call, its structure with these pages, and that one's address
 
-    def _batch(self, batch: KVBatch) -> KvBatch:
-        if batch.device != self.device:
-            raise AsdError(E_INVAL, "the batch is on another device than the pages")
-        b = KvBatch.from_buffer_copy(batch._c)          # (calls of several threads may share a batch)
-        b.pages, b.n_pages = self._pool, self.n_pages
-        return b
+    def _batch(self, batch: KVBatch):
+        """(batch, its structure with this cache's pages, the structure's address); it is only read, so calls of several threads may share it."""
+        last = self._last
+        if last[0] is not batch:
+            if batch.device != self.device:
+                raise AsdError(E_INVAL, "the batch is on another device than the pages")
+            b = KvBatch.from_buffer_copy(batch._c)
+            b.pages, b.n_pages = self.pages.data_ptr(), self.n_pages
+            self._last = last = (batch, b, ctypes.addressof(b))
+        return last
 
     def _rows(self, name: str, t, batch: KVBatch, heads: int):
         """(pointer, row stride) of a buffer of rows [>= n_rows, heads, head_dim]; heads packed."""
-        h, shape = self.head_dim, t.shape
-        if t.dtype is not self.torch_dtype or t.device != self.device:
+        if t.dtype is not self.torch_dtype or t.get_device() != self._index:
             raise AsdError(E_INVAL, f"{name} must be {self.torch_dtype} on {self.device}")
+        shape, h = t.shape, self.head_dim
         if len(shape) != 3 or shape[0] < batch.n_rows or shape[1] != heads or shape[2] != h:
             raise AsdError(E_INVAL, f"{name} must be [{batch.n_rows}, {heads}, {h}]")
         row, head, one = t.stride()
@@ -564,16 +569,26 @@ class KVCache:
 
     def _floats(self, name: str, t, *shape):
         """Pointer of a float32 tensor whose last dimensions are `shape`."""
-        if t.dtype is not self._torch.float32 or t.device != self.device or not t.is_contiguous() or t.shape[-len(shape):] != shape:
+        if t.dtype is not self._torch.float32 or t.get_device() != self._index or not t.is_contiguous() or t.shape[-len(shape):] != shape:
             raise AsdError(E_INVAL, f"{name} must be a contiguous float32 tensor [.., {', '.join(map(str, shape))}] on {self.device}")
         return t.data_ptr()
+
+    def _call(self, function, *args):
+        """function(*args, stream) with the cache's device as the current one and its current stream, as the library's launches expect them."""
+        before = self._torch._C._cuda_getDevice()
+        if before == self._index:
+            rc = function(*args, self._torch._C._cuda_getCurrentRawStream(before))
+        else:
+            rc = _on_device(self.device, lambda stream: function(*args, stream))
+        if rc:
+            _kv_ck(rc)
 
     def append(self, batch: KVBatch, q, k, v, q_out=None, rope=None, rot_dim: int = 0, interleaved: bool = False, q_gain=None, k_gain=None,
                eps: float = 1e-5):
         """Write the batch's new rows into the pages (asd_kv_append): q [n_rows, n_heads, head_dim] or None, k and v
         [n_rows, n_kv_heads, head_dim]; rope [positions, rot_dim / 2, 2] as rope_table makes it, gains [head_dim].  Returns the
         prepared queries (q_out, which may be q; a new tensor if it is not given)."""
-        b, prep = self._batch(batch), KvPrep(None, None, eps, None, 0, rot_dim, int(interleaved))
+        bound, prep = self._batch(batch), KvPrep(None, None, eps, None, 0, rot_dim, interleaved)
         if q is None and q_out is not None:
             raise AsdError(E_INVAL, "q_out without q")
         if q is not None and q_out is None:
@@ -587,19 +602,19 @@ class KVCache:
         qp = self._rows("q", q, batch, self.n_heads) if q is not None else (None, 0)
         op = self._rows("q_out", q_out, batch, self.n_heads) if q is not None else (None, 0)
         kp, vp = self._rows("k", k, batch, self.n_kv_heads), self._rows("v", v, batch, self.n_kv_heads)
-        _kv_ck(_on_device(self.device, lambda stream: self._lib.asd_kv_append(self._shape, b, prep, *qp, *kp, *vp, *op, stream)))
+        self._call(self._lib.asd_kv_append, self._s, bound[2], ctypes.addressof(prep), *qp, *kp, *vp, *op)
         return q_out
 
     def attend(self, batch: KVBatch, q, out=None, scale: float | None = None, workspace=None):
         """Causal attention of the batch's new rows over their sequences' pages (asd_kv_attend); q and out [n_rows, n_heads, head_dim],
         scale 1 / sqrt(head_dim) by default.  workspace: a uint8 tensor of attend_workspace(batch) bytes (by default one of the call's own)."""
-        b = self._batch(batch)
+        bound = self._batch(batch)
         if out is None:
             out = self._torch.empty((q.shape[0], self.n_heads, self.head_dim), dtype=self.torch_dtype, device=self.device)
         qp, op = self._rows("q", q, batch, self.n_heads), self._rows("out", out, batch, self.n_heads)
         need = batch._workspace.get(self._key)
         if need is None:
-            need = batch._workspace[self._key] = self._lib.asd_kv_attend_workspace(self._shape, b)
+            need = batch._workspace[self._key] = self._lib.asd_kv_attend_workspace(self._s, bound[2])
         if workspace is None:
             wp, wn = None, 0
             if need:
@@ -611,21 +626,23 @@ class KVCache:
             wp, wn = workspace.data_ptr(), workspace.numel()
         if scale is None:
             scale = self._scale
-        _kv_ck(_on_device(self.device, lambda stream: self._lib.asd_kv_attend(self._shape, b, *qp, *op, scale, wp, wn, stream)))
+        self._call(self._lib.asd_kv_attend, self._s, bound[2], *qp, *op, scale, wp, wn)
         return out
 
     def attend_workspace(self, batch: KVBatch) -> int:
         """Bytes of workspace that attend() of a batch with these bounds needs."""
-        return int(self._lib.asd_kv_attend_workspace(self._shape, self._batch(batch)))
+        return int(self._lib.asd_kv_attend_workspace(self._s, self._batch(batch)[2]))
 
     def read(self, batch: KVBatch, k_out=None, v_out=None):
         """The batch's rows out of the pages as values (asd_kv_read): (k, v) [n_rows, n_kv_heads, head_dim]; new tensors where none is given."""
-        b, out = self._batch(batch), []
-        for name, t in (("k_out", k_out), ("v_out", v_out)):
-            t = self._torch.empty((batch.n_rows, self.n_kv_heads, self.head_dim), dtype=self.torch_dtype, device=self.device) if t is None else t
-            out.append((t, self._rows(name, t, batch, self.n_kv_heads)))
-        _kv_ck(_on_device(self.device, lambda stream: self._lib.asd_kv_read(self._shape, b, *out[0][1], *out[1][1], stream)))
-        return out[0][0], out[1][0]
+        bound = self._batch(batch)
+        if k_out is None:
+            k_out = self._torch.empty((batch.n_rows, self.n_kv_heads, self.head_dim), dtype=self.torch_dtype, device=self.device)
+        if v_out is None:
+            v_out = self._torch.empty_like(k_out, memory_format=self._torch.contiguous_format)
+        kp, vp = self._rows("k_out", k_out, batch, self.n_kv_heads), self._rows("v_out", v_out, batch, self.n_kv_heads)
+        self._call(self._lib.asd_kv_read, self._s, bound[2], *kp, *vp)
+        return k_out, v_out
 
 
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3

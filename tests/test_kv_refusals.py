@@ -20,10 +20,11 @@ def batch(**kw):
 
 def call(name, s, b, **kw):
     L = asd._kv_lib()
+    s, b = (None if x is None else ctypes.addressof(x) for x in (s, b))
     a = dict(q=P, qs=512, k=P, ks=128, v=P, vs=128, out=P, os=512, scale=0.125, ws=P, wb=1 << 40,
              prep=asd.KvPrep(None, None, 1e-5, P, 10, 64, 0)) | kw
     if name == "append":
-        rc = L.asd_kv_append(s, b, a["prep"], a["q"], a["qs"], a["k"], a["ks"], a["v"], a["vs"], a["out"], a["os"], None)
+        rc = L.asd_kv_append(s, b, None if a["prep"] is None else ctypes.addressof(a["prep"]), a["q"], a["qs"], a["k"], a["ks"], a["v"], a["vs"], a["out"], a["os"], None)
     elif name == "attend":
         rc = L.asd_kv_attend(s, b, a["q"], a["qs"], a["out"], a["os"], a["scale"], a["ws"], a["wb"], None)
     else:
@@ -37,7 +38,8 @@ def test_shapes(kw):
     assert asd._kv_lib().asd_kv_page_bytes(ctypes.byref(shape(**kw))) == 0
     for name in ("append", "attend", "read"):
         assert call(name, shape(**kw), batch())[0] == asd.E_INVAL
-    assert asd._kv_lib().asd_kv_attend_workspace(shape(**kw), batch()) == 0
+    s, b = shape(**kw), batch()
+    assert asd._kv_lib().asd_kv_attend_workspace(ctypes.addressof(s), ctypes.addressof(b)) == 0
     assert call("attend", None, batch())[0] == asd.E_INVAL
 
 
@@ -68,7 +70,8 @@ def test_buffers(name, kw):
 
 def test_workspace():
     big = batch(max_len=5000, table_stride=100)
-    need = asd._kv_lib().asd_kv_attend_workspace(shape(), big)
+    s = shape()
+    need = asd._kv_lib().asd_kv_attend_workspace(ctypes.addressof(s), ctypes.addressof(big))
     assert need > 0
     assert call("attend", shape(), big, wb=need - 1)[0] == asd.E_NOMEM
     assert call("attend", shape(), big, ws=None)[0] == asd.E_INVAL
