@@ -570,8 +570,7 @@ template <class C> __device__ __forceinline__ uint32_t kv_kept(int n_keys, int k
 #endif
 // 16 * NT rows against a run of chunks, in units: the keys of one step of V^T pieces (16 fp32, 32 bf16, 64 codes).  Four waves, wave w
 // the units w, w + 4, ... of the run with a running maximum and sum per row, merged through LDS at the end.  Scores S[key][row] = K q^T and the output O[dim][row] = V^T P are matrix-core products with the rows as
-// columns (see asd_attn.h); a unit's fragments go from memory into registers, and the next unit's K is asked for when the
-// scores are done, its V when the output is: memory-bound while the rows are few.
+// columns (see asd_attn.h); a unit's fragments go from memory into registers ahead of their use: memory-bound while the rows are few.
 // 8 bits: K is widened with its scale, V without: V's scales go into the probabilities, one value per key.
 template <class A, class C, int H, int NT>
 __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_kernel(const KvAttendArgs a) {
@@ -618,57 +617,65 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
 #pragma unroll
         for (int ht = 0; ht < HT; ++ht) o[t][ht] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    u32x4 kf[KT][HP], vf[HT][KSU], ke, ve;
-    auto ask_k = [&](const char* p) {
+    struct Unit { u32x4 k[KT][HP], v[HT][KSU], ke, ve; };
+    auto ask_k = [&](Unit& f, const char* p) {
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
             for (int hp = 0; hp < HP; ++hp) {
-                if constexpr (KK * sizeof(typename C::elem) == 16) kf[kt][hp] = __builtin_nontemporal_load((const u32x4*)(p + ((kt * HP + hp) * 64 + lane) * 16));
-                else { const uint64_t x = __builtin_nontemporal_load((const uint64_t*)(p + ((kt * HP + hp) * 64 + lane) * 8)); kf[kt][hp] = u32x4{(uint32_t)x, (uint32_t)(x >> 32), 0u, 0u}; }
+                if constexpr (KK * sizeof(typename C::elem) == 16) f.k[kt][hp] = __builtin_nontemporal_load((const u32x4*)(p + ((kt * HP + hp) * 64 + lane) * 16));
+                else { const uint64_t x = __builtin_nontemporal_load((const uint64_t*)(p + ((kt * HP + hp) * 64 + lane) * 8)); f.k[kt][hp] = u32x4{(uint32_t)x, (uint32_t)(x >> 32), 0u, 0u}; }
             }
-        if constexpr (L::Q8) { ke = *(const u32x4*)(p + 2 * L::K_BYTES + 16 * (m >> 2)); }
+        if constexpr (L::Q8) f.ke = *(const u32x4*)(p + 2 * L::K_BYTES + 16 * (m >> 2));
     };
-    auto ask_v = [&](const char* p) {
+    auto ask_v = [&](Unit& f, const char* p) {
 #pragma unroll
         for (int ht = 0; ht < HT; ++ht)
 #pragma unroll
-            for (int ks = 0; ks < KSU; ++ks) vf[ht][ks] = __builtin_nontemporal_load((const u32x4*)(p + ((ht * KST + ks) * 64 + lane) * 16));
-        if constexpr (L::Q8) ve = *(const u32x4*)(p + L::K_BYTES + 64 + 16 * g);
+            for (int ks = 0; ks < KSU; ++ks) f.v[ht][ks] = __builtin_nontemporal_load((const u32x4*)(p + ((ht * KST + ks) * 64 + lane) * 16));
+        if constexpr (L::Q8) f.ve = *(const u32x4*)(p + L::K_BYTES + 64 + 16 * g);
     };
-    // a unit without a page counts as hidden
-    auto next = [&](int u, const char** k, const char** v) {
+    // The pages of 64 entries of the table lie in the wave's lanes (-1: no page of the pool): a look-up in memory per unit would wait
+    // for every fragment asked for before it
+    const int cpp = a.kv.page_tokens / 64;
+    int page_base = -64, pages = 0;
+    // the first unit from u on that has a page, and where it is; one without counts as hidden
+    const char *at_k = nullptr, *at_v = nullptr;
+    auto next = [&](int u) {
         for (; u < u_end; u += 4) {
-            const char* p = kv_chunk<C, H>(a.kv, seq, u / UPC, kvh);
-            *k = p + u % UPC * KT * HP * 64 * KK * sizeof(typename C::elem);
-            *v = p + L::K_BYTES + u % UPC * KSU * 1024;
-            if (p) break;
+            const int c = u / UPC, i = c / cpp;
+            if (i - page_base >= 64) {
+                page_base = i;
+                pages = i + lane < a.kv.table_stride ? a.kv.table[(size_t)seq * a.kv.table_stride + i + lane] : -1;
+                if ((unsigned)pages >= (unsigned)a.kv.n_pages) pages = -1;
+            }
+            const int page = __builtin_amdgcn_readlane(pages, i - page_base);
+            const char* p = a.kv.pages + (((size_t)max(page, 0) * n_kv + kvh) * cpp + c % cpp) * L::CHUNK;
+            at_k = p + u % UPC * KT * HP * 64 * KK * sizeof(typename C::elem);
+            at_v = p + L::K_BYTES + u % UPC * KSU * 1024;
+            if (page >= 0) break;
             if (lane == 0) kv_flag(a.kv, ASD_KV_BAD_PAGE);
         }
         return u;
     };
     bool odd = false;
-    const char *k = nullptr, *v = nullptr;
-    int unit = next(split * per * UPC + w, &k, &v);
-    if (unit < u_end) { ask_k(k); ask_v(v); }
-    while (unit < u_end) {
-        const int un = next(unit + 4, &k, &v), key0 = unit * UK;
+    auto work = [&](Unit& f, const int key0, auto after_scores) {
         f32x4 sc[NT][KT];
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
             float scale = 1.f;
-            if constexpr (L::Q8) scale = q8_scale((ke[kt] >> (8 * (m & 3))) & 255u);
+            if constexpr (L::Q8) scale = q8_scale((f.ke[kt] >> (8 * (m & 3))) & 255u);
 #pragma unroll
             for (int t = 0; t < NT; ++t) sc[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < QS; ++i) {
-                const u32x4 x = kv_operand<A, C>(kf[kt][i / US], i % US, scale);
+                const u32x4 x = kv_operand<A, C>(f.k[kt][i / US], i % US, scale);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) mma16<A>(sc[t][kt], x, qf[t][i]);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        if (un < u_end) ask_k(k);
+        after_scores();
         __builtin_amdgcn_sched_barrier(0);
         // some rows do not see all of the unit; some of its keys are behind the sequence's end
         const bool edge = key0 + UK - 1 > from;
@@ -678,7 +685,7 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) vs[kt][j] = q8_scale((ve[kt] >> (8 * j)) & 255u);
+                for (int j = 0; j < 4; ++j) vs[kt][j] = q8_scale((f.ve[kt] >> (8 * j)) & 255u);
         u32x4 pf[NT][PS];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -739,7 +746,7 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
                     for (int x = 0; x < 4; ++x) {
                         const uint32_t keep = kv_kept<C>(n_keys, ks, g, x);
 #pragma unroll
-                        for (int ht = 0; ht < HT; ++ht) vf[ht][ks][x] &= keep;
+                        for (int ht = 0; ht < HT; ++ht) f.v[ht][ks][x] &= keep;
                     }
             }
             uint32_t hit = 0;
@@ -748,7 +755,7 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
 #pragma unroll
                 for (int ks = 0; ks < KSU; ++ks)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) hit |= kv_odd<C>(vf[ht][ks][x]);
+                    for (int x = 0; x < 4; ++x) hit |= kv_odd<C>(f.v[ht][ks][x]);
             if (__any(hit != 0)) {
                 odd = true;
 #pragma unroll
@@ -756,21 +763,49 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
 #pragma unroll
                     for (int ks = 0; ks < KSU; ++ks)
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) vf[ht][ks][x] = kv_clean<C>(vf[ht][ks][x]);
+                        for (int x = 0; x < 4; ++x) f.v[ht][ks][x] = kv_clean<C>(f.v[ht][ks][x]);
             }
         }
 #pragma unroll
         for (int ht = 0; ht < HT; ++ht)
 #pragma unroll
             for (int i = 0; i < PS; ++i) {
-                const u32x4 v = kv_operand<A, C>(vf[ht][i / VS], i % VS, 1.f);
+                const u32x4 v = kv_operand<A, C>(f.v[ht][i / VS], i % VS, 1.f);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) mma16<A>(o[t][ht], v, pf[t][i]);
             }
-        __builtin_amdgcn_sched_barrier(0);
-        if (un < u_end) ask_v(v);
-        __builtin_amdgcn_sched_barrier(0);
-        unit = un;
+    };
+    int unit = next(split * per * UPC + w);
+    // One token against bf16 pages: two units in registers, all of the next on its way while one is worked on (one sequence of 8192 tokens,
+    // 32 heads: 29.4 -> 28.6 us).  Codes and fp32 rows take more registers per unit or more time per key: with two units, 48 sequences
+    // of 8-bit pages took 103 us and not 90, a small fp32 batch 10.6 and not 9.5
+    if constexpr (NT == 1 && sizeof(typename C::elem) == 2) {
+        Unit f0, f1;
+        auto ask = [&](Unit& f) { ask_k(f, at_k); ask_v(f, at_v); };
+        auto turn = [&](Unit& now, Unit& then) {
+            const int un = next(unit + 4);
+            if (un < u_end) ask(then);
+            __builtin_amdgcn_sched_barrier(0);
+            work(now, unit * UK, [] {});
+            unit = un;
+        };
+        if (unit < u_end) ask(f0);
+        while (unit < u_end) {
+            turn(f0, f1);
+            if (unit >= u_end) break;
+            turn(f1, f0);
+        }
+    } else {                                            // one: the next K behind the scores, the next V behind the output
+        Unit f;
+        if (unit < u_end) { ask_k(f, at_k); ask_v(f, at_v); }
+        while (unit < u_end) {
+            const int un = next(unit + 4);
+            work(f, unit * UK, [&] { if (un < u_end) ask_k(f, at_k); });
+            __builtin_amdgcn_sched_barrier(0);
+            if (un < u_end) ask_v(f, at_v);
+            __builtin_amdgcn_sched_barrier(0);
+            unit = un;
+        }
     }
 
     // ---- the waves' results, 16 rows at a time, wave order
