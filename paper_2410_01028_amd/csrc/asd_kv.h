@@ -563,17 +563,15 @@ template <class C> __device__ __forceinline__ uint32_t kv_kept(int n_keys, int k
     return left >= PER ? 0xffffffffu : left <= 0 ? 0u : (1u << (left * EB & 31)) - 1u;
 }
 
-// Units of a chunk, so that a wave's share is small where the work of a key is large (fp32 products) and one step of V^T pieces needs no more
-#define KV_UNITS(C) (sizeof(typename C::elem) == 4 ? 4 : sizeof(typename C::elem) == 2 ? KV_BF16_UNITS : 1)
-#ifndef KV_BF16_UNITS
-#define KV_BF16_UNITS 2
-#endif
+// Units of a chunk: one step of V^T pieces each, so that a wave's share is small where the work of a key is large (fp32 products) and a
+// unit takes no more registers than it must (bf16: one sequence of 8192 tokens 32.8 us with whole chunks, 29.4 with halves)
+#define KV_UNITS(C) (16 / C::KE)
 // 16 * NT rows against a run of chunks, in units: the keys of one step of V^T pieces (16 fp32, 32 bf16, 64 codes).  Four waves, wave w
 // the units w, w + 4, ... of the run with a running maximum and sum per row, merged through LDS at the end.  Scores S[key][row] = K q^T and the output O[dim][row] = V^T P are matrix-core products with the rows as
 // columns (see asd_attn.h); a unit's fragments go from memory into registers ahead of their use: memory-bound while the rows are few.
 // 8 bits: K is widened with its scale, V without: V's scales go into the probabilities, one value per key.
 template <class A, class C, int H, int NT>
-__global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_kernel(const KvAttendArgs a) {
+__global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(const KvAttendArgs a) {
     using L = KvLayout<C, H>;
     using E = typename A::elem;
     constexpr int AE = A::KE, KK = L::KK, HP = L::HP, US = KK / AE, QS = HP * US;      // operand steps of a K piece, of a row
@@ -856,7 +854,7 @@ __global__ __launch_bounds__(256, A::KE == 4 || NT == 4 ? 1 : 2) void kv_attend_
 // direct loads into a ring of five half-chunks (K, V^T, K, ..): one barrier per chunk c, behind which K and V^T of c have landed
 // and the slots of c - 1 may be asked for anew (V^T of c + 1, K of c + 2).  A SIMD has several waves, one's products beside the other's exponentials.
 template <class C, int H, int NT, int NW>
-__global__ __launch_bounds__(64 * NW, ROWS_EU) void kv_rows_kernel(const KvAttendArgs a) {
+__global__ __launch_bounds__(64 * NW, 2) void kv_rows_kernel(const KvAttendArgs a) {
     using A = BF16;
     using L = KvLayout<C, H>;
     constexpr int AE = A::KE, KK = L::KK, HP = L::HP, US = KK / AE, QS = HP * US, HT = L::HT, KST = L::KST, VS = L::KV / AE, PS = KST * VS;

@@ -1,10 +1,5 @@
 // Host side of the operators over a paged cache of several sequences: argument checks, launch rules, the C ABI of asd.h.
 #include "../../include/asd.h"
-#ifndef ROWS_NT
-#define ROWS_NT 2
-#define ROWS_NW 4
-#define ROWS_EU 2
-#endif
 #include "asd_kv.h"
 
 #include <cmath>
@@ -92,12 +87,6 @@ int units() {
     return n;
 }
 
-#ifdef KV_DEV
-#include <cstdlib>
-#define DEV_TUNE if (getenv("KV_TL")) p.target = atoi(getenv("KV_TL")); if (getenv("KV_MR")) p.min_run = atoi(getenv("KV_MR"));
-#else
-#define DEV_TUNE
-#endif
 // How asd_kv_attend runs a batch of these bounds
 struct AttendPlan {
     int nt;                        // 16-row column blocks of a tile
@@ -111,20 +100,30 @@ AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b) {
     AttendPlan p{};
     const int group = s->n_heads / s->n_kv_heads;
     const int64_t rows = (int64_t)b->max_new * group, chunks = (kv_args(s, b).cap + 63) / 64;
-    // Rows share a chunk's fragments: as many columns as the largest sequence fills, up to 64 (fp32: 32, whose operands take twice the registers)
-    p.nt = rows <= 16 ? 1 : s->dtype == ASD_DT_F32 ? 2 : rows <= 32 ? 2 : 4;
-    if (s->dtype == ASD_DT_F32 && (int64_t)b->n_rows * s->n_heads / 32 < 2 * units()) p.nt = 1;
-    p.rows = s->dtype == ASD_DT_BF16 && s->head_dim >= 64 && rows > 64;
+    const bool bf16 = s->dtype == ASD_DT_BF16, q8 = s->kv_dtype == ASD_DT_FP8;
+    const int64_t seqs = b->n_seqs < b->n_rows ? b->n_seqs : b->n_rows;
+    auto tiles = [&](int nt) { return (int64_t)b->n_rows * group / (16 * nt) + seqs; };      // the most that there can be
+    // Which kernel.  kv_attend_kernel's workgroups are many and short, its tiles read a sequence's pages again for every 16 rows (mostly from L2);
+    // kv_rows_kernel reads them once for 128 rows, with a step's cost whether they are all in use or not.  Up to 32 rows the first one, whatever
+    // the lengths (64 sequences of 32 rows, 4000 tokens, 8 bits: 130 us against 172).  Above, the second one where the first has more than
+    // two rounds of workgroups (16 x 32 heads, 40 rows, 128 tokens: 13 us against 23) or more than 64 chunks per compute unit (2 x 32 heads, 100 rows, 4000 tokens:
+    // 42 against 59; with 1000 tokens 34 against 17).
+    const int64_t work = tiles(1) * s->n_kv_heads;
+    p.rows = bf16 && s->head_dim >= 64 && rows > 32 && (work > 4 * (int64_t)units() || work * chunks > 64 * (int64_t)units());
+    // 16 rows to a tile; 32 where a fragment's second use is worth more than twice the workgroups: bf16 pages of some length (64 sequences of 24 rows, 4000 tokens:
+    // 182 us against 256; 8 bits 141 against 128), and codes widened for fp32 products in a batch that fills the card (4 x 500 rows: 337 against 409)
+    p.nt = rows <= 16 ? 1 : bf16 ? (!q8 && chunks >= 8 ? 2 : 1) : (q8 && (int64_t)b->n_rows * s->n_heads / 32 >= 2 * units() ? 2 : 1);
     if (p.rows) p.nt = 8;
+    p.max_tiles = (int32_t)tiles(p.nt);
+    // Keys are cut into about four items per compute unit (48 sequences of 500 to 8192 tokens: 90 us, with two 100, with eight 97), but not
+    // into runs of fewer than 16 chunks (with 8, five rows of eight sequences of 1031 tokens take 19.1 us, not 16.9), and not where the
+    // tiles of kv_rows_kernel are as many by themselves
     p.min_run = 16;
     p.target = 4 * units();
-    p.max_tiles = (int32_t)((int64_t)b->n_rows * group / (16 * p.nt) + (b->n_seqs < b->n_rows ? b->n_seqs : b->n_rows));
-    const int64_t whole = (int64_t)p.max_tiles * s->n_kv_heads;
-    // No cut where the tiles alone are work enough for every compute unit, or the keys are too few
-    DEV_TUNE
-    p.join = (chunks + p.min_run / 2) / p.min_run > 1 && !(p.rows && whole >= p.target);
+    const int64_t whole = (int64_t)p.max_tiles * s->n_kv_heads, most = (chunks + p.min_run / 2) / p.min_run;      // runs of the longest sequence
+    p.join = most > 1 && !(p.rows && whole >= p.target);
     p.grid = p.join ? whole + p.target : whole;
-    if (p.join && whole * ((chunks + p.min_run / 2) / p.min_run) < p.grid) p.grid = whole * ((chunks + p.min_run / 2) / p.min_run);
+    if (p.join && whole * most < p.grid) p.grid = whole * most;
     if (p.join) {
         p.o_bytes = ((size_t)p.grid * 16 * p.nt * s->head_dim * 4 + 255) / 256 * 256;
         p.bytes = p.o_bytes + (size_t)p.grid * 16 * p.nt * 8;
@@ -219,14 +218,17 @@ int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, i
         if (p.join) kv_join_kernel<decltype(t), h.value, nt.value><<<join_grid, 256, 0, stream>>>(a);
     };
     by_shape(s, [&](auto t, auto c, auto h) {
-        if (p.rows) {
-            if constexpr (sizeof(typename decltype(t)::elem) == 2 && h.value >= 64) {
-                kv_rows_kernel<decltype(c), h.value, (sizeof(typename decltype(c)::elem) * h.value < 128 ? 2 : ROWS_NT), (sizeof(typename decltype(c)::elem) * h.value < 128 ? 4 : ROWS_NW)><<<(unsigned)p.grid, sizeof(typename decltype(c)::elem) * h.value < 128 ? 256 : 64 * ROWS_NW, 0, stream>>>(a);
-                if (p.join) kv_join_kernel<decltype(t), h.value, 8><<<join_grid, 256, 0, stream>>>(a);
+        using T = decltype(t);
+        using C = decltype(c);
+        constexpr bool bf16 = T::KE == 8, q8 = sizeof(typename C::elem) == 1;
+        if (p.nt == 1) go(t, c, h, std::integral_constant<int, 1>{});
+        if constexpr (bf16 != q8) { if (p.nt == 2) go(t, c, h, std::integral_constant<int, 2>{}); }
+        if constexpr (bf16 && h.value >= 64) {
+            if (p.nt == 8) {
+                kv_rows_kernel<C, h.value, 2, 4><<<(unsigned)p.grid, 256, 0, stream>>>(a);
+                if (p.join) kv_join_kernel<T, h.value, 8><<<join_grid, 256, 0, stream>>>(a);
             }
-        } else if (p.nt == 1) go(t, c, h, std::integral_constant<int, 1>{});
-        else if (p.nt == 2) go(t, c, h, std::integral_constant<int, 2>{});
-        else if constexpr (sizeof(typename decltype(t)::elem) == 2) go(t, c, h, std::integral_constant<int, 4>{});
+        }
     });
     return launched("asd_kv_attend");
 }

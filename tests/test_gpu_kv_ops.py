@@ -198,13 +198,13 @@ def test_attend(dtype, kv, lens, h, heads, kv_heads, page):
 
 
 @pytest.mark.parametrize("dtype,kv", COMBOS)
-@pytest.mark.parametrize("news", [(40, 6, 90), (5, 3, 4), (1, 6, 1)], ids=["many rows", "drafts", "tokens"])
+@pytest.mark.parametrize("news,kv_heads", [((40, 6, 90), 64), ((40, 6, 90), 2), ((5, 3, 4), 2), ((1, 6, 1), 2)], ids=["many rows", "chunks", "drafts", "tokens"])
 @pytest.mark.parametrize("h", [64, 128])
-def test_values_that_are_not_finite_stay_where_they_are_seen(dtype, kv, news, h):
+def test_values_that_are_not_finite_stay_where_they_are_seen(dtype, kv, news, kv_heads, h):
     """Infinities and NaN in V and NaN in K at keys that some rows of the call do not see, and in chunks that all rows see."""
     total = [100, 6, 130]
-    p = Pool(dtype, kv, 4, 2, h, 64, list(zip(news, total)), seed=1)
-    k, v = p.normal(sum(total), 2, h), p.normal(sum(total), 2, h)
+    p = Pool(dtype, kv, 2 * kv_heads, kv_heads, h, 64, list(zip(news, total)), seed=1)
+    k, v = p.normal(sum(total), kv_heads, h), p.normal(sum(total), kv_heads, h)
     v[70, 0, 3], v[95, 0, 7], v[95, 1, 9], v[97, 0, 7], v[103, 1, 60], v[220, 0, 33] = math.inf, math.inf, math.nan, -math.inf, -math.inf, math.nan
     v[110, 1, 2], v[233, 1, 5] = math.inf, -math.inf
     k[104, 0, 5] = math.nan
@@ -212,7 +212,7 @@ def test_values_that_are_not_finite_stay_where_they_are_seen(dtype, kv, news, h)
     p.cache.append(whole, None, k, v)
     k, v = (torch.split(x, total) for x in p.cache.read(whole))
     b = p.batch(news, total)
-    q = p.normal(sum(news), 4, h)
+    q = p.normal(sum(news), 2 * kv_heads, h)
     out = p.cache.attend(b, q)
     b.check()
     one, two = news[0], news[0] + news[1]
@@ -222,9 +222,46 @@ def test_values_that_are_not_finite_stay_where_they_are_seen(dtype, kv, news, h)
 
 
 @pytest.mark.parametrize("kv", ["fp8", "bf16"])
+@pytest.mark.parametrize("h,heads,kv_heads,page", [(128, 40, 40, 64), (128, 64, 8, 192), (64, 64, 8, 64), (64, 40, 40, 128)])
+def test_attend_many_rows(kv, h, heads, kv_heads, page):
+    """Batches whose tiles fill the card: 128 rows share a chunk (prompts, chunks behind a context, a single token and nothing among them)."""
+    news, total = [64, 70, 1, 130, 0, 200, 17, 2], [64, 333, 20, 1200, 9, 200, 17, 2]
+    p = Pool("bf16", kv, heads, kv_heads, h, page, list(zip(news, total)), seed=h)
+    k, v = p.fill()
+    q = p.normal(sum(news) + 3, heads + 2, h, scale=2.0)[:, 1:heads + 1]
+    out = torch.full((sum(news) + 3, heads, h), 7.0, dtype=p.t, device=DEV)
+    b = p.batch(news, total, extra=3)
+    p.cache.attend(b, q, out=out)
+    b.check()
+    assert bool((out[sum(news):] == 7.0).all())
+    check_attend(p, news, total, q, out, k, v, h ** -0.5)
+    p.d_table[3, 1] = -1                                 # a page that is not there, in the middle of the fourth sequence
+    p.cache.attend(b, q, out=out)
+    with pytest.raises(asd.AsdError, match="pages"):
+        b.check()
+    keep = torch.cat([torch.arange(page), torch.arange(2 * page, 1200)]).to(DEV)
+    at = 64 + 70 + 1
+    want, size, big = attention(q[at:at + 130], k[3][keep], v[3][keep], 1200 - page - 130, h ** -0.5)
+    e = 2 * h * 2.0 ** -24 * big[..., None] + 2.0 ** -20 + 1200 * 2.0 ** -24 + 2.0 ** -8
+    close(out[at:at + 130], want, size * e + (want.abs() + size * e) * 2.0 ** -8, "hidden page")
+
+
+def test_attend_many_rows_over_many_pages():
+    """Runs of more pages than a wave holds at a time."""
+    news, total = [1024, 1000], [4400, 4300]
+    p = Pool("bf16", "fp8", 64, 64, 64, 64, list(zip(news, total)), seed=8)
+    k, v = p.fill()
+    q = p.normal(2024, 64, 64)
+    b = p.batch(news, total)
+    out = p.cache.attend(b, q)
+    b.check()
+    check_attend(p, news, total, q, out, k, v, 0.125)
+
+
+@pytest.mark.parametrize("kv", ["fp8", "bf16"])
 def test_long_and_lopsided_batches(kv):
-    """One long sequence among short ones: its keys are cut into runs and joined, for a token, a few rows and a chunk of many."""
-    for news, total in (((1, 1, 1, 1), (20000, 40, 1, 700)), ((6, 0, 2, 6), (9000, 40, 2, 7000)), ((150, 1, 90, 3), (6000, 40, 90, 2100))):
+    """One long sequence among short ones: its keys are cut into runs and joined, for a token, a few rows and chunks of many."""
+    for news, total in (((1, 1, 1, 1), (20000, 40, 1, 700)), ((6, 0, 2, 6), (9000, 40, 2, 7000)), ((150, 1, 90, 3), (6000, 40, 90, 2100)), ((300, 1, 90, 3), (9000, 40, 90, 2100))):
         p = Pool("bf16", kv, 8, 2, 128, 256, list(zip(news, total)), seed=3)
         k, v = p.fill()
         b = p.batch(news, total)
