@@ -252,7 +252,8 @@ template <class T, int H, bool INTER> struct HeadVec {
 // once, 16 bytes a lane, four heads of a token in flight (their angles are read once); what the vector unit does per value is kept short, and
 // values that are not finite are looked for by one comparison of the largest magnitude.  The cache's elements go through LDS, K row by
 // row and V to be transposed, so that they leave in the layout's own 16-byte pieces, whole lines for whole chunks.  A V^T piece some of whose
-// keys are not new is written element by element, so that what the cache holds beside the new rows stays.
+// keys are not new is written element by element, so that what the cache holds beside the new rows stays.  Prompts of 6901 tokens, 32 + 32 heads
+// x 128, into 8-bit pages: 67 us, 283 MB, 4.2 TB/s; one token of 48 sequences, 64 + 8 heads: 7.0 us, a chain of look-ups (lengths, table, rows).
 // (Neighbours turn in a kernel of their own: an array whose elements two branches pair differently stays in memory.)
 template <class T, class C, int H, int TOK, bool INTER>
 __global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
@@ -420,7 +421,8 @@ struct KvReadArgs {
     int64_t k_stride, v_stride;
 };
 // A workgroup takes one chunk of one sequence and KV head, its K or its V: the pieces that hold wanted rows come in as they
-// lie, go through LDS as rows, and leave as rows.
+// lie, go through LDS as rows, and leave as rows.  Bound by memory: 16 sequences of up to 4096 tokens, 8 heads x 128 in 8 bits, 254 MB,
+// 58 us (4.4 TB/s; a large copy reaches 5.0); a few tokens 4.1 us, a chain of look-ups.
 template <class T, class C, int H>
 __global__ __launch_bounds__(256) void kv_read_kernel(const KvReadArgs a) {
     using L = KvLayout<C, H>;
@@ -570,6 +572,8 @@ template <class C> __device__ __forceinline__ uint32_t kv_kept(int n_keys, int k
 // the units w, w + 4, ... of the run with a running maximum and sum per row, merged through LDS at the end.  Scores S[key][row] = K q^T and the output O[dim][row] = V^T P are matrix-core products with the rows as
 // columns (see asd_attn.h); a unit's fragments go from memory into registers ahead of their use: memory-bound while the rows are few.
 // 8 bits: K is widened with its scale, V without: V's scales go into the probabilities, one value per key.
+// One token of 48 sequences of 500 to 8192 tokens, 64 / 8 heads x 128, 8 bits: 85 us, with the join 5.5 TB/s.  A batch too small for memory to
+// bound it waits for its loads, 1.7 us for each unit of a wave: five rows of eight sequences of up to 1031 tokens, 40 heads, 16 us.
 template <class A, class C, int H, int NT>
 __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(const KvAttendArgs a) {
     using L = KvLayout<C, H>;
@@ -852,7 +856,11 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(cons
 
 // Many rows (bf16): NW waves with 16 * NT rows each walk a run of chunks together, their fragments in LDS once for all of them.  They come by
 // direct loads into a ring of five half-chunks (K, V^T, K, ..): one barrier per chunk c, behind which K and V^T of c have landed
-// and the slots of c - 1 may be asked for anew (V^T of c + 1, K of c + 2).  A SIMD has several waves, one's products beside the other's exponentials.
+// and the slots of c - 1 may be asked for anew (V^T of c + 1, K of c + 2).  A SIMD has two waves, one's products beside the other's exponentials.
+// (Prompts of 1035 to 2048 tokens, 32 heads x 128, bf16 pages, took 160 us so at the step when four waves of 16 rows took 199 and two waves with the
+// next product's fragments in registers 200, both spilling.)  Bound by the vector unit, exponentials and in 8 bits the widening, which each wave
+// does for itself: it issues in 53 % of the busy cycles (8 bits 73), the matrix cores are at work in 38.  These prompts now take 144 us (716 TFLOP/s),
+// one of 8192 tokens 1001 TFLOP/s (8-bit pages 944); 512 rows behind 8195 tokens and 260 behind 2665 in 8 bits, 64 / 8 heads, 214 us with the join.
 template <class C, int H, int NT, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void kv_rows_kernel(const KvAttendArgs a) {
     using A = BF16;
@@ -1150,7 +1158,9 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_rows_kernel(const KvAttendArgs 
 }
 
 // Joins the runs of tiles whose keys were cut: a workgroup per tile, KV head and 16 of its rows.  16 lanes hold a row's dims;
-// where fewer rows are in use than 16, the lanes left over take every second (fourth, ..) run, added up through LDS at the end.
+// where fewer rows are in use than 16, the lanes left over take every second (fourth, ..) run, added up through LDS at the end.  A launch of its own,
+// 4 to 5 us for one token's runs, 13 us for those of 772 rows: joined by the last workgroup to arrive, counters would have to be zero when the
+// call starts, and the workspace could not be any memory.
 template <class A, int H, int NT>
 __global__ __launch_bounds__(256) void kv_join_kernel(const KvAttendArgs a) {
     using E = typename A::elem;

@@ -164,7 +164,7 @@ int asd_kv_append(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_pre
     a.q_gain = p->q_gain; a.k_gain = p->k_gain; a.rope = p->rope; a.eps = p->eps;
     a.rope_positions = p->rope_positions; a.rot = p->rot_dim;
     // Tiles of 64 tokens, whole chunks, where there are enough of them to fill the card (6900 tokens of 32 + 32 heads, with the rows read back:
-    // 107 us, tiles of 16 120 us); else tiles of 16, four times the workgroups
+    // 107 us, with tiles of 16 120 us); else tiles of 16, four times the workgroups
     const int64_t seqs = b->n_seqs < b->n_rows ? b->n_seqs : b->n_rows;
     const int tok = (int64_t)b->n_rows * s->n_kv_heads / 64 >= 2 * (int64_t)units() ? 64 : 16;
     const int most = b->max_new < tok ? b->max_new : tok;           // tokens of a tile
