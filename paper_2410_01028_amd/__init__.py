@@ -568,9 +568,13 @@ class KVCache:
         return t.data_ptr(), row if batch.n_rows > 1 else max(row, heads * h)
 
     def _floats(self, name: str, t, *shape):
-        """Pointer of a float32 tensor whose last dimensions are `shape`."""
-        if t.dtype is not self._torch.float32 or t.get_device() != self._index or not t.is_contiguous() or t.shape[-len(shape):] != shape:
-            raise AsdError(E_INVAL, f"{name} must be a contiguous float32 tensor [.., {', '.join(map(str, shape))}] on {self.device}")
+        """Pointer of a float32 tensor of `shape` (None first: any number)."""
+        if shape[0] is None:
+            fits = t.dim() == len(shape) and t.shape[1:] == shape[1:]
+        else:
+            fits = t.shape == shape
+        if not fits or t.dtype is not self._torch.float32 or t.get_device() != self._index or not t.is_contiguous():
+            raise AsdError(E_INVAL, f"{name} must be a contiguous float32 tensor [{', '.join('any' if n is None else str(n) for n in shape)}] on {self.device}")
         return t.data_ptr()
 
     def _call(self, function, *args):
@@ -594,7 +598,7 @@ class KVCache:
         if q is not None and q_out is None:
             q_out = self._torch.empty((q.shape[0], self.n_heads, self.head_dim), dtype=self.torch_dtype, device=self.device)
         if rope is not None:
-            prep.rope, prep.rope_positions = self._floats("rope", rope, rot_dim // 2, 2), rope.shape[0]
+            prep.rope, prep.rope_positions = self._floats("rope", rope, None, rot_dim // 2, 2), rope.shape[0]
         if q_gain is not None:
             prep.q_gain = self._floats("q_gain", q_gain, self.head_dim)
         if k_gain is not None:

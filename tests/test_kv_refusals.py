@@ -93,3 +93,17 @@ def test_engine_calls_without_an_engine():
     L = asd._kv_lib()
     assert L.asd_kv_view(None, 0, asd.KvShape(), asd.KvBatch()) == asd.E_INVAL
     assert L.asd_set_kv_len(None, 0) == asd.E_INVAL
+
+
+def test_a_table_is_told_from_one_of_its_rows():
+    """A rotary table has three dimensions: with one row of it, the kernels would take its pairs for positions."""
+    import torch
+    cache = asd.KVCache.__new__(asd.KVCache)
+    cache.__dict__.update(_torch=torch, _index=-1, device=torch.device("cpu"))       # (-1: a CPU tensor's device)
+    table = torch.zeros(10, 32, 2)
+    assert cache._floats("rope", table, None, 32, 2) == table.data_ptr()
+    for bad in (table[3], table[None], table.double(), table[:, :16], table[:, ::2]):
+        with pytest.raises(asd.AsdError):
+            cache._floats("rope", bad, None, 32, 2)
+    with pytest.raises(asd.AsdError):
+        cache._floats("q_gain", torch.zeros(2, 64), 64)
