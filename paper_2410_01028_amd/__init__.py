@@ -494,7 +494,16 @@ def _on_device(device, call):
         torch.cuda.set_device(before)
 
 
-class KVBatch:
+class _Fixed:
+    """Attributes are set once: calls pass addresses and bounds that were taken when the object was made."""
+
+    def __setattr__(self, name, value):
+        if name in self.__dict__:
+            raise AttributeError(f"{name} does not change: make a new {type(self).__name__}")
+        self.__dict__[name] = value
+
+
+class KVBatch(_Fixed):
     """New rows of several sequences (asd_kv_batch): int32 device tensors page_table [n_seqs, pages], row_start [n_seqs + 1],
     kv_len [n_seqs] (tokens with the new ones), and the bounds that hold for them: rows of the row buffers, most new rows
     and most tokens of a sequence.  The tensors are read when a call's kernels run: update them in place between calls.
@@ -526,7 +535,7 @@ class KVBatch:
             raise AsdError(E_INVAL, "batch out of range: " + ", ".join(names))
 
 
-class KVCache:
+class KVCache(_Fixed):
     """Pages of a paged cache for several sequences: pages is a uint8 device tensor of n_pages * kv_page_bytes(...) bytes, which the
     caller owns.  The calls enqueue on the current stream of its device and return without synchronising; asd.h has
     the layout and what each call does."""
@@ -542,18 +551,14 @@ class KVCache:
         self._shape = KvShape(n_heads, n_kv_heads, head_dim, page_tokens, dtype, kv_dtype)
         self._torch, self._lib, self._scale, self._index = torch, _kv_lib(), head_dim ** -0.5, pages.device.index
         self._key, self._s = (n_heads, n_kv_heads, head_dim, page_tokens, dtype, kv_dtype), ctypes.addressof(self._shape)
-        self._last = (None, None, 0)                    # the batch of the last call, its structure with these pages, and that one's address
 
     def _batch(self, batch: KVBatch):
-        """(batch, its structure with this cache's pages, the structure's address); it is only read, so calls of several threads may share it."""
-        last = self._last
-        if last[0] is not batch:
-            if batch.device != self.device:
-                raise AsdError(E_INVAL, "the batch is on another device than the pages")
-            b = KvBatch.from_buffer_copy(batch._c)
-            b.pages, b.n_pages = self.pages.data_ptr(), self.n_pages
-            self._last = last = (batch, b, ctypes.addressof(b))
-        return last
+        """The batch's structure with this cache's pages (each call has its own: calls of several threads may share a batch)."""
+        if batch.device != self.device:
+            raise AsdError(E_INVAL, "the batch is on another device than the pages")
+        b = KvBatch.from_buffer_copy(batch._c)
+        b.pages, b.n_pages = self.pages.data_ptr(), self.n_pages
+        return b
 
     def _rows(self, name: str, t, batch: KVBatch, heads: int):
         """(pointer, row stride) of a buffer of rows [>= n_rows, heads, head_dim]; heads packed."""
@@ -606,7 +611,7 @@ class KVCache:
         qp = self._rows("q", q, batch, self.n_heads) if q is not None else (None, 0)
         op = self._rows("q_out", q_out, batch, self.n_heads) if q is not None else (None, 0)
         kp, vp = self._rows("k", k, batch, self.n_kv_heads), self._rows("v", v, batch, self.n_kv_heads)
-        self._call(self._lib.asd_kv_append, self._s, bound[2], ctypes.addressof(prep), *qp, *kp, *vp, *op)
+        self._call(self._lib.asd_kv_append, self._s, ctypes.addressof(bound), ctypes.addressof(prep), *qp, *kp, *vp, *op)
         return q_out
 
     def attend(self, batch: KVBatch, q, out=None, scale: float | None = None, workspace=None):
@@ -618,7 +623,7 @@ class KVCache:
         qp, op = self._rows("q", q, batch, self.n_heads), self._rows("out", out, batch, self.n_heads)
         need = batch._workspace.get(self._key)
         if need is None:
-            need = batch._workspace[self._key] = self._lib.asd_kv_attend_workspace(self._s, bound[2])
+            need = batch._workspace[self._key] = self._lib.asd_kv_attend_workspace(self._s, ctypes.addressof(bound))
         if workspace is None:
             wp, wn = None, 0
             if need:
@@ -630,12 +635,13 @@ class KVCache:
             wp, wn = workspace.data_ptr(), workspace.numel()
         if scale is None:
             scale = self._scale
-        self._call(self._lib.asd_kv_attend, self._s, bound[2], *qp, *op, scale, wp, wn)
+        self._call(self._lib.asd_kv_attend, self._s, ctypes.addressof(bound), *qp, *op, scale, wp, wn)
         return out
 
     def attend_workspace(self, batch: KVBatch) -> int:
         """Bytes of workspace that attend() of a batch with these bounds needs."""
-        return int(self._lib.asd_kv_attend_workspace(self._s, self._batch(batch)[2]))
+        bound = self._batch(batch)
+        return int(self._lib.asd_kv_attend_workspace(self._s, ctypes.addressof(bound)))
 
     def read(self, batch: KVBatch, k_out=None, v_out=None):
         """The batch's rows out of the pages as values (asd_kv_read): (k, v) [n_rows, n_kv_heads, head_dim]; new tensors where none is given."""
@@ -645,7 +651,7 @@ class KVCache:
         if v_out is None:
             v_out = self._torch.empty_like(k_out, memory_format=self._torch.contiguous_format)
         kp, vp = self._rows("k_out", k_out, batch, self.n_kv_heads), self._rows("v_out", v_out, batch, self.n_kv_heads)
-        self._call(self._lib.asd_kv_read, self._s, bound[2], *kp, *vp)
+        self._call(self._lib.asd_kv_read, self._s, ctypes.addressof(bound), *kp, *vp)
         return k_out, v_out
 
 

@@ -107,3 +107,15 @@ def test_a_table_is_told_from_one_of_its_rows():
             cache._floats("rope", bad, None, 32, 2)
     with pytest.raises(asd.AsdError):
         cache._floats("q_gain", torch.zeros(2, 64), 64)
+
+
+@pytest.mark.parametrize("kind,names", [(asd.KVBatch, ("page_table", "row_start", "kv_len", "status", "n_rows", "max_new", "max_len")),
+                                        (asd.KVCache, ("pages", "n_pages", "n_heads", "n_kv_heads", "head_dim", "torch_dtype"))])
+def test_what_calls_rely_on_does_not_change(kind, names):
+    """Calls pass addresses and bounds that were taken when the object was made: another tensor or bound in its place is refused."""
+    x = kind.__new__(kind)
+    for name in names:
+        setattr(x, name, 1)
+        with pytest.raises(AttributeError):
+            setattr(x, name, 2)
+        assert getattr(x, name) == 1
