@@ -423,7 +423,8 @@ typedef struct {
 } asd_kv_shape;
 
 /* A batch: pages (16-byte aligned), the arrays described above, and bounds that hold for them: rows of the row buffers,
- * most new rows of a sequence (1 .. n_rows), most tokens of a sequence (1 .. 2^24).  n_seqs 1 .. 65536. */
+ * most new rows of a sequence (1 .. n_rows), most tokens of a sequence (1 .. 2^24).  n_seqs 1 .. 65536.
+ * A batch whose launch would have 2^32 threads or more is refused. */
 typedef struct {
     void* pages;
     const int32_t* page_table;      /* [n_seqs][table_stride] */

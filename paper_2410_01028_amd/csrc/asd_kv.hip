@@ -87,6 +87,9 @@ int units() {
     return n;
 }
 
+// Workgroups of 256 that a launch can have: its threads are counted in 32 bits
+constexpr int64_t MOST_GROUPS = ((int64_t)1 << 32) / 256 - 1;
+
 // How asd_kv_attend runs a batch of these bounds
 struct AttendPlan {
     int nt;                        // 16-row column blocks of a tile
@@ -178,7 +181,7 @@ int asd_kv_append(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_pre
     const int64_t loose = b->n_rows / tok + 2 * seqs;
     a.blocks = 2 * a.kv_blocks + q_blocks;
     const int64_t grid = (loose < b->n_rows ? loose : b->n_rows) * a.blocks;
-    if (grid >= (int64_t)1 << 31) return refuse(ASD_E_INVAL, "asd_kv_append: the batch is too large");
+    if (grid > MOST_GROUPS) return refuse(ASD_E_INVAL, "asd_kv_append: the batch is too large");
     by_shape(s, [&](auto t, auto c, auto h) {
         auto go = [&](auto tiles, auto inter) { kv_append_kernel<decltype(t), decltype(c), h.value, tiles.value, inter.value><<<(unsigned)grid, 256, 0, (hipStream_t)hip_stream>>>(a); };
         auto turned = [&](auto tiles) { if (p->interleaved && p->rot_dim) go(tiles, std::true_type{}); else go(tiles, std::false_type{}); };
@@ -204,7 +207,7 @@ int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, i
     const AttendPlan p = attend_plan(s, b);
     if (p.bytes && (!workspace || (uintptr_t)workspace % 256)) return refuse(ASD_E_INVAL, "asd_kv_attend: workspace must be 256-byte aligned");
     if (workspace_bytes < p.bytes) return refuse(ASD_E_NOMEM, "asd_kv_attend: workspace too small: %zu bytes given, %zu needed", workspace_bytes, p.bytes);
-    if (p.grid >= (int64_t)1 << 31) return refuse(ASD_E_INVAL, "asd_kv_attend: the batch is too large");
+    if (p.grid > MOST_GROUPS) return refuse(ASD_E_INVAL, "asd_kv_attend: the batch is too large");
     KvAttendArgs a{};
     a.kv = kv_args(s, b);
     a.q = q; a.out = out; a.q_stride = q_stride; a.out_stride = out_stride;
@@ -244,7 +247,9 @@ int asd_kv_read(const asd_kv_shape* s, const asd_kv_batch* b, void* k_out, int64
     a.kv = kv_args(s, b);
     a.k_out = k_out; a.v_out = v_out; a.k_stride = k_stride; a.v_stride = v_stride;
     const int64_t seqs = b->n_seqs < b->n_rows ? b->n_seqs : b->n_rows, loose = b->n_rows / 64 + 2 * seqs;
-    const dim3 grid((unsigned)(loose < b->n_rows ? loose : b->n_rows), s->n_kv_heads, 2);
+    const int64_t most = loose < b->n_rows ? loose : b->n_rows;
+    if (most > MOST_GROUPS) return refuse(ASD_E_INVAL, "asd_kv_read: the batch is too large");
+    const dim3 grid((unsigned)most, s->n_kv_heads, 2);
     by_shape(s, [&](auto t, auto c, auto h) { kv_read_kernel<decltype(t), decltype(c), h.value><<<grid, 256, 0, (hipStream_t)hip_stream>>>(a); });
     return launched("asd_kv_read");
 }

@@ -119,3 +119,16 @@ def test_what_calls_rely_on_does_not_change(kind, names):
         with pytest.raises(AttributeError):
             setattr(x, name, 2)
         assert getattr(x, name) == 1
+
+
+@pytest.mark.parametrize("name", ["append", "attend"])
+def test_launches_that_no_card_takes(name):
+    """65536 tokens of as many sequences with 4096 heads: more than 2^32 threads, and a launch's number of them must fit 32 bits."""
+    s, b = shape(n_heads=4096, n_kv_heads=4096, head_dim=32), batch(n_seqs=65536, n_rows=65536, max_new=1)
+    rc, why = call(name, s, b, qs=4096 * 32, ks=4096 * 32, vs=4096 * 32, os=4096 * 32, prep=asd.KvPrep(None, None, 0, P, 10, 32, 0))
+    assert rc == asd.E_INVAL and name in why and "too large" in why
+
+
+def test_a_read_that_no_card_takes():
+    rc, why = call("read", shape(n_heads=1, n_kv_heads=1, head_dim=32), batch(n_rows=(1 << 31) - 1), ks=32, vs=32)
+    assert rc == asd.E_INVAL and "too large" in why
