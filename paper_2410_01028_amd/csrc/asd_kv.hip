@@ -202,7 +202,8 @@ int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, i
     if (!why && (!q || !out)) why = "q and out must be device pointers";
     if (!why) why = rows_fault(s, q, q_stride, s->n_heads);
     if (!why) why = rows_fault(s, out, out_stride, s->n_heads);
-    if (!why && !(scale > 0.f && std::isfinite(scale))) why = "scale must be a positive number";
+    const float c2 = (float)((double)scale * 1.4426950408889634074);      // log2(e)
+    if (!why && !(scale > 0.f && std::isfinite(c2))) why = "scale must be a positive number, scale * log2(e) too";
     if (why) return refuse(ASD_E_INVAL, "asd_kv_attend: %s", why);
     const AttendPlan p = attend_plan(s, b);
     if (p.bytes && (!workspace || (uintptr_t)workspace % 256)) return refuse(ASD_E_INVAL, "asd_kv_attend: workspace must be 256-byte aligned");
@@ -211,7 +212,7 @@ int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, i
     KvAttendArgs a{};
     a.kv = kv_args(s, b);
     a.q = q; a.out = out; a.q_stride = q_stride; a.out_stride = out_stride;
-    a.c2 = (float)((double)scale * 1.4426950408889634074);
+    a.c2 = c2;
     a.o_part = (float*)workspace; a.ml_part = (float*)((char*)workspace + p.o_bytes);
     a.target = p.target; a.cut = p.join; a.min_run = p.min_run;
     const hipStream_t stream = (hipStream_t)hip_stream;

@@ -132,3 +132,9 @@ def test_launches_that_no_card_takes(name):
 def test_a_read_that_no_card_takes():
     rc, why = call("read", shape(n_heads=1, n_kv_heads=1, head_dim=32), batch(n_rows=(1 << 31) - 1), ks=32, vs=32)
     assert rc == asd.E_INVAL and "too large" in why
+
+
+def test_a_scale_that_overflows():
+    """scale * log2(e) is what the kernels multiply by: it must be a number, too."""
+    rc, why = call("attend", shape(), batch(), scale=3e38)
+    assert rc == asd.E_INVAL and "scale" in why
