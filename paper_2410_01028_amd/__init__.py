@@ -308,24 +308,31 @@ class Engine:
 
     def park(self, caches, page_table) -> int:
         """Copy the engine's sequence (positions 0 .. kv_len-1) into other pages, one KVCache per layer, 8-bit ones say, with the page table
-        [1, pages] of its place there (int32, on the device); returns its length.  Enqueued on the engine's stream, behind the current one's work."""
-        n = self.kv_len
+        [1, pages] of its place there (int32, on the device); returns its length.  Runs on the engine's stream, behind the current one's work,
+        and has ended when the call returns."""
+        n, target = self.kv_len, self._layers(caches, page_table)
         if n:
-            self._move(n, [self.kv_cache(l) for l in range(self.cfg.n_layers)], [(c, page_table) for c in caches])
+            self._move(n, [self.kv_cache(l) for l in range(self.cfg.n_layers)], target)
         return n
 
     def resume(self, caches, page_table, n: int):
-        """Put a sequence of n tokens that park() has copied back into the engine: the next pass starts at position n."""
+        """Put a sequence of n tokens that park() has copied back into the engine: the next pass starts at position n.  If the copy fails
+        (a page or a length out of range), the engine holds no sequence."""
         if n < 0 or n > self.cfg.max_seq:
             raise AsdError(E_INVAL, f"length {n} outside the cache capacity {self.cfg.max_seq}")
+        source = self._layers(caches, page_table)
+        self._ck(_kv_lib().asd_set_kv_len(self._h, 0))
         if n:
-            self._move(n, [(c, page_table) for c in caches], [self.kv_cache(l) for l in range(self.cfg.n_layers)])
+            self._move(n, source, [self.kv_cache(l) for l in range(self.cfg.n_layers)])
         self._ck(_kv_lib().asd_set_kv_len(self._h, n))
+
+    def _layers(self, caches, page_table):
+        if len(caches) != self.cfg.n_layers:
+            raise AsdError(E_INVAL, f"one cache for each of the {self.cfg.n_layers} layers")
+        return [(c, page_table) for c in caches]
 
     def _move(self, n: int, source, target):
         """Rows 0 .. n-1 of every layer out of `source` into `target`: (KVCache, page table) pairs."""
-        if len(source) != self.cfg.n_layers or len(target) != self.cfg.n_layers:
-            raise AsdError(E_INVAL, f"one cache for each of the {self.cfg.n_layers} layers")
         torch = self._torch
         self.stream.wait_stream(torch.cuda.current_stream(self.device))
         with torch.cuda.stream(self.stream):
@@ -333,9 +340,9 @@ class Engine:
             for (a, a_table), (b, b_table) in zip(source, target):
                 both = [KVBatch(t, rows, length, n, n, n) for t in (a_table, b_table)]
                 k, v = a.read(both[0])
+                both[0].check()                          # (what could not be read is not written either)
                 b.append(both[1], None, k, v)
-                for batch in both:
-                    batch.check()
+                both[1].check()
 
     def reset(self):
         self._ck(lib().asd_reset(self._h))

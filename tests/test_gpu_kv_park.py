@@ -65,3 +65,30 @@ def test_the_engines_cache_under_attend():
     e = 2 * TINY.head_dim * 2.0 ** -24 * big[..., None] + 2.0 ** -20 + 100 * 2.0 ** -24
     assert bool(((out.double() - want).abs() <= size * e + want.abs() * 2.0 ** -24).all())
     eng.close()
+
+
+def test_a_sequence_that_cannot_be_put_back():
+    """A page table that leads out of the pool, or does not reach far enough: the engine's pages may hold parts of two sequences then, so it has none.
+    Where nothing was begun, its own stays."""
+    eng = asd.Engine(asd.make_config(TINY, 256, page_tokens=64)).init_synthetic(3)
+    caches = pools(TINY, 2, 64, TINY.dtype)
+    table = torch.tensor([[1, 0]], dtype=torch.int32, device="cuda:0")
+    toks = si.prompt(2, 100, TINY.vocab)
+    eng.prefill(toks)
+    want = eng.get_kv(1, 0, 100)
+    assert eng.park(caches, table) == 100
+    for bad in (caches[1:], caches + caches[:1]):
+        with pytest.raises(asd.AsdError):
+            eng.resume(bad, table, 100)
+        assert eng.kv_len == 100
+    with pytest.raises(asd.AsdError, match="pages"):
+        eng.resume(caches, torch.tensor([[1, 2]], dtype=torch.int32, device="cuda:0"), 100)
+    assert eng.kv_len == 0
+    with pytest.raises(asd.AsdError, match="lengths"):
+        eng.resume(caches, table, 129)
+    assert eng.kv_len == 0
+    eng.resume(caches, table, 100)
+    assert eng.kv_len == 100
+    got = eng.get_kv(1, 0, 100)
+    assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
+    eng.close()
