@@ -394,10 +394,11 @@ int asd_plan_prompt(const asd_config* cfg, int32_t n, int32_t block, asd_prompt_
  *
  * Rows: the new tokens of all sequences lie packed, sequence s in rows row_start[s] .. row_start[s+1]-1 of q, k, v, out;
  * rows outside are left as they are.  kv_len[s] counts the tokens of the sequence WITH its new ones: row i of n has
- * position kv_len[s] - n + i and sees the keys 0 .. position of its own sequence.
+ * position kv_len[s] - n + i and sees the keys 0 .. position of its own sequence.  Rows in front of position 0 (more new rows than tokens,
+ * which ASD_KV_BAD_ROWS reports) have no place: asd_kv_append and asd_kv_read leave them as they are, asd_kv_attend gives zeros.
  *
  * Pages: page p holds page_tokens consecutive tokens of one sequence for all KV heads, asd_kv_page_bytes() bytes.  The j-th
- * page of sequence s is page_table[s * table_stride + j].  A page is, per KV head, page_tokens / 64 chunks of 64 tokens,
+ * page of sequence s is page_table[s * table_stride + j]; sequences may share pages, as long as no two of a batch write the same token's place.  A page is, per KV head, page_tokens / 64 chunks of 64 tokens,
  * each the chunk's K fragments, then its V^T fragments; a fragment is what a wave of 64 lanes loads at once, 16 bytes a lane
  * (lane 16g + r), KE values (16 codes, 8 bf16, 4 fp32; D = min(KE, head_dim / 4) values of K):
  *   K fragment (kt, hp), order kt * head_dim / 4D + hp: key(kt, r) of the chunk, dims hp * 4D + g * D ..
@@ -456,7 +457,7 @@ int asd_kv_append(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_pre
 
 /*
  * Attention of the batch's new rows over their sequences' pages (the new tokens' keys and values are in them already):
- * out = sum_j softmax_j(scale * q.k_j) v_j over the keys j <= position; zeros for a row that sees no key.  scale > 0.  workspace:
+ * out = sum_j softmax_j(scale * q.k_j) v_j over the keys j <= position; zeros for a row that sees no key.  scale > 0.  out may be q.  workspace:
  * at least asd_kv_attend_workspace() bytes, 256-byte aligned; its contents need not be set and mean nothing afterwards, but no
  * other work may use it until the call's kernels have run.  A captured call keeps using the workspace it was given.
  * With 8-bit or bf16 caches and bf16 rows the weights are rounded to bf16 for the product with V; sums are fp32.

@@ -514,7 +514,8 @@ class KVBatch(_Fixed):
     """New rows of several sequences (asd_kv_batch): int32 device tensors page_table [n_seqs, pages], row_start [n_seqs + 1],
     kv_len [n_seqs] (tokens with the new ones), and the bounds that hold for them: rows of the row buffers, most new rows
     and most tokens of a sequence.  The tensors are read when a call's kernels run: update them in place between calls.
-    status: an int32 word on the device that kernels set bits of where the arrays held something out of range; check() reads it."""
+    status: an int32 word on the device that kernels set bits of where the arrays held something out of range; check() reads it.  The word is cleared, and read, on the
+    current stream: calls on another one wait for it, and check() comes after them."""
 
     def __init__(self, page_table, row_start, kv_len, n_rows: int, max_new: int, max_len: int):
         import torch

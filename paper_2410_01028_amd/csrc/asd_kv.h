@@ -728,7 +728,7 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(cons
 #pragma unroll
             for (int i = 0; i < PS; ++i) {
                 if constexpr (AE == 8) {
-                    // bf16, as V is: each weight is off by at most 2^-9 of itself, and the sum of weights is taken unrounded
+                    // bf16, as V is: each weight is off by at most 2^-8 of itself, and the sum of weights is taken unrounded
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
                         const int e = 2 * x, kt = 2 * i + e / 4;
