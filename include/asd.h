@@ -409,7 +409,8 @@ int asd_plan_prompt(const asd_config* cfg, int32_t n, int32_t block, asd_prompt_
  * max|x| * 2^-e <= 448 over that token's finite values of the head; a code is x * 2^-e rounded to nearest even, and stands for
  * code * 2^e.  A value that is not finite is held as NaN.
  *
- * What the arrays hold cannot be refused when a call is made.  Rows and lengths are cut to the bounds, a page outside the pool is
+ * What the arrays hold cannot be refused when a call is made.  Rows and lengths are cut to the bounds, no row belongs to two sequences (where
+ * row_start descends, and behind that, a sequence that begins in front of the end of an earlier one has no rows), a page outside the pool is
  * neither written nor read (its keys count as hidden, its rows are not read back), a position past the rotary table takes the
  * table's last row; each sets a bit in *status, which the caller clears and reads (ASD_KV_BAD_*; optional).
  */

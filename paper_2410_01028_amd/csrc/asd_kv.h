@@ -61,14 +61,26 @@ __device__ __forceinline__ KvSeq kv_seq(const KvArgs& a, int s, bool* bad = null
 __device__ __forceinline__ void kv_flag(const KvArgs& a, int bit) { if (a.status) atomicOr(a.status, bit); }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// A wave's view of the batch, 64 sequences at a time: the first 64 stay in registers.  check: the wave reports arrays out of range.
+// A wave's view of the batch, 64 sequences at a time, in order: the first 64 stay in registers.  check: the wave reports arrays out of range.
+// Launches and workspaces have room for tiles of n_rows rows, so no row may belong to two sequences.  Where nothing is bad, none does; from the first
+// bad sequence on, one that begins in front of the end (top) of an earlier one has no rows.
 struct KvLanes {
     KvSeq v;
+    int top = -1;                                       // (nothing was bad so far)
     __device__ __forceinline__ void load(const KvArgs& a, int s0, int lane, bool check) {
         v = KvSeq{0, 0, 0};
         bool bad = false;
         if (s0 + lane < a.n_seqs) v = kv_seq(a, s0 + lane, &bad);
-        if (check && bad) kv_flag(a, ASD_KV_BAD_ROWS);
+        if (__any(bad) || top >= 0) apart(a, s0, lane, check && bad);
+    }
+    __device__ __forceinline__ void apart(const KvArgs& a, int s0, int lane, bool flag) {
+        if (flag) kv_flag(a, ASD_KV_BAD_ROWS);
+        if (top < 0) top = min(max(a.row_start[s0], 0), a.n_rows);      // (the sequences in front of s0 lie one behind the other)
+        int end = v.r0 + v.n;
+        for (int o = 1; o < 64; o <<= 1) { const int t = __shfl_up(end, o); if (lane >= o) end = max(end, t); }
+        const int before = __shfl_up(end, 1);
+        if (v.r0 < max(top, lane ? before : 0)) v.n = 0;
+        top = max(top, __shfl(end, 63));
     }
 };
 __device__ __forceinline__ int wave_sum_upto(int c, int lane) {          // inclusive
