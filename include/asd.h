@@ -409,10 +409,11 @@ int asd_plan_prompt(const asd_config* cfg, int32_t n, int32_t block, asd_prompt_
  * max|x| * 2^-e <= 448 over that token's finite values of the head; a code is x * 2^-e rounded to nearest even, and stands for
  * code * 2^e.  A value that is not finite is held as NaN.
  *
- * What the arrays hold cannot be refused when a call is made.  Rows and lengths are cut to the bounds, no row belongs to two sequences (where
- * row_start descends, and behind that, a sequence that begins in front of the end of an earlier one has no rows), a page outside the pool is
- * neither written nor read (its keys count as hidden, its rows are not read back), a position past the rotary table takes the
- * table's last row; each sets a bit in *status, which the caller clears and reads (ASD_KV_BAD_*; optional).
+ * What the arrays hold cannot be refused when a call is made.  Rows outside 0 .. n_rows-1, more rows of a sequence than max_new (the first ones count) and
+ * rows at positions past max_len or the table's reach are as if they were no rows of the batch; the others keep their position, kv_len[s] - row_start[s+1]
+ * plus the row's number.  No row belongs to two sequences: where row_start descends, and behind that, a sequence that begins in front of the end of an
+ * earlier one has no rows.  A page outside the pool is neither written nor read (its keys count as hidden, its rows are not read back), a position past the
+ * rotary table takes the table's last row.  Each sets a bit in *status, which the caller clears and reads (ASD_KV_BAD_*; optional).
  */
 enum { ASD_KV_BAD_ROWS = 1,     /* row_start not ascending within 0 .. n_rows, more new rows than max_new or than tokens, kv_len above max_len or the table's reach */
        ASD_KV_BAD_PAGE = 2,     /* a page outside 0 .. n_pages-1 where a page was needed */

@@ -47,7 +47,8 @@ struct KvArgs {
     int32_t n_h, n_kv, group, page_tokens;
 };
 
-// One sequence's rows and length, held inside the buffers whatever the arrays say
+// One sequence's rows (n of them from row r0 on) and the position behind the last (len; rows in front of position 0 are possible), held inside the
+// buffers whatever the arrays say
 struct KvSeq { int r0, n, len; };
 __device__ __forceinline__ KvSeq kv_seq(const KvArgs& a, int s, bool* bad = nullptr) {
     const int f0 = a.row_start[s], f1 = a.row_start[s + 1], fl = a.kv_len[s];
@@ -62,8 +63,8 @@ __device__ __forceinline__ void kv_flag(const KvArgs& a, int bit) { if (a.status
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // A wave's view of the batch, 64 sequences at a time, in order: the first 64 stay in registers.  check: the wave reports arrays out of range.
-// Launches and workspaces have room for tiles of n_rows rows, so no row may belong to two sequences.  Where nothing is bad, none does; from the first
-// bad sequence on, one that begins in front of the end (top) of an earlier one has no rows.
+// From the first bad sequence on: rows keep the positions that the arrays give them, whatever is cut, and those past cap are left out.  Launches and
+// workspaces have room for tiles of n_rows rows, so no row may belong to two sequences: one that begins in front of the end (top) of an earlier one has none.
 struct KvLanes {
     KvSeq v;
     int top = -1;                                       // (nothing was bad so far)
@@ -71,12 +72,21 @@ struct KvLanes {
         v = KvSeq{0, 0, 0};
         bool bad = false;
         if (s0 + lane < a.n_seqs) v = kv_seq(a, s0 + lane, &bad);
-        if (__any(bad) || top >= 0) apart(a, s0, lane, check && bad);
+        if (__any(bad) || top >= 0) mend(a, s0, lane, bad, check);
     }
-    __device__ __forceinline__ void apart(const KvArgs& a, int s0, int lane, bool flag) {
-        if (flag) kv_flag(a, ASD_KV_BAD_ROWS);
+    __device__ __forceinline__ void mend(const KvArgs& a, int s0, int lane, bool bad, bool check) {
+        int end = 0;
+        if (s0 + lane < a.n_seqs) {
+            const int f1 = a.row_start[s0 + lane + 1];
+            end = min(max(f1, v.r0), a.n_rows);
+            if (bad) {
+                if (check) kv_flag(a, ASD_KV_BAD_ROWS);
+                const int64_t first = (int64_t)a.kv_len[s0 + lane] - f1 + v.r0;      // position of row r0
+                v.n = (int)max(min((int64_t)v.n, a.cap - first), (int64_t)0);
+                v.len = (int)min(max(first + v.n, (int64_t)0), (int64_t)a.cap);
+            }
+        }
         if (top < 0) top = min(max(a.row_start[s0], 0), a.n_rows);      // (the sequences in front of s0 lie one behind the other)
-        int end = v.r0 + v.n;
         for (int o = 1; o < 64; o <<= 1) { const int t = __shfl_up(end, o); if (lane >= o) end = max(end, t); }
         const int before = __shfl_up(end, 1);
         if (v.r0 < max(top, lane ? before : 0)) v.n = 0;
@@ -529,7 +539,7 @@ template <int NT> __device__ __forceinline__ int kv_run(const KvAttendArgs& a, c
     if (!a.cut) return 1 << 28;
     auto units = [&](const KvSeq& v) { return (int64_t)kv_tiles<NT>(a.kv, v) * ((v.len + 63) / 64); };
     int64_t t = units(all.v);
-    for (int s = lane + 64; s < a.kv.n_seqs; s += 64) t += units(kv_seq(a.kv, s));
+    for (int s = lane + 64; s < a.kv.n_seqs; s += 64) t += units(kv_seq(a.kv, s));      // (of bad ones no less than they have: longer runs)
     if (a.kv.n_seqs > 1) {
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);

@@ -24,9 +24,8 @@ def rows_of(row_start, n_rows, max_new, disjoint=True):
     out, top = [], 0
     for f0, f1 in zip(row_start, row_start[1:]):
         r0 = min(max(f0, 0), n_rows)
-        n = min(min(max(f1, r0), n_rows) - r0, max_new)
-        end = r0 + n
-        out.append((r0, 0 if disjoint and r0 < top else n))
+        end = min(max(f1, r0), n_rows)
+        out.append((r0, 0 if disjoint and r0 < top else min(end - r0, max_new)))
         top = max(top, end)
     return out
 
