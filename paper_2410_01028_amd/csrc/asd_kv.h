@@ -1133,7 +1133,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_rows_kernel(const KvAttendArgs 
             }
             if (c >= c_end) break;
             turn();
-            clean(c);
+            if (c >= c_main) clean(c);                   // (beside a missing page: what all rows see goes through the products)
             if (c < c_my && !((gone >> (c & 31)) & 1u)) work(c, std::true_type{}); else ask();
             done();
             gone &= ~(1u << (c & 31));
