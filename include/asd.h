@@ -407,7 +407,7 @@ int asd_plan_prompt(const asd_config* cfg, int32_t n, int32_t block, asd_prompt_
  * which for fp32 and bf16 is the engine's own cache of one layer.  An 8-bit cache holds e4m3 codes there and behind them 64
  * bytes for K and 64 for V, one per token: 127 + e, where e is the least integer (in -100 .. 120; 0 for a row of zeros) with
  * max|x| * 2^-e <= 448 over that token's finite values of the head; a code is x * 2^-e rounded to nearest even, and stands for
- * code * 2^e.  A value that is not finite is held as NaN.
+ * code * 2^e (magnitudes of 248 * 2^120 and more as 240 * 2^120: a finite value stays finite).  A value that is not finite is held as NaN.
  *
  * What the arrays hold cannot be refused when a call is made.  Rows outside 0 .. n_rows-1, more rows of a sequence than max_new (the first ones count) and
  * rows at positions past max_len or the table's reach are as if they were no rows of the batch; the others keep their position, kv_len[s] - row_start[s+1]

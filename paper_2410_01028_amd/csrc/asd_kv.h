@@ -354,7 +354,10 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
 #pragma unroll
             for (int o = 1; o < LPV; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
             float y[2][DU];
-            const bool odd = top >= 0x7f800000u;       // something is not finite: it becomes NaN, and the scale comes from the rest
+            // Something is not finite: it becomes NaN, and the scale comes from the rest.  Or a magnitude of 248 * 2^120 and more, whose code would be
+            // 256, beyond fp32 with that scale, the largest: 240 (off by 2^-4 of it at most, as a rounding may be)
+            constexpr uint32_t MOST = 0x7f780000u;
+            const bool odd = top >= MOST;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -365,8 +368,13 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const KvAppendArgs a) {
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int j = 0; j < DU; ++j) {
-                        if (finite(y[i][j])) top = max(top, __float_as_uint(y[i][j]) & 0x7fffffffu);
-                        else y[i][j] = __uint_as_float(0x7fc00000u);
+                        const uint32_t u = __float_as_uint(y[i][j]), m = u & 0x7fffffffu;
+                        if (m < 0x7f800000u) {
+                            top = max(top, m);
+                            if (m >= MOST) y[i][j] = __uint_as_float((u & 0x80000000u) | 0x7f700000u);
+                        } else {
+                            y[i][j] = __uint_as_float(0x7fc00000u);
+                        }
                     }
 #pragma unroll
                 for (int o = 1; o < LPV; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
