@@ -480,8 +480,16 @@ def _kv_ck(rc: int):
         raise AsdError(rc, lib().asd_last_error(None).decode())
 
 
+def _fits(**numbers):
+    """The library takes these in 32 bits (ctypes would keep the low ones and say nothing)."""
+    for name, n in numbers.items():
+        if not -1 << 31 <= n < 1 << 31:
+            raise AsdError(E_INVAL, f"{name} = {n} does not fit 32 bits")
+
+
 def kv_page_bytes(n_heads: int, n_kv_heads: int, head_dim: int, page_tokens: int, dtype: int = DT_BF16, kv_dtype: int = DT_FP8) -> int:
     """Bytes of one page of a KVCache (asd_kv_page_bytes)."""
+    _fits(n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, page_tokens=page_tokens, dtype=dtype, kv_dtype=kv_dtype)
     n = int(_kv_lib().asd_kv_page_bytes(ctypes.byref(KvShape(n_heads, n_kv_heads, head_dim, page_tokens, dtype, kv_dtype))))
     if n == 0:
         raise AsdError(E_INVAL, "invalid cache shape")
@@ -519,6 +527,7 @@ class KVBatch(_Fixed):
 
     def __init__(self, page_table, row_start, kv_len, n_rows: int, max_new: int, max_len: int):
         import torch
+        _fits(n_rows=n_rows, max_new=max_new, max_len=max_len)
         for name, t, dims in (("page_table", page_table, 2), ("row_start", row_start, 1), ("kv_len", kv_len, 1)):
             if t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous() or t.device != kv_len.device:
                 raise AsdError(E_INVAL, f"{name} must be a contiguous int32 tensor of {dims} dimension(s) on the batch's device")
@@ -605,6 +614,8 @@ class KVCache(_Fixed):
         """Write the batch's new rows into the pages (asd_kv_append): q [n_rows, n_heads, head_dim] or None, k and v
         [n_rows, n_kv_heads, head_dim]; rope [positions, rot_dim / 2, 2] as rope_table makes it, gains [head_dim].  Returns the
         prepared queries (q_out, which may be q; a new tensor if it is not given)."""
+        if not 0 <= rot_dim <= self.head_dim:
+            raise AsdError(E_INVAL, f"rot_dim {rot_dim} of head_dim {self.head_dim}")
         bound, prep = self._batch(batch), KvPrep(None, None, eps, None, 0, rot_dim, interleaved)
         if q is None and q_out is not None:
             raise AsdError(E_INVAL, "q_out without q")
@@ -670,6 +681,7 @@ def rope_table(rot_dim: int, positions: int, theta: float = 10000.0, kind: int =
                trained: float = 4096.0, gain: float = 1.0, device: str = "cuda:0"):
     """Rotary table [positions, rot_dim / 2, 2] for KVCache.append (asd_rope_table), enqueued on the device's current stream."""
     import torch
+    _fits(rot_dim=rot_dim, positions=positions, kind=kind)
     device = torch.device(device)
     if device.type != "cuda":
         raise AsdError(E_INVAL, "the table is made on the GPU")
