@@ -541,7 +541,7 @@ struct KvAttendArgs {
 };
 // How a batch is cut.  The rows of a sequence and KV head are its new tokens x the heads of the group; a tile is 16 * NT of
 // them.  With `cut`, all tiles' key ranges are cut into runs of `run` chunks, the same for every sequence, so that about `target` items come out
-// whatever the lengths are: one long conversation among short ones is spread over the card.
+// whatever the lengths are: one long conversation among short ones is spread over the card.  (attend_plan in asd_kv.hip says which batches are cut.)
 template <int NT> __device__ __forceinline__ int kv_tiles(const KvArgs& a, const KvSeq& v) { return (int)(((int64_t)v.n * a.group + 16 * NT - 1) / (16 * NT)); }
 template <int NT> __device__ __forceinline__ int kv_run(const KvAttendArgs& a, const KvLanes& all, int lane) {
     if (!a.cut) return 1 << 28;

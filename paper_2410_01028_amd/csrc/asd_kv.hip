@@ -119,12 +119,15 @@ AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b) {
     if (p.rows) p.nt = 8;
     p.max_tiles = (int32_t)tiles(p.nt);
     // Keys are cut into about four items per compute unit (48 sequences of 500 to 8192 tokens: 90 us, with two 100, with eight 97), but not
-    // into runs of fewer than 16 chunks (with 8, five rows of eight sequences of 1031 tokens take 19.1 us, not 16.9), and not where the
-    // tiles of kv_rows_kernel are as many by themselves
+    // into runs of fewer than 16 chunks (with 8, five rows of eight sequences of 1031 tokens take 19.1 us, not 16.9), and not where
+    // kv_rows_kernel's tiles are as many by themselves: full ones, or, as long as none is long, ones that a token alone may have.  (64 / 8 heads x 128,
+    // 8 bits, 128 tokens behind 400, 512 rows behind 3488 and a token behind 4000: 164 us, cut 177; behind 8192: 245 and 178; behind 60000: 1493
+    // and 221.  128 tokens behind 400 .. 8192 and the 512 rows: 402 and 428, behind 400 .. 16384 734 and 703)
     p.min_run = 16;
     p.target = 4 * units();
-    const int64_t whole = (int64_t)p.max_tiles * s->n_kv_heads, most = (chunks + p.min_run / 2) / p.min_run;      // runs of the longest sequence
-    p.join = most > 1 && !(p.rows && whole >= p.target);
+    const int64_t whole = (int64_t)p.max_tiles * s->n_kv_heads, full = (int64_t)b->n_rows * group / (16 * p.nt) * s->n_kv_heads;
+    const int64_t most = (chunks + p.min_run / 2) / p.min_run;      // runs of the longest sequence
+    p.join = most > 1 && !(p.rows && (full >= p.target || (whole >= p.target && chunks < 128)));
     p.grid = p.join ? whole + p.target : whole;
     if (p.join && whole * most < p.grid) p.grid = whole * most;
     if (p.join) {
