@@ -459,10 +459,12 @@ int asd_kv_append(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_pre
 
 /*
  * Attention of the batch's new rows over their sequences' pages (the new tokens' keys and values are in them already):
- * out = sum_j softmax_j(scale * q.k_j) v_j over the keys j <= position; zeros for a row that sees no key.  scale > 0.  out may be q.  workspace:
+ * out = sum_j softmax_j(scale * q.k_j) v_j over the keys j <= position; zeros for a row that sees no key, or none whose score is above -infinity.
+ * scale > 0.  out may be q.  workspace:
  * at least asd_kv_attend_workspace() bytes, 256-byte aligned; its contents need not be set and mean nothing afterwards, but no
  * other work may use it until the call's kernels have run.  A captured call keeps using the workspace it was given.
- * With 8-bit or bf16 caches and bf16 rows the weights are rounded to bf16 for the product with V; sums are fp32.
+ * With 8-bit or bf16 caches and bf16 rows the weights are rounded to bf16 for the product with V (2^-8 of each at most; the engine's own passes keep two
+ * bf16 planes of them); sums are fp32, of weights of up to 2^8 times values, and divided at the end: 256 * keys * max|v| must stay below 2^128.
  */
 size_t asd_kv_attend_workspace(const asd_kv_shape* s, const asd_kv_batch* b);
 int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, int64_t q_stride, void* out, int64_t out_stride, float scale,

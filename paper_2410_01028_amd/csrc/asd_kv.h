@@ -886,11 +886,12 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(cons
 
 // Many rows (bf16): NW waves with 16 * NT rows each walk a run of chunks together, their fragments in LDS once for all of them.  They come by
 // direct loads into a ring of five half-chunks (K, V^T, K, ..): one barrier per chunk c, behind which K and V^T of c have landed
-// and the slots of c - 1 may be asked for anew (V^T of c + 1, K of c + 2).  A SIMD has two waves, one's products beside the other's exponentials.
+// and the slots of c - 1 may be asked for anew (V^T of c + 1, K of c + 2).  A SIMD has two waves.
 // (Prompts of 1035 to 2048 tokens, 32 heads x 128, bf16 pages, took 160 us so at the step when four waves of 16 rows took 199 and two waves with the
-// next product's fragments in registers 200, both spilling.)  Bound by the vector unit, exponentials and in 8 bits the widening, which each wave
-// does for itself: it issues in 53 % of the busy cycles (8 bits 73), the matrix cores are at work in 38.  These prompts now take 144 us (716 TFLOP/s),
-// one of 8192 tokens 1001 TFLOP/s (8-bit pages 944); 512 rows behind 8195 tokens and 260 behind 2665 in 8 bits, 64 / 8 heads, 214 us with the join.
+// next product's fragments in registers 200, both spilling.)  Bound by products and exponentials (in 8 bits the widening, too, which each
+// wave does for itself) one after the other: the vector unit issues in 53 % of the busy cycles (8 bits 73), the matrix cores are at work in 38 (37),
+// little of it at the same time; and by what each tile takes once.  These prompts now take 137 to 143 us (8-bit pages 156), 720 to 750 TFLOP/s,
+// one of 8192 tokens 1001 TFLOP/s (944); 512 rows behind 8195 tokens and 260 behind 2665 in 8 bits, 64 / 8 heads, 214 us with the join.
 template <class C, int H, int NT, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void kv_rows_kernel(const KvAttendArgs a) {
     using A = BF16;
@@ -1003,7 +1004,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_rows_kernel(const KvAttendArgs 
             // The four score tiles side by side, so that no product waits for the one before it, and the fragments of a step
             // are read while the step before it runs; so too the output tiles below, two at a time (the fences keep that order)
             u32x4 f[2][4];
-            __builtin_amdgcn_s_setprio(1);               // products ahead of another wave's exponentials
+            __builtin_amdgcn_s_setprio(1);               // products ahead of what else the other wave has to issue
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) f[0][kt] = kp[kt * HP * 64];
 #pragma unroll

@@ -107,14 +107,16 @@ AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b) {
     const int64_t seqs = b->n_seqs < b->n_rows ? b->n_seqs : b->n_rows;
     auto tiles = [&](int nt) { return (int64_t)b->n_rows * group / (16 * nt) + seqs; };      // the most that there can be
     // Which kernel.  kv_attend_kernel's workgroups are many and short, its tiles read a sequence's pages again for every 16 rows (mostly from L2);
-    // kv_rows_kernel reads them once for 128 rows, with a step's cost whether they are all in use or not.  Up to 32 rows the first one, whatever
-    // the lengths (64 sequences of 32 rows, 4000 tokens, 8 bits: 130 us against 172).  Above, the second one where the first has more than
-    // two rounds of workgroups (16 x 32 heads, 40 rows, 128 tokens: 13 us against 23) or more than 64 chunks per compute unit (2 x 32 heads, 100 rows, 4000 tokens:
-    // 42 against 59; with 1000 tokens 34 against 17).
+    // kv_rows_kernel reads them once for 128 rows, with a step's cost whether they are all in use or not.  Up to 32 rows (new tokens x heads of a group)
+    // the first one, whatever the lengths (64 sequences of 4 new tokens, 4000 in all, 64 / 8 heads x 128: 8 bits 131 us against 171, bf16 pages 191
+    // against 217).  Above, the second one where the first has more than two rounds of workgroups (16 sequences of 40 new tokens, 128 in all, 32 / 32
+    // heads: 13 us against 23, 14 against 25) or more than 64 chunks per compute unit (two sequences of 100 new tokens, 32 / 32 heads, 4000 in all:
+    // 42 against 62, 41 against 71; with 1000 in all 33 against 17, 29 against 19).
     const int64_t work = tiles(1) * s->n_kv_heads;
     p.rows = bf16 && s->head_dim >= 64 && rows > 32 && (work > 4 * (int64_t)units() || work * chunks > 64 * (int64_t)units());
-    // 16 rows to a tile; 32 where a fragment's second use is worth more than twice the workgroups: bf16 pages of some length (64 sequences of 24 rows, 4000 tokens:
-    // 182 us against 256; 8 bits 141 against 128), and codes widened for fp32 products in a batch that fills the card (4 x 500 rows: 337 against 409)
+    // 16 rows to a tile; 32 where a fragment's second use is worth more than twice the workgroups: bf16 pages of some length (64 sequences of 3 new tokens,
+    // 4000 in all, 64 / 8 heads x 128: 187 us against 269; 8 bits 142 against 135), and codes widened for fp32 products in a batch that fills the card
+    // (four prompts of 500, 32 / 32 heads x 128: 186 against 224; with 8 / 8 heads, just below the border, the rule's 63 against 57).
     p.nt = rows <= 16 ? 1 : bf16 ? (!q8 && chunks >= 8 ? 2 : 1) : (q8 && (int64_t)b->n_rows * s->n_heads / 32 >= 2 * units() ? 2 : 1);
     if (p.rows) p.nt = 8;
     p.max_tiles = (int32_t)tiles(p.nt);
@@ -170,7 +172,8 @@ int asd_kv_append(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_pre
     a.q_gain = p->q_gain; a.k_gain = p->k_gain; a.rope = p->rope; a.eps = p->eps;
     a.rope_positions = p->rope_positions; a.rot = p->rot_dim;
     // Tiles of 64 tokens, whole chunks, where there are enough of them to fill the card (6900 tokens of 32 + 32 heads, with the rows read back:
-    // 107 us, with tiles of 16 120 us); else tiles of 16, four times the workgroups
+    // 107 us, with tiles of 16 120 us; 20 tokens of 256 sequences 72 against 112); else tiles of 16, four times the workgroups.  (Rows are counted,
+    // not tiles: one token of each of 1024 sequences gets tiles of 64, too, and takes 176 us, with tiles of 16 158; into bf16 pages 159 and 127.)
     const int64_t seqs = b->n_seqs < b->n_rows ? b->n_seqs : b->n_rows;
     const int tok = (int64_t)b->n_rows * s->n_kv_heads / 64 >= 2 * (int64_t)units() ? 64 : 16;
     const int most = b->max_new < tok ? b->max_new : tok;           // tokens of a tile
