@@ -417,7 +417,8 @@ int asd_plan_prompt(const asd_config* cfg, int32_t n, int32_t block, asd_prompt_
  */
 enum { ASD_KV_BAD_ROWS = 1,     /* row_start not ascending within 0 .. n_rows, more new rows than max_new or than tokens, kv_len above max_len or the table's reach */
        ASD_KV_BAD_PAGE = 2,     /* a page outside 0 .. n_pages-1 where a page was needed */
-       ASD_KV_BAD_POS = 4 };    /* a position past the rotary table */
+       ASD_KV_BAD_POS = 4,      /* a position past the rotary table */
+       ASD_KV_BAD_GROUP = 8 };  /* group_start not ascending within 0 .. n_seqs, shared_len below 0 or above max_len or the table's reach */
 
 /* Types and widths.  head_dim 32, 64 or 128; n_heads a multiple of n_kv_heads (query head h uses KV head h / (n_heads / n_kv_heads));
  * page_tokens a multiple of 64; dtype (rows in and out) ASD_DT_F32 or ASD_DT_BF16; kv_dtype the same or ASD_DT_FP8. */
@@ -469,6 +470,34 @@ int asd_kv_append(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_pre
 size_t asd_kv_attend_workspace(const asd_kv_shape* s, const asd_kv_batch* b);
 int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, int64_t q_stride, void* out, int64_t out_stride, float scale,
                   void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The same with a sliding window: a row at position p sees the keys p - window + 1 .. p and the keys 0 .. sinks - 1, as far as they are at or in front of
+ * its position (window >= 1, sinks >= 0).  Keys that no row of the batch sees are not read: the pages behind a sequence's window, except those of
+ * its first tokens, may go back to the pool, and their entries in the page table may be anything.
+ */
+size_t asd_kv_attend_window_workspace(const asd_kv_shape* s, const asd_kv_batch* b, int32_t window, int32_t sinks);
+int asd_kv_attend_window(const asd_kv_shape* s, const asd_kv_batch* b, int32_t window, int32_t sinks, const void* q, int64_t q_stride, void* out,
+                         int64_t out_stride, float scale, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The same for groups of sequences that begin with the same tokens (samples of one prompt, drafts of one conversation, requests behind one system
+ * prompt): these keys are read once for all rows of a group.  Group g is the sequences group_start[g] .. group_start[g+1]-1; sequences may be in no
+ * group.  The keys 0 .. shared_len[g]-1 of its sequences are those of its FIRST sequence, read through that one's page table; the keys behind
+ * them are each sequence's own, read through its own.  So a sequence can leave a common beginning anywhere, inside a page too: its
+ * page there holds its own tokens only, and nothing is copied.  A sequence of which some new row does not lie behind the shared tokens
+ * (kv_len - new rows < shared_len) is read through its own table altogether, as is one in no group.
+ * group_start outside 0 .. n_seqs or descending: no sequence belongs to two groups, a group that begins in front of the end of an earlier one has none
+ * (ASD_KV_BAD_GROUP).  A group whose rows are not in order (ASD_KV_BAD_ROWS) may be taken as if its sequences were in none.
+ */
+typedef struct {
+    const int32_t* group_start;     /* [n_groups + 1] */
+    const int32_t* shared_len;      /* [n_groups] */
+    int32_t n_groups;               /* 1 .. 65536 */
+} asd_kv_groups;
+size_t asd_kv_attend_shared_workspace(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_groups* g);
+int asd_kv_attend_shared(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_groups* g, const void* q, int64_t q_stride, void* out,
+                         int64_t out_stride, float scale, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* The batch's rows (the last row_start[s+1] - row_start[s] tokens of each sequence) out of the pages, as values in dtype: k_out and v_out
  * [n_rows][n_kv_heads][head_dim] with a stride; either may be NULL. */

@@ -80,6 +80,10 @@ class KvBatch(ctypes.Structure):
                [(n, ctypes.c_int32) for n in ("n_pages", "table_stride", "n_seqs", "n_rows", "max_new", "max_len")]
 
 
+class KvGroups(ctypes.Structure):
+    _fields_ = [("group_start", ctypes.c_void_p), ("shared_len", ctypes.c_void_p), ("n_groups", ctypes.c_int32)]
+
+
 class KvPrep(ctypes.Structure):
     _fields_ = [("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p), ("eps", ctypes.c_float), ("rope", ctypes.c_void_p)] + \
                [(n, ctypes.c_int32) for n in ("rope_positions", "rot_dim", "interleaved")]
@@ -153,6 +157,12 @@ def _kv_lib():
         L.asd_kv_attend_workspace.restype = sz
         L.asd_kv_attend_workspace.argtypes = [vp, vp]
         L.asd_kv_attend.argtypes = [vp, vp, vp, i64, vp, i64, ctypes.c_float, vp, sz, vp]
+        L.asd_kv_attend_window_workspace.restype = sz
+        L.asd_kv_attend_window_workspace.argtypes = [vp, vp, i32, i32]
+        L.asd_kv_attend_window.argtypes = [vp, vp, i32, i32, vp, i64, vp, i64, ctypes.c_float, vp, sz, vp]
+        L.asd_kv_attend_shared_workspace.restype = sz
+        L.asd_kv_attend_shared_workspace.argtypes = [vp, vp, vp]
+        L.asd_kv_attend_shared.argtypes = [vp, vp, vp, vp, i64, vp, i64, ctypes.c_float, vp, sz, vp]
         L.asd_kv_read.argtypes = [vp, vp, vp, i64, vp, i64, vp]
         L.asd_rope_table.argtypes = [ctypes.POINTER(Rope), i32, vp, vp]
         L.asd_kv_view.argtypes = [vp, i32, shape, batch]
@@ -548,8 +558,27 @@ class KVBatch(_Fixed):
         bits = int(self.status.item())
         if bits:
             self.status.zero_()
-            names = [n for b, n in ((1, "rows or lengths"), (2, "pages"), (4, "positions past the rotary table")) if bits & b]
+            names = [n for b, n in ((1, "rows or lengths"), (2, "pages"), (4, "positions past the rotary table"), (8, "groups")) if bits & b]
             raise AsdError(E_INVAL, "batch out of range: " + ", ".join(names))
+
+
+class KVGroups(_Fixed):
+    """Groups of a batch's sequences that begin with the same tokens (asd_kv_groups): int32 device tensors group_start [n_groups + 1], the sequences
+    of each, and shared_len [n_groups], the tokens that they share.  Read when a call's kernels run, as a KVBatch's are."""
+
+    def __init__(self, group_start, shared_len):
+        import torch
+        for name, t in (("group_start", group_start), ("shared_len", shared_len)):
+            if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.device != shared_len.device:
+                raise AsdError(E_INVAL, f"{name} must be a contiguous int32 tensor of 1 dimension(s) on the groups' device")
+        if shared_len.device.type != "cuda":
+            raise AsdError(E_INVAL, "the groups' tensors must be on the GPU")
+        n = shared_len.numel()
+        if n < 1 or group_start.numel() != n + 1:
+            raise AsdError(E_INVAL, "group_start and shared_len must be of n_groups + 1 and n_groups entries, one group at least")
+        self.group_start, self.shared_len, self.n_groups, self.device = group_start, shared_len, n, shared_len.device
+        self._c = KvGroups(group_start.data_ptr(), shared_len.data_ptr(), n)
+        self._at = ctypes.addressof(self._c)
 
 
 class KVCache(_Fixed):
@@ -633,16 +662,15 @@ class KVCache(_Fixed):
         self._call(self._lib.asd_kv_append, self._s, ctypes.addressof(bound), ctypes.addressof(prep), *qp, *kp, *vp, *op)
         return q_out
 
-    def attend(self, batch: KVBatch, q, out=None, scale: float | None = None, workspace=None):
-        """Causal attention of the batch's new rows over their sequences' pages (asd_kv_attend); q and out [n_rows, n_heads, head_dim],
-        scale 1 / sqrt(head_dim) by default.  workspace: a uint8 tensor of attend_workspace(batch) bytes (by default one of the call's own)."""
+    def _attend(self, function, size, batch: KVBatch, form: tuple, key: tuple, q, out, scale, workspace):
+        """One of the library's forms of attention; form: its arguments behind the batch, key: what its workspace depends on beside the batch's bounds."""
         bound = self._batch(batch)
         if out is None:
             out = self._torch.empty((q.shape[0], self.n_heads, self.head_dim), dtype=self.torch_dtype, device=self.device)
         qp, op = self._rows("q", q, batch, self.n_heads), self._rows("out", out, batch, self.n_heads)
-        need = batch._workspace.get(self._key)
+        need = batch._workspace.get(key)
         if need is None:
-            need = batch._workspace[self._key] = self._lib.asd_kv_attend_workspace(self._s, ctypes.addressof(bound))
+            need = batch._workspace[key] = size(self._s, ctypes.addressof(bound), *form)
         if workspace is None:
             wp, wn = None, 0
             if need:
@@ -654,13 +682,42 @@ class KVCache(_Fixed):
             wp, wn = workspace.data_ptr(), workspace.numel()
         if scale is None:
             scale = self._scale
-        self._call(self._lib.asd_kv_attend, self._s, ctypes.addressof(bound), *qp, *op, scale, wp, wn)
+        self._call(function, self._s, ctypes.addressof(bound), *form, *qp, *op, scale, wp, wn)
         return out
+
+    def attend(self, batch: KVBatch, q, out=None, scale: float | None = None, workspace=None):
+        """Causal attention of the batch's new rows over their sequences' pages (asd_kv_attend); q and out [n_rows, n_heads, head_dim],
+        scale 1 / sqrt(head_dim) by default.  workspace: a uint8 tensor of attend_workspace(batch) bytes (by default one of the call's own)."""
+        return self._attend(self._lib.asd_kv_attend, self._lib.asd_kv_attend_workspace, batch, (), self._key, q, out, scale, workspace)
 
     def attend_workspace(self, batch: KVBatch) -> int:
         """Bytes of workspace that attend() of a batch with these bounds needs."""
         bound = self._batch(batch)
         return int(self._lib.asd_kv_attend_workspace(self._s, ctypes.addressof(bound)))
+
+    def attend_window(self, batch: KVBatch, q, window: int, sinks: int = 0, out=None, scale: float | None = None, workspace=None):
+        """attend() with a sliding window (asd_kv_attend_window): a row sees the last `window` tokens up to its own, and the first `sinks` tokens of
+        its sequence.  Pages that hold neither are not read.  workspace: attend_window_workspace(batch, window, sinks) bytes."""
+        _fits(window=window, sinks=sinks)
+        return self._attend(self._lib.asd_kv_attend_window, self._lib.asd_kv_attend_window_workspace, batch, (window, sinks), (self._key, window, sinks), q, out, scale, workspace)
+
+    def attend_window_workspace(self, batch: KVBatch, window: int, sinks: int = 0) -> int:
+        """Bytes of workspace that attend_window() of a batch with these bounds needs."""
+        _fits(window=window, sinks=sinks)
+        bound = self._batch(batch)
+        return int(self._lib.asd_kv_attend_window_workspace(self._s, ctypes.addressof(bound), window, sinks))
+
+    def attend_shared(self, batch: KVBatch, groups: KVGroups, q, out=None, scale: float | None = None, workspace=None):
+        """attend() where groups of sequences begin with the same tokens (asd_kv_attend_shared): those are read once for all rows of a group, through the
+        page table of its first sequence, the others through each sequence's own.  workspace: attend_shared_workspace(batch, groups) bytes."""
+        if groups.device != self.device:
+            raise AsdError(E_INVAL, "the groups are on another device than the pages")
+        return self._attend(self._lib.asd_kv_attend_shared, self._lib.asd_kv_attend_shared_workspace, batch, (groups._at,), (self._key, groups.n_groups), q, out, scale, workspace)
+
+    def attend_shared_workspace(self, batch: KVBatch, groups: KVGroups) -> int:
+        """Bytes of workspace that attend_shared() of a batch with these bounds and as many groups needs."""
+        bound = self._batch(batch)
+        return int(self._lib.asd_kv_attend_shared_workspace(self._s, ctypes.addressof(bound), groups._at))
 
     def read(self, batch: KVBatch, k_out=None, v_out=None):
         """The batch's rows out of the pages as values (asd_kv_read): (k, v) [n_rows, n_kv_heads, head_dim]; new tensors where none is given."""

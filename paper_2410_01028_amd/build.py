@@ -7,7 +7,7 @@ import sys
 import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRCS = [os.path.join(HERE, "csrc", n) for n in ("asd_engine.hip", "asd_kv.hip")]
+SRCS = [os.path.join(HERE, "csrc", n) for n in ("asd_engine.hip", "asd_kv.hip", "asd_kv_spans.hip")]
 LIB = os.path.join(HERE, "libasd.so")
 
 FLAGS = [

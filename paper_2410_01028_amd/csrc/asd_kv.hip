@@ -1,145 +1,36 @@
 // Host side of the operators over a paged cache of several sequences: argument checks, launch rules, the C ABI of asd.h.
-#include "../../include/asd.h"
-#include "asd_kv.h"
+#include "asd_kv_host.h"
+#include "asd_kv_attend.h"
+#include "asd_kv_plan.h"
 
-#include <cmath>
-#include <cstdarg>
-#include <cstdio>
-
-__attribute__((visibility("hidden"))) void asd_note_error(const char* message);
-
-namespace {
-
-int refuse(int code, const char* fmt, ...) {
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
-    try { asd_note_error(buf); } catch (...) {}
-    return code;
-}
-
-const char* shape_fault(const asd_kv_shape* s) {
-    if (!s) return "shape is NULL";
-    if (s->n_heads < 1 || s->n_kv_heads < 1 || s->n_heads % s->n_kv_heads) return "n_heads must be a positive multiple of n_kv_heads";
-    if (s->n_heads > 4096) return "more than 4096 heads";
-    if (s->head_dim != 32 && s->head_dim != 64 && s->head_dim != 128) return "head_dim must be 32, 64 or 128";
-    if (s->page_tokens < 64 || s->page_tokens % 64 || s->page_tokens > 1 << 24) return "page_tokens must be a positive multiple of 64";
-    if (s->dtype != ASD_DT_F32 && s->dtype != ASD_DT_BF16) return "dtype must be ASD_DT_F32 or ASD_DT_BF16";
-    if (s->kv_dtype != s->dtype && s->kv_dtype != ASD_DT_FP8) return "kv_dtype must be dtype or ASD_DT_FP8";
-    return nullptr;
-}
-
-const char* batch_fault(const asd_kv_shape* s, const asd_kv_batch* b) {
-    if (!b) return "batch is NULL";
-    if (!b->pages || (uintptr_t)b->pages % 16) return "pages must be a device pointer, 16-byte aligned";
-    if (!b->page_table || !b->row_start || !b->kv_len) return "page_table, row_start and kv_len must be device pointers";
-    if (((uintptr_t)b->page_table | (uintptr_t)b->row_start | (uintptr_t)b->kv_len | (uintptr_t)b->status) % 4) return "the batch's arrays must be 4-byte aligned";
-    if (b->n_pages < 1 || b->table_stride < 1) return "n_pages and table_stride must be positive";
-    if (b->n_seqs < 1 || b->n_seqs > 65536) return "n_seqs must be in 1..65536";
-    if (b->n_rows < 1 || (int64_t)b->n_rows * s->n_heads >= (int64_t)1 << 31) return "n_rows must be positive, and n_rows * n_heads below 2^31";
-    if (b->max_new < 1 || b->max_new > b->n_rows) return "max_new must be in 1..n_rows";
-    if (b->max_len < 1 || b->max_len > 1 << 24) return "max_len must be in 1..2^24";
-    return nullptr;
-}
-
-// a buffer of rows: pointer, stride from row to row, heads of a row
-const char* rows_fault(const asd_kv_shape* s, const void* p, int64_t stride, int heads) {
-    const int es = s->dtype == ASD_DT_BF16 ? 2 : 4;
-    if ((uintptr_t)p % 16 || stride * es % 16) return "row pointers and strides must be multiples of 16 bytes";
-    if (stride < (int64_t)heads * s->head_dim || stride > (int64_t)1 << 40) return "a row stride is smaller than a row";
-    return nullptr;
-}
-
-KvArgs kv_args(const asd_kv_shape* s, const asd_kv_batch* b) {
-    KvArgs a{};
-    a.pages = (char*)b->pages; a.table = b->page_table; a.row_start = b->row_start; a.kv_len = b->kv_len; a.status = b->status;
-    a.n_pages = b->n_pages; a.table_stride = b->table_stride; a.n_seqs = b->n_seqs; a.n_rows = b->n_rows; a.max_new = b->max_new;
-    const int64_t reach = (int64_t)b->table_stride * s->page_tokens;
-    a.cap = (int32_t)(reach < b->max_len ? reach : b->max_len);
-    a.n_h = s->n_heads; a.n_kv = s->n_kv_heads; a.group = s->n_heads / s->n_kv_heads; a.page_tokens = s->page_tokens;
-    return a;
-}
-
-// f<row type, cache type, head dim>() for the shape
-template <class F> void by_shape(const asd_kv_shape* s, F f) {
-    auto dim = [&](auto t, auto c) {
-        if (s->head_dim == 32) f(t, c, std::integral_constant<int, 32>{});
-        else if (s->head_dim == 64) f(t, c, std::integral_constant<int, 64>{});
-        else f(t, c, std::integral_constant<int, 128>{});
-    };
-    const bool q8 = s->kv_dtype == ASD_DT_FP8;
-    if (s->dtype == ASD_DT_BF16) { if (q8) dim(BF16{}, FP8{}); else dim(BF16{}, BF16{}); }
-    else { if (q8) dim(F32{}, FP8{}); else dim(F32{}, F32{}); }
-}
-
-int launched(const char* what) {
-    const hipError_t r = hipGetLastError();
-    return r == hipSuccess ? ASD_OK : refuse(ASD_E_HIP, "%s: %s", what, hipGetErrorString(r));
-}
-
-int units() {
-    static const int n = [] {
-        int dev = 0, v = 0;
-        return hipGetDevice(&dev) == hipSuccess && hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && v > 0 ? v : 256;
-    }();
-    return n;
-}
-
-// Workgroups of 256 that a launch can have: its threads are counted in 32 bits
-constexpr int64_t MOST_GROUPS = ((int64_t)1 << 32) / 256 - 1;
-
-// How asd_kv_attend runs a batch of these bounds
-struct AttendPlan {
-    int nt;                        // 16-row column blocks of a tile
-    bool rows;                     // kv_rows_kernel
-    int32_t target, max_tiles, min_run;
-    int64_t grid;                  // most work items
-    bool join;                     // some sequence's keys may be cut
-    size_t o_bytes, bytes;
-};
-AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b) {
-    AttendPlan p{};
-    const int group = s->n_heads / s->n_kv_heads;
-    const int64_t rows = (int64_t)b->max_new * group, chunks = (kv_args(s, b).cap + 63) / 64;
-    const bool bf16 = s->dtype == ASD_DT_BF16, q8 = s->kv_dtype == ASD_DT_FP8;
-    const int64_t seqs = b->n_seqs < b->n_rows ? b->n_seqs : b->n_rows;
-    auto tiles = [&](int nt) { return (int64_t)b->n_rows * group / (16 * nt) + seqs; };      // the most that there can be
-    // Which kernel.  kv_attend_kernel's workgroups are many and short, its tiles read a sequence's pages again for every 16 rows (mostly from L2);
-    // kv_rows_kernel reads them once for 128 rows, with a step's cost whether they are all in use or not.  Up to 32 rows (new tokens x heads of a group)
-    // the first one, whatever the lengths (64 sequences of 4 new tokens, 4000 in all, 64 / 8 heads x 128: 8 bits 131 us against 171, bf16 pages 191
-    // against 217).  Above, the second one where the first has more than two rounds of workgroups (16 sequences of 40 new tokens, 128 in all, 32 / 32
-    // heads: 13 us against 23, 14 against 25) or more than 64 chunks per compute unit (two sequences of 100 new tokens, 32 / 32 heads, 4000 in all:
-    // 42 against 62, 41 against 71; with 1000 in all 33 against 17, 29 against 19).
-    const int64_t work = tiles(1) * s->n_kv_heads;
-    p.rows = bf16 && s->head_dim >= 64 && rows > 32 && (work > 4 * (int64_t)units() || work * chunks > 64 * (int64_t)units());
-    // 16 rows to a tile; 32 where a fragment's second use is worth more than twice the workgroups: bf16 pages of some length (64 sequences of 3 new tokens,
-    // 4000 in all, 64 / 8 heads x 128: 187 us against 269; 8 bits 142 against 135), and codes widened for fp32 products in a batch that fills the card
-    // (four prompts of 500, 32 / 32 heads x 128: 186 against 224; with 8 / 8 heads, just below the border, the rule's 63 against 57).
-    p.nt = rows <= 16 ? 1 : bf16 ? (!q8 && chunks >= 8 ? 2 : 1) : (q8 && (int64_t)b->n_rows * s->n_heads / 32 >= 2 * units() ? 2 : 1);
-    if (p.rows) p.nt = 8;
-    p.max_tiles = (int32_t)tiles(p.nt);
-    // Keys are cut into about four items per compute unit (48 sequences of 500 to 8192 tokens: 90 us, with two 100, with eight 97), but not
-    // into runs of fewer than 16 chunks (with 8, five rows of eight sequences of 1031 tokens take 19.1 us, not 16.9), and not where
-    // kv_rows_kernel's tiles are as many by themselves: full ones, or, as long as none is long, ones that a token alone may have.  (64 / 8 heads x 128,
-    // 8 bits, 128 tokens behind 400, 512 rows behind 3488 and a token behind 4000: 164 us, cut 177; behind 8192: 245 and 178; behind 60000: 1493
-    // and 221.  128 tokens behind 400 .. 8192 and the 512 rows: 402 and 428, behind 400 .. 16384 734 and 703)
-    p.min_run = 16;
-    p.target = 4 * units();
-    const int64_t whole = (int64_t)p.max_tiles * s->n_kv_heads, full = (int64_t)b->n_rows * group / (16 * p.nt) * s->n_kv_heads;
-    const int64_t most = (chunks + p.min_run / 2) / p.min_run;      // runs of the longest sequence
-    p.join = most > 1 && !(p.rows && (full >= p.target || (whole >= p.target && chunks < 128)));
-    p.grid = p.join ? whole + p.target : whole;
-    if (p.join && whole * most < p.grid) p.grid = whole * most;
-    if (p.join) {
-        p.o_bytes = ((size_t)p.grid * 16 * p.nt * s->head_dim * 4 + 255) / 256 * 256;
-        p.bytes = p.o_bytes + (size_t)p.grid * 16 * p.nt * 8;
+// ---------------------------------------------------------------- rotary tables
+// (cos, sin) of pos * frequency, in double; frequencies theta^(-2j / rot), changed for contexts longer than the trained one
+// (turns of frequency f over the trained length: r = trained * f / 2 pi):
+//   ASD_ROPE_LINEAR  f / factor
+//   ASD_ROPE_BANDS   f where r >= high, f / factor where r <= low, in between mixed by (r - low) / (high - low)
+//   ASD_ROPE_RAMP    mixed by the pair's index between the indexes that make `high` and `low` turns (rounded outwards), values times `gain`
+struct RopeArgs { double theta, factor, low, high, trained, gain; int32_t rot, kind, positions; };
+__global__ __launch_bounds__(256) void kv_rope_kernel(const RopeArgs a, float* out) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int hr = a.rot / 2;
+    if (i >= (int64_t)a.positions * hr) return;
+    const int j = (int)(i % hr), pos = (int)(i / hr);
+    const double two_pi = 6.283185307179586476925;
+    double f = pow(a.theta, -2.0 * j / a.rot);
+    if (a.kind == ASD_ROPE_LINEAR) f /= a.factor;
+    if (a.kind == ASD_ROPE_BANDS) {
+        const double keep = fmin(1.0, fmax(0.0, (a.trained * f / two_pi - a.low) / (a.high - a.low)));
+        f = keep * f + (1.0 - keep) * f / a.factor;
     }
-    return p;
+    if (a.kind == ASD_ROPE_RAMP) {
+        auto index = [&](double turns) { return a.rot * log(a.trained / (turns * two_pi)) / (2.0 * log(a.theta)); };
+        const double lo = fmax(0.0, floor(index(a.high))), hi = fmin(a.rot - 1.0, ceil(index(a.low)));
+        const double keep = 1.0 - fmin(1.0, fmax(0.0, (j - lo) / fmax(hi - lo, 1e-3)));
+        f = keep * f + (1.0 - keep) * f / a.factor;
+    }
+    out[2 * i] = (float)(cos(pos * f) * a.gain);
+    out[2 * i + 1] = (float)(sin(pos * f) * a.gain);
 }
-
-}  // namespace
 
 extern "C" {
 
@@ -198,7 +89,7 @@ int asd_kv_append(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_pre
 
 size_t asd_kv_attend_workspace(const asd_kv_shape* s, const asd_kv_batch* b) {
     if (shape_fault(s) || batch_fault(s, b)) return 0;
-    return attend_plan(s, b).bytes;
+    return attend_plan(s, b, whole_lengths(s, b)).bytes;
 }
 
 int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, int64_t q_stride, void* out, int64_t out_stride, float scale,
@@ -211,7 +102,7 @@ int asd_kv_attend(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, i
     const float c2 = (float)((double)scale * 1.4426950408889634074);      // log2(e)
     if (!why && !(scale > 0.f && std::isfinite(c2))) why = "scale must be a positive number, scale * log2(e) too";
     if (why) return refuse(ASD_E_INVAL, "asd_kv_attend: %s", why);
-    const AttendPlan p = attend_plan(s, b);
+    const AttendPlan p = attend_plan(s, b, whole_lengths(s, b));
     if (p.bytes && (!workspace || (uintptr_t)workspace % 256)) return refuse(ASD_E_INVAL, "asd_kv_attend: workspace must be 256-byte aligned");
     if (workspace_bytes < p.bytes) return refuse(ASD_E_NOMEM, "asd_kv_attend: workspace too small: %zu bytes given, %zu needed", workspace_bytes, p.bytes);
     if (p.grid > MOST_GROUPS) return refuse(ASD_E_INVAL, "asd_kv_attend: the batch is too large");

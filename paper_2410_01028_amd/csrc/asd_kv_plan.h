@@ -1,0 +1,66 @@
+// How the attention of a batch is run: which kernel, which tiles, how keys are cut.
+#pragma once
+#include "asd_kv_host.h"
+
+namespace {
+
+// How attention over a batch of these bounds runs
+struct AttendPlan {
+    int nt;                        // 16-row column blocks of a tile
+    bool rows;                     // kv_rows_kernel
+    int32_t target, max_tiles, min_run;
+    int64_t grid;                  // most work items
+    bool join;                     // some sequence's keys may be cut
+    size_t o_bytes, bytes;
+};
+// walk(R): the chunks that tiles of R rows walk at most.  small_tiles: 16 rows to a tile, always
+template <class F> AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b, F walk, bool small_tiles = false) {
+    AttendPlan p{};
+    const int group = s->n_heads / s->n_kv_heads;
+    const int64_t rows = (int64_t)b->max_new * group;
+    int64_t chunks = walk(16);
+    const bool bf16 = s->dtype == ASD_DT_BF16, q8 = s->kv_dtype == ASD_DT_FP8;
+    const int64_t seqs = b->n_seqs < b->n_rows ? b->n_seqs : b->n_rows;
+    auto tiles = [&](int nt) { return (int64_t)b->n_rows * group / (16 * nt) + seqs; };      // the most that there can be
+    // Which kernel.  kv_attend_kernel's workgroups are many and short, its tiles read a sequence's pages again for every 16 rows (mostly from L2);
+    // kv_rows_kernel reads them once for 128 rows, with a step's cost whether they are all in use or not.  Up to 32 rows (new tokens x heads of a group)
+    // the first one, whatever the lengths (64 sequences of 4 new tokens, 4000 in all, 64 / 8 heads x 128: 8 bits 131 us against 171, bf16 pages 191
+    // against 217).  Above, the second one where the first has more than two rounds of workgroups (16 sequences of 40 new tokens, 128 in all, 32 / 32
+    // heads: 13 us against 23, 14 against 25) or more than 64 chunks per compute unit (two sequences of 100 new tokens, 32 / 32 heads, 4000 in all:
+    // 42 against 62, 41 against 71; with 1000 in all 33 against 17, 29 against 19).
+    const int64_t work = tiles(1) * s->n_kv_heads;
+    p.rows = bf16 && s->head_dim >= 64 && rows > 32 && (work > 4 * (int64_t)units() || work * chunks > 64 * (int64_t)units());
+    // 16 rows to a tile; 32 where a fragment's second use is worth more than twice the workgroups: bf16 pages of some length (64 sequences of 3 new tokens,
+    // 4000 in all, 64 / 8 heads x 128: 187 us against 269; 8 bits 142 against 135), and codes widened for fp32 products in a batch that fills the card
+    // (four prompts of 500, 32 / 32 heads x 128: 186 against 224; with 8 / 8 heads, just below the border, the rule's 63 against 57).
+    p.nt = rows <= 16 ? 1 : bf16 ? (!q8 && chunks >= 8 ? 2 : 1) : (q8 && (int64_t)b->n_rows * s->n_heads / 32 >= 2 * units() ? 2 : 1);
+    if (p.rows) p.nt = 8;
+    if (small_tiles) { p.rows = false; p.nt = 1; }
+    p.max_tiles = (int32_t)tiles(p.nt);
+    chunks = walk(16 * p.nt);
+    // Keys are cut into about four items per compute unit (48 sequences of 500 to 8192 tokens: 90 us, with two 100, with eight 97), but not
+    // into runs of fewer than 16 chunks (with 8, five rows of eight sequences of 1031 tokens take 19.1 us, not 16.9), and not where
+    // kv_rows_kernel's tiles are as many by themselves: full ones, or, as long as none is long, ones that a token alone may have.  (64 / 8 heads x 128,
+    // 8 bits, 128 tokens behind 400, 512 rows behind 3488 and a token behind 4000: 164 us, cut 177; behind 8192: 245 and 178; behind 60000: 1493
+    // and 221.  128 tokens behind 400 .. 8192 and the 512 rows: 402 and 428, behind 400 .. 16384 734 and 703)
+    p.min_run = 16;
+    p.target = 4 * units();
+    const int64_t whole = (int64_t)p.max_tiles * s->n_kv_heads, full = (int64_t)b->n_rows * group / (16 * p.nt) * s->n_kv_heads;
+    const int64_t most = (chunks + p.min_run / 2) / p.min_run;      // runs of the longest sequence
+    p.join = most > 1 && !(p.rows && (full >= p.target || (whole >= p.target && chunks < 128)));
+    p.grid = p.join ? whole + p.target : whole;
+    if (p.join && whole * most < p.grid) p.grid = whole * most;
+    if (p.join) {
+        p.o_bytes = ((size_t)p.grid * 16 * p.nt * s->head_dim * 4 + 255) / 256 * 256;
+        p.bytes = p.o_bytes + (size_t)p.grid * 16 * p.nt * 8;
+    }
+    return p;
+}
+
+// causal attention: all that a sequence can have
+auto whole_lengths(const asd_kv_shape* s, const asd_kv_batch* b) {
+    const int64_t chunks = (kv_args(s, b).cap + 63) / 64;
+    return [=](int) { return chunks; };
+}
+
+}  // namespace

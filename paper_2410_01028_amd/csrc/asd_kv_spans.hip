@@ -1,0 +1,139 @@
+// Host side of the attention with a window and of the attention of sequences that begin with the same tokens (asd.h).
+#include "asd_kv_host.h"
+#include "asd_kv_plan.h"
+#include "asd_kv_spans.h"
+
+namespace {
+
+const char* attend_fault(const asd_kv_shape* s, const asd_kv_batch* b, const void* q, int64_t q_stride, const void* out, int64_t out_stride, float scale) {
+    const char* why = shape_fault(s);
+    if (!why) why = batch_fault(s, b);
+    if (!why && (!q || !out)) why = "q and out must be device pointers";
+    if (!why) why = rows_fault(s, q, q_stride, s->n_heads);
+    if (!why) why = rows_fault(s, out, out_stride, s->n_heads);
+    const float c2 = (float)((double)scale * 1.4426950408889634074);      // log2(e)
+    if (!why && !(scale > 0.f && std::isfinite(c2))) why = "scale must be a positive number, scale * log2(e) too";
+    return why;
+}
+const char* window_fault(int32_t window, int32_t sinks) {
+    if (window < 1) return "window must be positive";
+    if (sinks < 0) return "sinks must be 0 or more";
+    return nullptr;
+}
+const char* groups_fault(const asd_kv_groups* g) {
+    if (!g) return "groups is NULL";
+    if (!g->group_start || !g->shared_len) return "group_start and shared_len must be device pointers";
+    if (((uintptr_t)g->group_start | (uintptr_t)g->shared_len) % 4) return "the groups' arrays must be 4-byte aligned";
+    if (g->n_groups < 1 || g->n_groups > 65536) return "n_groups must be in 1..65536";
+    return nullptr;
+}
+int room(const char* what, size_t need, const void* workspace, size_t bytes) {
+    if (need && (!workspace || (uintptr_t)workspace % 256)) return refuse(ASD_E_INVAL, "%s: workspace must be 256-byte aligned", what);
+    if (bytes < need) return refuse(ASD_E_NOMEM, "%s: workspace too small: %zu bytes given, %zu needed", what, bytes, need);
+    return ASD_OK;
+}
+void attend_args(KvAttendArgs* a, const asd_kv_shape* s, const asd_kv_batch* b, const void* q, int64_t q_stride, void* out, int64_t out_stride, float scale) {
+    a->kv = kv_args(s, b);
+    a->q = q; a->out = out; a->q_stride = q_stride; a->out_stride = out_stride;
+    a->c2 = (float)((double)scale * 1.4426950408889634074);
+}
+
+int32_t at_most(int32_t x, int32_t most) { return x < most ? x : most; }
+AttendPlan window_plan(const asd_kv_shape* s, const asd_kv_batch* b, int32_t window, int32_t sinks) {
+    const int64_t cap = kv_args(s, b).cap, chunks = (cap + 63) / 64, group = s->n_heads / s->n_kv_heads;
+    return attend_plan(s, b, [=](int rows) {           // as kv_window_chunks
+        const int64_t most = rows % group ? (rows + group - 2) / group + 1 : rows / group, tokens = most < b->max_new ? most : b->max_new;
+        const int64_t n = ((int64_t)at_most(sinks, (int32_t)cap) + 63) / 64 + (at_most(window, (int32_t)cap) + tokens + 125) / 64;
+        return n < chunks ? n : chunks;
+    }, true);
+}
+// The shared keys, read for all rows of a group, and each sequence's own
+struct SharedPlan {
+    AttendPlan front, own;
+    size_t own_at, bytes;
+};
+SharedPlan shared_plan(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_groups* g) {
+    SharedPlan p;
+    asd_kv_batch rows = *b;                             // a group is one sequence to its shared keys
+    rows.n_seqs = g->n_groups;
+    rows.max_new = b->n_rows;
+    p.front = attend_plan(s, &rows, whole_lengths(s, b), true);
+    p.own = attend_plan(s, b, whole_lengths(s, b), true);
+    // every tile has a place, cut or not
+    for (AttendPlan* x : {&p.front, &p.own}) {
+        x->o_bytes = ((size_t)x->grid * 16 * x->nt * s->head_dim * 4 + 255) / 256 * 256;
+        x->bytes = (x->o_bytes + (size_t)x->grid * 16 * x->nt * 8 + 255) / 256 * 256;
+    }
+    p.own_at = p.front.bytes;
+    p.bytes = p.front.bytes + p.own.bytes;
+    return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t asd_kv_attend_window_workspace(const asd_kv_shape* s, const asd_kv_batch* b, int32_t window, int32_t sinks) {
+    if (shape_fault(s) || batch_fault(s, b) || window_fault(window, sinks)) return 0;
+    return window_plan(s, b, window, sinks).bytes;
+}
+
+int asd_kv_attend_window(const asd_kv_shape* s, const asd_kv_batch* b, int32_t window, int32_t sinks, const void* q, int64_t q_stride, void* out,
+                         int64_t out_stride, float scale, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    static const char* const name = "asd_kv_attend_window";
+    const char* why = attend_fault(s, b, q, q_stride, out, out_stride, scale);
+    if (!why) why = window_fault(window, sinks);
+    if (why) return refuse(ASD_E_INVAL, "%s: %s", name, why);
+    const AttendPlan p = window_plan(s, b, window, sinks);
+    if (const int rc = room(name, p.bytes, workspace, workspace_bytes)) return rc;
+    if (p.grid > MOST_GROUPS) return refuse(ASD_E_INVAL, "%s: the batch is too large", name);
+    KvWindowArgs a{};
+    attend_args(&a, s, b, q, q_stride, out, out_stride, scale);
+    a.o_part = (float*)workspace; a.ml_part = (float*)((char*)workspace + p.o_bytes);
+    a.target = p.target; a.cut = p.join; a.min_run = p.min_run;
+    a.window = at_most(window, a.kv.cap); a.sinks = at_most(sinks, a.kv.cap);
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    const unsigned join_grid = (unsigned)(((int64_t)b->n_rows * a.kv.group / 16 + at_most(b->n_seqs, b->n_rows)) * s->n_kv_heads);
+    by_shape(s, [&](auto t, auto c, auto h) {
+        using T = decltype(t);
+        using C = decltype(c);
+        kv_window_kernel<T, C, h.value, 1><<<(unsigned)p.grid, 256, 0, stream>>>(a);
+        if (p.join) kv_window_join_kernel<T, h.value, 16><<<join_grid, 256, 0, stream>>>(a);
+    });
+    return launched(name);
+}
+
+size_t asd_kv_attend_shared_workspace(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_groups* g) {
+    if (shape_fault(s) || batch_fault(s, b) || groups_fault(g)) return 0;
+    return shared_plan(s, b, g).bytes;
+}
+
+int asd_kv_attend_shared(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_groups* g, const void* q, int64_t q_stride, void* out,
+                         int64_t out_stride, float scale, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    static const char* const name = "asd_kv_attend_shared";
+    const char* why = attend_fault(s, b, q, q_stride, out, out_stride, scale);
+    if (!why) why = groups_fault(g);
+    if (why) return refuse(ASD_E_INVAL, "%s: %s", name, why);
+    const SharedPlan p = shared_plan(s, b, g);
+    if (const int rc = room(name, p.bytes, workspace, workspace_bytes)) return rc;
+    if (p.front.grid > MOST_GROUPS || p.own.grid > MOST_GROUPS) return refuse(ASD_E_INVAL, "%s: the batch is too large", name);
+    KvSharedArgs a{};
+    attend_args(&a, s, b, q, q_stride, out, out_stride, scale);
+    a.group_start = g->group_start; a.shared_len = g->shared_len; a.n_groups = g->n_groups;
+    a.front_o = (float*)workspace; a.front_ml = (float*)((char*)workspace + p.front.o_bytes);
+    a.o_part = (float*)((char*)workspace + p.own_at); a.ml_part = (float*)((char*)workspace + p.own_at + p.own.o_bytes);
+    a.front_target = p.front.target; a.front_cut = p.front.join;
+    a.target = p.own.target; a.cut = p.own.join; a.min_run = p.own.min_run;
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    const unsigned join_grid = (unsigned)(((int64_t)b->n_rows * a.kv.group / 16 + at_most(b->n_seqs, b->n_rows)) * s->n_kv_heads);
+    by_shape(s, [&](auto t, auto c, auto h) {
+        using T = decltype(t);
+        using C = decltype(c);
+        kv_front_kernel<T, C, h.value, 1><<<(unsigned)p.front.grid, 256, 0, stream>>>(a);
+        kv_own_kernel<T, C, h.value, 1><<<(unsigned)p.own.grid, 256, 0, stream>>>(a);
+        kv_shared_join_kernel<T, h.value, 16, 16><<<join_grid, 256, 0, stream>>>(a);
+    });
+    return launched(name);
+}
+
+}  // extern "C"
