@@ -13,6 +13,7 @@ struct KvAttendArgs {
     int32_t target;                 // work items to cut the batch into
     int32_t min_run;                // chunks that are worth a run
     int32_t cut;                    // 0: every tile's keys stay together
+    int32_t tile_rows;              // rows of a tile
 };
 // What the rows of a tile see.  KV_ALL: the keys 0 .. position of their sequence.  KV_WINDOW: of those the last `window` and the first `sinks`.  Sequences that
 // share their first keys: KV_SHARED those (the rows of all sequences of a group, each sees them all), KV_OWN the keys low .. position behind them.

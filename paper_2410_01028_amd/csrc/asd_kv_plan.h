@@ -13,8 +13,8 @@ struct AttendPlan {
     bool join;                     // some sequence's keys may be cut
     size_t o_bytes, bytes;
 };
-// walk(R): the chunks that tiles of R rows walk at most.  small_tiles: 16 rows to a tile, always
-template <class F> AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b, F walk, bool small_tiles = false) {
+// walk(R): the chunks that tiles of R rows walk at most
+template <class F> AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b, F walk) {
     AttendPlan p{};
     const int group = s->n_heads / s->n_kv_heads;
     const int64_t rows = (int64_t)b->max_new * group;
@@ -35,7 +35,6 @@ template <class F> AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_ba
     // (four prompts of 500, 32 / 32 heads x 128: 186 against 224; with 8 / 8 heads, just below the border, the rule's 63 against 57).
     p.nt = rows <= 16 ? 1 : bf16 ? (!q8 && chunks >= 8 ? 2 : 1) : (q8 && (int64_t)b->n_rows * s->n_heads / 32 >= 2 * units() ? 2 : 1);
     if (p.rows) p.nt = 8;
-    if (small_tiles) { p.rows = false; p.nt = 1; }
     p.max_tiles = (int32_t)tiles(p.nt);
     chunks = walk(16 * p.nt);
     // Keys are cut into about four items per compute unit (48 sequences of 500 to 8192 tokens: 90 us, with two 100, with eight 97), but not

@@ -4,12 +4,14 @@
 #pragma once
 #include "asd_kv_attend.h"
 
-// runs of all entries of x, bad ones as they are mended (each has no more items than the plan allows for whatever `chunks` says)
-template <int R, class Lanes, class F> __device__ __forceinline__ int kv_run_all(const KvAttendArgs& a, Lanes x, int lane, F chunks) {
+// tiles of `rows` rows
+__device__ __forceinline__ int kv_tiles_of(const KvArgs& a, const KvSeq& v, int rows) { return (int)(((int64_t)v.n * a.group + rows - 1) / rows); }
+// the run of all entries of x, bad ones as they are mended: no more items than the plan has room for, whatever `chunks` says
+template <class Lanes, class F> __device__ __forceinline__ int kv_run_all(const KvAttendArgs& a, Lanes x, int lane, int rows, F chunks) {
     if (!a.cut) return 1 << 28;
     int64_t t = 0;
     for (int s0 = 0;;) {
-        t += (int64_t)kv_tiles<R / 16>(a.kv, x.v) * chunks(x.v);
+        t += (int64_t)kv_tiles_of(a.kv, x.v, rows) * chunks(x.v);
         s0 += 64;
         if (s0 >= x.entries(a.kv)) break;
         x.load(a.kv, s0, lane, false);
@@ -38,7 +40,7 @@ __device__ __forceinline__ void kv_place_item(KvItem& it, int local, int64_t fir
 
 // ---------------------------------------------------------------- a sliding window and the first tokens
 // The chunks that the tiles of R rows of a sequence walk at most: those of the first tokens, and those from the first row's window on to the last row
-template <int R> __device__ __forceinline__ int kv_window_chunks(const KvWindowArgs& a, const KvSeq& v) {
+__device__ __forceinline__ int kv_window_chunks(const KvWindowArgs& a, const KvSeq& v, int R) {
     const int whole = (v.len + 63) / 64, sink = (a.sinks + 63) / 64, group = a.kv.group;
     if ((int64_t)v.n * group <= R) {                    // one tile: as it is
         const int first = max(v.len - v.n - a.window + 1, 0) / 64;
@@ -54,11 +56,11 @@ template <int R, class F> __device__ __forceinline__ bool kv_window_item(const K
     const bool check = blockIdx.x == 0 && threadIdx.x < 64;
     KvLanes all;
     all.load(a.kv, 0, lane, check);
-    auto chunks = [&](const KvSeq& v) { return kv_window_chunks<R>(a, v); };
-    const int run = kv_run_all<R>(a, all, lane, chunks);
-    if (!kv_find(a.kv, all, blockIdx.x, lane, check, [&](const KvSeq& v) { return kv_tiles<R / 16>(a.kv, v) * kv_splits(chunks(v), run) * n_kv; }, &it.seq, &local, &first, &it.s)) return false;
+    auto chunks = [&](const KvSeq& v) { return kv_window_chunks(a, v, R); };
+    const int run = kv_run_all(a, all, lane, R, chunks);
+    if (!kv_find(a.kv, all, blockIdx.x, lane, check, [&](const KvSeq& v) { return kv_tiles_of(a.kv, v, R) * kv_splits(chunks(v), run) * n_kv; }, &it.seq, &local, &first, &it.s)) return false;
     const int n_splits = kv_splits(chunks(it.s), run);
-    kv_place_item(it, local, first, kv_tiles<R / 16>(a.kv, it.s), n_kv, F::value);
+    kv_place_item(it, local, first, kv_tiles_of(a.kv, it.s, R), n_kv, F::value);
     it.per = kv_per_split(chunks(it.s), n_splits);
     it.whole = n_splits == 1;
     return true;
@@ -69,20 +71,26 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_window_kernel(cons
     KvItem it;
     if (kv_window_item<16 * NT>(a, it, std::false_type{})) kv_few_rows<A, C, H, NT, KV_WINDOW>(a, it, lds);
 }
-template <class A, int H, int R>
+template <class C, int H, int NT, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void kv_window_rows_kernel(const KvWindowArgs a) {
+    __shared__ u32x4 mem[KV_RING<C, H>];
+    KvItem it;
+    if (kv_window_item<16 * NT * NW>(a, it, std::true_type{})) kv_many_rows<C, H, NT, NW, KV_WINDOW>(a, it, mem);
+}
+template <class A, int H>
 __global__ __launch_bounds__(256) void kv_window_join_kernel(const KvWindowArgs a) {
-    const int lane = threadIdx.x & 63, n_kv = a.kv.n_kv, group = a.kv.group;
+    const int lane = threadIdx.x & 63, n_kv = a.kv.n_kv, group = a.kv.group, R = a.tile_rows;
     int seq, local;
     int64_t first;
     KvSeq s;
     KvLanes all;
     all.load(a.kv, 0, lane, false);
-    auto chunks = [&](const KvSeq& v) { return kv_window_chunks<R>(a, v); };
-    const int run = kv_run_all<R>(a, all, lane, chunks);
+    auto chunks = [&](const KvSeq& v) { return kv_window_chunks(a, v, R); };
+    const int run = kv_run_all(a, all, lane, R, chunks);
     // 16 rows of a cut sequence and KV head
-    if (!kv_find(a.kv, all, blockIdx.x, lane, false, [&](const KvSeq& v) { return kv_splits(chunks(v), run) > 1 ? kv_tiles<1>(a.kv, v) * n_kv : 0; }, &seq, &local, &first, &s)) return;
-    const int64_t item0 = kv_items_before(a.kv, all, seq, lane, [&](const KvSeq& v) { return (int64_t)kv_tiles<R / 16>(a.kv, v) * kv_splits(chunks(v), run) * n_kv; });
-    const int n_splits = kv_splits(chunks(s), run), n_tiles = kv_tiles<R / 16>(a.kv, s), kvh = local % n_kv, row0 = local / n_kv * 16;
+    if (!kv_find(a.kv, all, blockIdx.x, lane, false, [&](const KvSeq& v) { return kv_splits(chunks(v), run) > 1 ? kv_tiles_of(a.kv, v, 16) * n_kv : 0; }, &seq, &local, &first, &s)) return;
+    const int64_t item0 = kv_items_before(a.kv, all, seq, lane, [&](const KvSeq& v) { return (int64_t)kv_tiles_of(a.kv, v, R) * kv_splits(chunks(v), run) * n_kv; });
+    const int n_splits = kv_splits(chunks(s), run), n_tiles = kv_tiles_of(a.kv, s, R), kvh = local % n_kv, row0 = local / n_kv * 16;
     const int64_t step = (int64_t)n_tiles * n_kv * R, at = (item0 + (int64_t)(row0 / R) * n_kv + kvh) * R + row0 % R;
     kv_join_rows<A, H>(a, s, kvh, row0, min(s.n * group - row0, 16), n_splits, [&](int i, int r) { const int64_t p = at + r + i * step; return KvPartial{a.o_part + p * H, a.ml_part + p * 2}; });
 }
@@ -94,7 +102,7 @@ __global__ __launch_bounds__(256) void kv_window_join_kernel(const KvWindowArgs 
 struct KvSharedArgs : KvAttendArgs {                    // (o_part .. cut: of the own keys)
     const int32_t *group_start, *shared_len;
     int32_t n_groups;
-    int32_t front_target, front_cut;
+    int32_t front_target, front_cut, front_rows;
     float *front_o, *front_ml;
     __device__ __forceinline__ KvAttendArgs front() const {
         KvAttendArgs f = *this;
@@ -164,11 +172,11 @@ template <int R, class F> __device__ __forceinline__ bool kv_front_item(const Kv
     const bool check = item == 0 && threadIdx.x < 64;
     KvGroupLanes all(a);
     all.load(a.kv, 0, lane, check);
-    const int run = kv_run_all<R>(a.front(), all, lane, kv_front_chunks);
-    auto count = [&](const KvSeq& v) { return v.len > 0 ? kv_tiles<R / 16>(a.kv, v) * kv_splits(kv_front_chunks(v), run) * n_kv : 0; };
+    const int run = kv_run_all(a.front(), all, lane, R, kv_front_chunks);
+    auto count = [&](const KvSeq& v) { return v.len > 0 ? kv_tiles_of(a.kv, v, R) * kv_splits(kv_front_chunks(v), run) * n_kv : 0; };
     if (!kv_find(a.kv, all, item, lane, check, count, &group, &local, &first, &it.s)) return false;
     it.seq = a.group_start[group];
-    kv_place_item(it, local, first, kv_tiles<R / 16>(a.kv, it.s), n_kv, F::value);
+    kv_place_item(it, local, first, kv_tiles_of(a.kv, it.s, R), n_kv, F::value);
     it.per = kv_per_split(kv_front_chunks(it.s), kv_splits(kv_front_chunks(it.s), run));
     it.whole = false;
     return true;
@@ -183,11 +191,11 @@ template <int R, class F> __device__ __forceinline__ bool kv_own_item(const KvSh
     groups.load(a.kv, 0, lane, false);
     KvOwnLanes all(groups);
     all.load(a.kv, 0, lane, check);
-    const int run = kv_run_all<R>(a, all, lane, kv_own_chunks);
-    auto count = [&](const KvSeq& v) { return kv_tiles<R / 16>(a.kv, v) * kv_splits(kv_own_chunks(v), run) * n_kv; };
+    const int run = kv_run_all(a, all, lane, R, kv_own_chunks);
+    auto count = [&](const KvSeq& v) { return kv_tiles_of(a.kv, v, R) * kv_splits(kv_own_chunks(v), run) * n_kv; };
     if (!kv_find(a.kv, all, item, lane, check, count, &it.seq, &local, &first, &it.s)) return false;
     const int n_splits = kv_splits(kv_own_chunks(it.s), run);
-    kv_place_item(it, local, first, kv_tiles<R / 16>(a.kv, it.s), n_kv, F::value);
+    kv_place_item(it, local, first, kv_tiles_of(a.kv, it.s, R), n_kv, F::value);
     it.per = kv_per_split(kv_own_chunks(it.s), n_splits);
     it.whole = n_splits == 1 && it.s.low == 0;
     return true;
@@ -204,10 +212,22 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_own_kernel(const K
     KvItem it;
     if (kv_own_item<16 * NT>(a, blockIdx.x, it, std::false_type{})) kv_few_rows<A, C, H, NT, KV_OWN>(a, it, lds);
 }
-// Puts the parts of every row together: FR and R rows to a tile of the shared and of the own keys
-template <class A, int H, int FR, int R>
+template <class C, int H, int NT, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void kv_front_rows_kernel(const KvSharedArgs a) {
+    __shared__ u32x4 mem[KV_RING<C, H>];
+    KvItem it;
+    if (kv_front_item<16 * NT * NW>(a, blockIdx.x, it, std::false_type{})) kv_many_rows<C, H, NT, NW, KV_SHARED>(a.front(), it, mem);
+}
+template <class C, int H, int NT, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void kv_own_rows_kernel(const KvSharedArgs a) {
+    __shared__ u32x4 mem[KV_RING<C, H>];
+    KvItem it;
+    if (kv_own_item<16 * NT * NW>(a, blockIdx.x, it, std::true_type{})) kv_many_rows<C, H, NT, NW, KV_OWN>(a, it, mem);
+}
+// Puts the parts of every row together
+template <class A, int H>
 __global__ __launch_bounds__(256) void kv_shared_join_kernel(const KvSharedArgs a) {
-    const int lane = threadIdx.x & 63, n_kv = a.kv.n_kv, rows_each = a.kv.group;
+    const int lane = threadIdx.x & 63, n_kv = a.kv.n_kv, rows_each = a.kv.group, R = a.tile_rows, FR = a.front_rows;
     int seq, local;
     int64_t first;
     KvSeq s;
@@ -215,20 +235,20 @@ __global__ __launch_bounds__(256) void kv_shared_join_kernel(const KvSharedArgs 
     groups.load(a.kv, 0, lane, false);
     KvOwnLanes all(groups);
     all.load(a.kv, 0, lane, false);
-    const int run = kv_run_all<R>(a, all, lane, kv_own_chunks);
+    const int run = kv_run_all(a, all, lane, R, kv_own_chunks);
     // 16 rows of a sequence with more than one part and KV head
-    if (!kv_find(a.kv, all, blockIdx.x, lane, false, [&](const KvSeq& v) { return kv_splits(kv_own_chunks(v), run) > 1 || v.low > 0 ? kv_tiles<1>(a.kv, v) * n_kv : 0; },
+    if (!kv_find(a.kv, all, blockIdx.x, lane, false, [&](const KvSeq& v) { return kv_splits(kv_own_chunks(v), run) > 1 || v.low > 0 ? kv_tiles_of(a.kv, v, 16) * n_kv : 0; },
                  &seq, &local, &first, &s)) return;
-    const int64_t item0 = kv_items_before(a.kv, all, seq, lane, [&](const KvSeq& v) { return (int64_t)kv_tiles<R / 16>(a.kv, v) * kv_splits(kv_own_chunks(v), run) * n_kv; });
-    const int n_own = kv_splits(kv_own_chunks(s), run), n_tiles = kv_tiles<R / 16>(a.kv, s), kvh = local % n_kv, row0 = local / n_kv * 16;
+    const int64_t item0 = kv_items_before(a.kv, all, seq, lane, [&](const KvSeq& v) { return (int64_t)kv_tiles_of(a.kv, v, R) * kv_splits(kv_own_chunks(v), run) * n_kv; });
+    const int n_own = kv_splits(kv_own_chunks(s), run), n_tiles = kv_tiles_of(a.kv, s, R), kvh = local % n_kv, row0 = local / n_kv * 16;
     const int64_t step = (int64_t)n_tiles * n_kv * R, at = (item0 + (int64_t)(row0 / R) * n_kv + kvh) * R + row0 % R;
     // the group of the sequence, its first item, and the sequence's first row among the group's
     int n_front = 0, front_tiles = 0;
     int64_t front0 = 0, front_row = 0;
     if (s.low > 0) {
-        const int front_run = kv_run_all<FR>(a.front(), groups, lane, kv_front_chunks);
+        const int front_run = kv_run_all(a.front(), groups, lane, FR, kv_front_chunks);
         for (int g0 = 0;;) {
-            const int64_t c = groups.v.len > 0 ? (int64_t)kv_tiles<FR / 16>(a.kv, groups.v) * kv_splits(kv_front_chunks(groups.v), front_run) * n_kv : 0;
+            const int64_t c = groups.v.len > 0 ? (int64_t)kv_tiles_of(a.kv, groups.v, FR) * kv_splits(kv_front_chunks(groups.v), front_run) * n_kv : 0;
             const unsigned long long mine = __ballot(seq >= groups.f0 && seq < groups.f1);
             const int l = mine ? __ffsll(mine) - 1 : 64;
             int64_t t = lane < l ? c : 0;
@@ -238,7 +258,7 @@ __global__ __launch_bounds__(256) void kv_shared_join_kernel(const KvSharedArgs 
             if (mine) {
                 const KvSeq g{uniform(__shfl(groups.v.r0, l)), uniform(__shfl(groups.v.n, l)), uniform(__shfl(groups.v.len, l))};
                 n_front = kv_splits(kv_front_chunks(g), front_run);
-                front_tiles = kv_tiles<FR / 16>(a.kv, g);
+                front_tiles = kv_tiles_of(a.kv, g, FR);
                 front_row = (int64_t)(s.r0 - g.r0) * rows_each + row0;
                 break;
             }

@@ -45,7 +45,7 @@ AttendPlan window_plan(const asd_kv_shape* s, const asd_kv_batch* b, int32_t win
         const int64_t most = rows % group ? (rows + group - 2) / group + 1 : rows / group, tokens = most < b->max_new ? most : b->max_new;
         const int64_t n = ((int64_t)at_most(sinks, (int32_t)cap) + 63) / 64 + (at_most(window, (int32_t)cap) + tokens + 125) / 64;
         return n < chunks ? n : chunks;
-    }, true);
+    });
 }
 // The shared keys, read for all rows of a group, and each sequence's own
 struct SharedPlan {
@@ -57,8 +57,8 @@ SharedPlan shared_plan(const asd_kv_shape* s, const asd_kv_batch* b, const asd_k
     asd_kv_batch rows = *b;                             // a group is one sequence to its shared keys
     rows.n_seqs = g->n_groups;
     rows.max_new = b->n_rows;
-    p.front = attend_plan(s, &rows, whole_lengths(s, b), true);
-    p.own = attend_plan(s, b, whole_lengths(s, b), true);
+    p.front = attend_plan(s, &rows, whole_lengths(s, b));
+    p.own = attend_plan(s, b, whole_lengths(s, b));
     // every tile has a place, cut or not
     for (AttendPlan* x : {&p.front, &p.own}) {
         x->o_bytes = ((size_t)x->grid * 16 * x->nt * s->head_dim * 4 + 255) / 256 * 256;
@@ -90,15 +90,18 @@ int asd_kv_attend_window(const asd_kv_shape* s, const asd_kv_batch* b, int32_t w
     KvWindowArgs a{};
     attend_args(&a, s, b, q, q_stride, out, out_stride, scale);
     a.o_part = (float*)workspace; a.ml_part = (float*)((char*)workspace + p.o_bytes);
-    a.target = p.target; a.cut = p.join; a.min_run = p.min_run;
+    a.target = p.target; a.cut = p.join; a.min_run = p.min_run; a.tile_rows = 16 * p.nt;
     a.window = at_most(window, a.kv.cap); a.sinks = at_most(sinks, a.kv.cap);
     const hipStream_t stream = (hipStream_t)hip_stream;
     const unsigned join_grid = (unsigned)(((int64_t)b->n_rows * a.kv.group / 16 + at_most(b->n_seqs, b->n_rows)) * s->n_kv_heads);
     by_shape(s, [&](auto t, auto c, auto h) {
         using T = decltype(t);
         using C = decltype(c);
-        kv_window_kernel<T, C, h.value, 1><<<(unsigned)p.grid, 256, 0, stream>>>(a);
-        if (p.join) kv_window_join_kernel<T, h.value, 16><<<join_grid, 256, 0, stream>>>(a);
+        constexpr bool bf16 = T::KE == 8, q8 = sizeof(typename C::elem) == 1;
+        if (p.nt == 1) kv_window_kernel<T, C, h.value, 1><<<(unsigned)p.grid, 256, 0, stream>>>(a);
+        if constexpr (bf16 != q8) { if (p.nt == 2) kv_window_kernel<T, C, h.value, 2><<<(unsigned)p.grid, 256, 0, stream>>>(a); }
+        if constexpr (bf16 && h.value >= 64) { if (p.nt == 8) kv_window_rows_kernel<C, h.value, 2, 4><<<(unsigned)p.grid, 256, 0, stream>>>(a); }
+        if (p.join) kv_window_join_kernel<T, h.value><<<join_grid, 256, 0, stream>>>(a);
     });
     return launched(name);
 }
@@ -122,16 +125,25 @@ int asd_kv_attend_shared(const asd_kv_shape* s, const asd_kv_batch* b, const asd
     a.group_start = g->group_start; a.shared_len = g->shared_len; a.n_groups = g->n_groups;
     a.front_o = (float*)workspace; a.front_ml = (float*)((char*)workspace + p.front.o_bytes);
     a.o_part = (float*)((char*)workspace + p.own_at); a.ml_part = (float*)((char*)workspace + p.own_at + p.own.o_bytes);
-    a.front_target = p.front.target; a.front_cut = p.front.join;
-    a.target = p.own.target; a.cut = p.own.join; a.min_run = p.own.min_run;
+    a.front_target = p.front.target; a.front_cut = p.front.join; a.front_rows = 16 * p.front.nt;
+    a.target = p.own.target; a.cut = p.own.join; a.min_run = p.own.min_run; a.tile_rows = 16 * p.own.nt;
     const hipStream_t stream = (hipStream_t)hip_stream;
     const unsigned join_grid = (unsigned)(((int64_t)b->n_rows * a.kv.group / 16 + at_most(b->n_seqs, b->n_rows)) * s->n_kv_heads);
     by_shape(s, [&](auto t, auto c, auto h) {
         using T = decltype(t);
         using C = decltype(c);
-        kv_front_kernel<T, C, h.value, 1><<<(unsigned)p.front.grid, 256, 0, stream>>>(a);
-        kv_own_kernel<T, C, h.value, 1><<<(unsigned)p.own.grid, 256, 0, stream>>>(a);
-        kv_shared_join_kernel<T, h.value, 16, 16><<<join_grid, 256, 0, stream>>>(a);
+        constexpr bool bf16 = T::KE == 8, q8 = sizeof(typename C::elem) == 1;
+        if (p.front.nt == 1) kv_front_kernel<T, C, h.value, 1><<<(unsigned)p.front.grid, 256, 0, stream>>>(a);
+        if (p.own.nt == 1) kv_own_kernel<T, C, h.value, 1><<<(unsigned)p.own.grid, 256, 0, stream>>>(a);
+        if constexpr (bf16 != q8) {
+            if (p.front.nt == 2) kv_front_kernel<T, C, h.value, 2><<<(unsigned)p.front.grid, 256, 0, stream>>>(a);
+            if (p.own.nt == 2) kv_own_kernel<T, C, h.value, 2><<<(unsigned)p.own.grid, 256, 0, stream>>>(a);
+        }
+        if constexpr (bf16 && h.value >= 64) {
+            if (p.front.nt == 8) kv_front_rows_kernel<C, h.value, 2, 4><<<(unsigned)p.front.grid, 256, 0, stream>>>(a);
+            if (p.own.nt == 8) kv_own_rows_kernel<C, h.value, 2, 4><<<(unsigned)p.own.grid, 256, 0, stream>>>(a);
+        }
+        kv_shared_join_kernel<T, h.value><<<join_grid, 256, 0, stream>>>(a);
     });
     return launched(name);
 }
