@@ -61,6 +61,24 @@ __device__ __forceinline__ KvSeq kv_seq(const KvArgs& a, int s, bool* bad = null
 }
 __device__ __forceinline__ void kv_flag(const KvArgs& a, int bit) { if (a.status) atomicOr(a.status, bit); }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int from_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }      // (the same lane for all)
+// Sums and maxima over a wave's lanes in front of a lane and itself, in the vector unit: within rows of 16, then from row to row.  Exchanges through LDS take
+// several times as long, and every workgroup waits for a few of these before its first request.
+template <int STEP, int ROWS> __device__ __forceinline__ int wave_step(int x) { return __builtin_amdgcn_update_dpp(0, x, STEP, ROWS, 0xf, false); }
+template <class F> __device__ __forceinline__ int wave_upto(int x, F join) {      // join(x, 0) is x
+    x = join(x, wave_step<0x111, 0xf>(x));
+    x = join(x, wave_step<0x112, 0xf>(x));
+    x = join(x, wave_step<0x114, 0xf>(x));
+    x = join(x, wave_step<0x118, 0xf>(x));
+    x = join(x, wave_step<0x142, 0xa>(x));
+    return join(x, wave_step<0x143, 0xc>(x));
+}
+__device__ __forceinline__ int wave_sum_upto(int c) { return wave_upto(c, [](int a, int b) { return a + b; }); }
+__device__ __forceinline__ int wave_max_upto(int c) { return wave_upto(c, [](int a, int b) { return max(a, b); }); }      // (of numbers >= 0)
+__device__ __forceinline__ int64_t wave_sum(int64_t t) {                          // (0 <= t, all of it below 2^48)
+    const int lo = from_lane(wave_sum_upto((int)(t & 0xffffff)), 63), hi = from_lane(wave_sum_upto((int)(t >> 24)), 63);
+    return ((int64_t)hi << 24) + lo;
+}
 
 // A wave's view of the batch, 64 sequences at a time, in order: the first 64 stay in registers.  check: the wave reports arrays out of range.
 // From the first bad sequence on: rows keep the positions that the arrays give them, whatever is cut, and those past cap are left out.  Launches and
@@ -88,17 +106,12 @@ struct KvLanes {
             }
         }
         if (top < 0) top = min(max(a.row_start[s0], 0), a.n_rows);      // (the sequences in front of s0 lie one behind the other)
-        for (int o = 1; o < 64; o <<= 1) { const int t = __shfl_up(end, o); if (lane >= o) end = max(end, t); }
+        end = wave_max_upto(end);
         const int before = __shfl_up(end, 1);
         if (v.r0 < max(top, lane ? before : 0)) v.n = 0;
-        top = max(top, __shfl(end, 63));
+        top = max(top, from_lane(end, 63));
     }
 };
-__device__ __forceinline__ int wave_sum_upto(int c, int lane) {          // inclusive
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const int t = __shfl_up(c, o); if (lane >= o) c += t; }
-    return c;
-}
 // Work items of all sequences one behind the other: count(sequence) items each.  Finds the sequence of `item`, its
 // number within it and the first item of the sequence; each wave counts for itself, so no list has to be built in a launch of its own.
 template <class Lanes, class F>
@@ -112,13 +125,13 @@ __device__ __forceinline__ bool kv_find(const KvArgs& a, Lanes x, int64_t item, 
             *view = KvSeq{uniform(x.v.r0), uniform(x.v.n), uniform(x.v.len), uniform(x.v.low)};
             return item < uniform(c);
         }
-        const int incl = wave_sum_upto(c, lane), total = uniform(__shfl(incl, 63));
+        const int incl = wave_sum_upto(c), total = from_lane(incl, 63);
         if (item < base + total) {
-            const int l = __ffsll((unsigned long long)__ballot(base + incl > item)) - 1;
+            const int l = uniform(__ffsll((unsigned long long)__ballot(base + incl > item)) - 1);
             *seq = uniform(s0 + l);
-            *first = base + uniform(__shfl(incl - c, l));
+            *first = base + from_lane(incl - c, l);
             *local = uniform((int)(item - *first));
-            *view = KvSeq{uniform(__shfl(x.v.r0, l)), uniform(__shfl(x.v.n, l)), uniform(__shfl(x.v.len, l)), uniform(__shfl(x.v.low, l))};
+            *view = KvSeq{from_lane(x.v.r0, l), from_lane(x.v.n, l), from_lane(x.v.len, l), from_lane(x.v.low, l)};
             if (check) for (s0 += 64; s0 < n; s0 += 64) x.load(a, s0, lane, true);
             return true;
         }

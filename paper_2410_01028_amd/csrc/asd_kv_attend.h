@@ -59,7 +59,7 @@ struct KvPages {
 // How a batch is cut.  The rows of a sequence and KV head are its new tokens x the heads of the group; a tile is 16 * NT of
 // them.  With `cut`, all tiles' key ranges are cut into runs of `run` chunks, the same for every sequence, so that about `target` items come out
 // whatever the lengths are: one long conversation among short ones is spread over the card.  (attend_plan in asd_kv.hip says which batches are cut.)
-template <int NT> __device__ __forceinline__ int kv_tiles(const KvArgs& a, const KvSeq& v) { return (int)(((int64_t)v.n * a.group + 16 * NT - 1) / (16 * NT)); }
+template <int NT> __device__ __forceinline__ int kv_tiles(const KvArgs& a, const KvSeq& v) { return (int)(((uint32_t)v.n * a.group + 16 * NT - 1) / (16 * NT)); }      // (n_rows * n_h is below 2^31)
 __device__ __forceinline__ int kv_run_of(const KvAttendArgs& a, int64_t t) {      // t: chunks of all tiles of a KV head
     const int run = (int)fminf((float)(t * a.kv.n_kv) / (float)a.target, 1e8f) + 1;
     return uniform(max(run, a.min_run));
@@ -70,15 +70,11 @@ template <int NT, class F> __device__ __forceinline__ int kv_run(const KvAttendA
     auto units = [&](const KvSeq& v) { return (int64_t)kv_tiles<NT>(a.kv, v) * chunks(v); };
     int64_t t = units(all.v);
     for (int s = lane + 64; s < a.kv.n_seqs; s += 64) t += units(kv_seq(a.kv, s));      // (of bad ones no less than they have: longer runs)
-    if (a.kv.n_seqs > 1) {
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);
-    }
-    return kv_run_of(a, t);
+    return kv_run_of(a, a.kv.n_seqs > 1 ? wave_sum(t) : t);
 }
 // runs of a sequence, of equal length: its chunks / run, to the nearest
-__device__ __forceinline__ int kv_splits(int chunks, int run) { return max(1, (int)(((int64_t)chunks + run / 2) / run)); }
-__device__ __forceinline__ int kv_per_split(int chunks, int n_splits) { return (chunks + n_splits - 1) / n_splits; }
+__device__ __forceinline__ int kv_splits(int chunks, int run) { return max(1, (int)((uint32_t)(chunks + run / 2) / (uint32_t)run)); }
+__device__ __forceinline__ int kv_per_split(int chunks, int n_splits) { return (int)((uint32_t)(chunks + n_splits - 1) / (uint32_t)n_splits); }
 
 // ---- V that is not finite at a key that some rows of a tile do not see: 0 times it is not 0.  In the chunks where that can be (edge
 // chunks: not all rows of the tile see all keys) such values are taken out of the products, and what a row sees of them is added to
@@ -883,10 +879,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(const KvAttendArgs a) {
     for (int s0 = 0; s0 <= seq; s0 += 64) {
         if (s0) all.load(a.kv, s0, lane, false);
         int64_t c = s0 + lane < seq ? (int64_t)kv_tiles<NT>(a.kv, all.v) * kv_splits(chunks(all.v), run) * n_kv : 0;
-        if (seq)
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o);
-        item0 += c;
+        item0 += seq ? wave_sum(c) : 0;
     }
     const int n_splits = kv_splits(chunks(s), run), n_tiles = kv_tiles<NT>(a.kv, s), kvh = local % n_kv, tile = local / n_kv;
     const int row0 = tile * R + blockIdx.y * 16, left = min(s.n * group - row0, 16);

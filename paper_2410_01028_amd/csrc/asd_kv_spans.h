@@ -5,7 +5,7 @@
 #include "asd_kv_attend.h"
 
 // tiles of `rows` rows
-__device__ __forceinline__ int kv_tiles_of(const KvArgs& a, const KvSeq& v, int rows) { return (int)(((int64_t)v.n * a.group + rows - 1) / rows); }
+__device__ __forceinline__ int kv_tiles_of(const KvArgs& a, const KvSeq& v, int rows) { return (int)(((uint32_t)v.n * a.group + rows - 1) / (uint32_t)rows); }
 // the run of all entries of x, bad ones as they are mended: no more items than the plan has room for, whatever `chunks` says
 template <class Lanes, class F> __device__ __forceinline__ int kv_run_all(const KvAttendArgs& a, Lanes x, int lane, int rows, F chunks) {
     if (!a.cut) return 1 << 28;
@@ -16,9 +16,7 @@ template <class Lanes, class F> __device__ __forceinline__ int kv_run_all(const 
         if (s0 >= x.entries(a.kv)) break;
         x.load(a.kv, s0, lane, false);
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);
-    return kv_run_of(a, t);
+    return kv_run_of(a, wave_sum(t));
 }
 // items of the entries in front of entry n
 template <class Lanes, class F> __device__ __forceinline__ int64_t kv_items_before(const KvArgs& a, Lanes x, int n, int lane, F count) {
@@ -27,9 +25,7 @@ template <class Lanes, class F> __device__ __forceinline__ int64_t kv_items_befo
         if (s0) x.load(a, s0, lane, false);
         t += s0 + lane < n ? count(x.v) : 0;
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);
-    return t;
+    return wave_sum(t);
 }
 // item `local` of an entry: its run, tile and KV head.  last_first: the tiles that see most come first
 __device__ __forceinline__ void kv_place_item(KvItem& it, int local, int64_t first, int n_tiles, int n_kv, bool last_first) {
@@ -112,10 +108,9 @@ struct KvSharedArgs : KvAttendArgs {                    // (o_part .. cut: of th
 };
 // the largest of the lanes in front of this one, and of what came before (top, which takes them all in)
 __device__ __forceinline__ int kv_max_before(int x, int& top, int lane) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const int t = __shfl_up(x, o); if (lane >= o) x = max(x, t); }
+    x = wave_max_upto(x);
     const int t = __shfl_up(x, 1), before = lane ? max(top, t) : top;
-    top = max(top, __shfl(x, 63));
+    top = max(top, from_lane(x, 63));
     return before;
 }
 // A wave's view of the groups, 64 at a time: sequences f0 .. f1 - 1, their rows (v.r0, v.n) and the tokens that they share (v.len).  As with the rows: no
@@ -250,13 +245,10 @@ __global__ __launch_bounds__(256) void kv_shared_join_kernel(const KvSharedArgs 
         for (int g0 = 0;;) {
             const int64_t c = groups.v.len > 0 ? (int64_t)kv_tiles_of(a.kv, groups.v, FR) * kv_splits(kv_front_chunks(groups.v), front_run) * n_kv : 0;
             const unsigned long long mine = __ballot(seq >= groups.f0 && seq < groups.f1);
-            const int l = mine ? __ffsll(mine) - 1 : 64;
-            int64_t t = lane < l ? c : 0;
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);
-            front0 += t;
+            const int l = uniform(mine ? __ffsll(mine) - 1 : 64);
+            front0 += wave_sum(lane < l ? c : 0);
             if (mine) {
-                const KvSeq g{uniform(__shfl(groups.v.r0, l)), uniform(__shfl(groups.v.n, l)), uniform(__shfl(groups.v.len, l))};
+                const KvSeq g{from_lane(groups.v.r0, l), from_lane(groups.v.n, l), from_lane(groups.v.len, l)};
                 n_front = kv_splits(kv_front_chunks(g), front_run);
                 front_tiles = kv_tiles_of(a.kv, g, FR);
                 front_row = (int64_t)(s.r0 - g.r0) * rows_each + row0;
