@@ -49,7 +49,7 @@ struct KvArgs {
 
 // One sequence's rows (n of them from row r0 on) and the position behind the last (len; rows in front of position 0 are possible), held inside the
 // buffers whatever the arrays say
-struct KvSeq { int r0, n, len, low = 0; };      // low: first key of its own (behind those that it shares)
+struct KvSeq { int r0, n, len, low = 0, lead = 0; };      // low: first key of its own, behind those that it shares with sequence `lead`
 __device__ __forceinline__ KvSeq kv_seq(const KvArgs& a, int s, bool* bad = nullptr) {
     const int f0 = a.row_start[s], f1 = a.row_start[s + 1], fl = a.kv_len[s];
     KvSeq v;
@@ -122,7 +122,7 @@ __device__ __forceinline__ bool kv_find(const KvArgs& a, Lanes x, int64_t item, 
         const int c = count(x.v);
         if (n == 1) {                                   // (nothing to add up)
             *seq = 0; *first = 0; *local = (int)item;
-            *view = KvSeq{uniform(x.v.r0), uniform(x.v.n), uniform(x.v.len), uniform(x.v.low)};
+            *view = KvSeq{uniform(x.v.r0), uniform(x.v.n), uniform(x.v.len), uniform(x.v.low), uniform(x.v.lead)};
             return item < uniform(c);
         }
         const int incl = wave_sum_upto(c), total = from_lane(incl, 63);
@@ -131,7 +131,7 @@ __device__ __forceinline__ bool kv_find(const KvArgs& a, Lanes x, int64_t item, 
             *seq = uniform(s0 + l);
             *first = base + from_lane(incl - c, l);
             *local = uniform((int)(item - *first));
-            *view = KvSeq{from_lane(x.v.r0, l), from_lane(x.v.n, l), from_lane(x.v.len, l), from_lane(x.v.low, l)};
+            *view = KvSeq{from_lane(x.v.r0, l), from_lane(x.v.n, l), from_lane(x.v.len, l), from_lane(x.v.low, l), from_lane(x.v.lead, l)};
             if (check) for (s0 += 64; s0 < n; s0 += 64) x.load(a, s0, lane, true);
             return true;
         }

@@ -16,26 +16,28 @@ struct KvAttendArgs {
     int32_t tile_rows;              // rows of a tile
 };
 // What the rows of a tile see.  KV_ALL: the keys 0 .. position of their sequence.  KV_WINDOW: of those the last `window` and the first `sinks`.  Sequences that
-// share their first keys: KV_SHARED those (the rows of all sequences of a group, each sees them all), KV_OWN the keys low .. position behind them.
-enum { KV_ALL = 0, KV_WINDOW = 1, KV_SHARED = 2, KV_OWN = 3 };
+// share their first keys: KV_SHARED those (the rows of all sequences of a group, each sees them all), KV_OWN the keys low .. position behind them, KV_BOTH
+// both, the keys 0 .. low - 1 through the table of the group's first sequence.
+enum { KV_ALL = 0, KV_WINDOW = 1, KV_SHARED = 2, KV_OWN = 3, KV_BOTH = 4 };
 struct KvWindowArgs : KvAttendArgs { int32_t window, sinks; };
 // A work item: a tile of a sequence's rows for one KV head against one of the runs that its chunks are cut into
 struct KvItem {
-    int seq;                        // whose page table
+    int seq;                        // whose page table (KV_BOTH: s.lead's for the keys below s.low)
     KvSeq s;
     int kvh, tile, split, per;      // per: chunks of a run
     bool whole;                     // nothing else belongs to the tile's rows: the results go to `out`
     int64_t part;                   // else: its place among the partial sums
     // the same in scalar registers (left to itself the compiler keeps what comes through the structure in 16 vector registers)
     __device__ __forceinline__ KvItem scalar() const {
-        return KvItem{uniform(seq), KvSeq{uniform(s.r0), uniform(s.n), uniform(s.len), uniform(s.low)}, uniform(kvh), uniform(tile), uniform(split), uniform(per), uniform(whole) != 0,
+        return KvItem{uniform(seq), KvSeq{uniform(s.r0), uniform(s.n), uniform(s.len), uniform(s.low), uniform(s.lead)}, uniform(kvh), uniform(tile), uniform(split), uniform(per), uniform(whole) != 0,
                       (int64_t)((uint64_t)(uint32_t)uniform((int)part) | (uint64_t)(uint32_t)uniform((int)(part >> 32)) << 32)};
     }
 };
-// The chunks (units) that a tile walks, numbered without those that no row sees: the first `sinks` of them, then those behind `skip` others
+// The chunks (units) that a tile walks, numbered without those that no row sees: the `first` ones (of the first tokens; of the shared ones), then those behind `skip`
+// others (-1: the chunk in which the shared tokens end comes twice, through either table)
 struct KvSteps {
-    int sinks = 0, skip = 0;
-    __device__ __forceinline__ int at(int i) const { return i >= sinks ? i + skip : i; }
+    int first = 0, skip = 0;
+    __device__ __forceinline__ int at(int i) const { return i >= first ? i + skip : i; }
 };
 template <int SEES, class Args> __device__ __forceinline__ KvSteps kv_steps(const Args& a, int low, int keys) {      // low: first key of the tile's window; keys of a step
     KvSteps t;
@@ -44,6 +46,7 @@ template <int SEES, class Args> __device__ __forceinline__ KvSteps kv_steps(cons
         if (n < first) t = KvSteps{n, first - n};
     }
     if constexpr (SEES == KV_OWN) t.skip = low / keys;
+    if constexpr (SEES == KV_BOTH) { t.first = (low + keys - 1) / keys; t.skip = low / keys - t.first; }
     return t;
 }
 // The pages of 64 entries of a table from `base` on, in a wave's lanes (-1: no page of the pool)
@@ -155,13 +158,14 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
     const int from = SEES == KV_SHARED ? s.len - 1 : base + tile * NT * 16 / a.kv.group;
     int window = 0, sinks = 0, low = 0, low_last = 0;
     if constexpr (SEES == KV_WINDOW) { window = a.window; sinks = a.sinks; low = from - window + 1; low_last = last - window + 1; }
-    if constexpr (SEES == KV_OWN) low = low_last = s.low;
+    if constexpr (SEES >= KV_OWN) low = low_last = s.low;
     const KvSteps steps = kv_steps<SEES>(a, low, UK);
     const int u_begin = split * per * UPC, u_end = min((last + UK) / UK - steps.skip, (split + 1) * per * UPC);      // (nothing to do where last is negative)
-    auto hidden = [&](int key, int t) {
+    auto hidden = [&](int key, int t, bool first) {      // first: of the first steps
         bool h = key > pos[t];
         if constexpr (SEES == KV_WINDOW) h = h || (key <= pos[t] - window && key >= sinks);
         if constexpr (SEES == KV_OWN) h = h || key < low;
+        if constexpr (SEES == KV_BOTH) h = h || (key < low) != first;
         return h;
     };
 
@@ -191,13 +195,15 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
             for (int ks = 0; ks < KSU; ++ks) f.v[ht][ks] = __builtin_nontemporal_load((const u32x4*)(p + ((ht * KST + ks) * 64 + lane) * 16));
         if constexpr (L::Q8) f.ve = *(const u32x4*)(p + L::K_BYTES + 64 + 16 * g);
     };
-    // The pages lie in the wave's lanes, those of the first keys apart from the others: a look-up in memory per unit would wait
+    // The pages lie in the wave's lanes, those of the first steps apart from the others: a look-up in memory per unit would wait
     // for every fragment asked for before it
     const int cpp = a.kv.page_tokens / 64;
-    KvPages pages, sink_pages;
-    if constexpr (SEES == KV_WINDOW) if (u_begin < steps.sinks) {
-        pages.load(a.kv, seq, (steps.sinks + steps.skip) / UPC / cpp, lane);
-        sink_pages.load(a.kv, seq, 0, lane);
+    constexpr bool TWO = SEES == KV_WINDOW || SEES == KV_BOTH;
+    const int first_seq = SEES == KV_BOTH ? s.lead : seq;
+    KvPages pages, first_pages;
+    if constexpr (TWO) if (u_begin < steps.first) {
+        if (u_end > steps.first) pages.load(a.kv, seq, (steps.first + steps.skip) / UPC / cpp, lane);
+        first_pages.load(a.kv, first_seq, u_begin / UPC / cpp, lane);
     }
     // the first unit from u on that has a page, and where it is; one without counts as hidden
     const char *at_k = nullptr, *at_v = nullptr;
@@ -205,9 +211,9 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
         for (; u < u_end; u += 4) {
             const int r = steps.at(u), c = r / UPC, i = c / cpp;
             int page;
-            if (SEES == KV_WINDOW && u < steps.sinks) {
-                if (i - sink_pages.base >= 64) sink_pages.load(a.kv, seq, i, lane);
-                page = sink_pages.at(i);
+            if (TWO && u < steps.first) {
+                if (i - first_pages.base >= 64) first_pages.load(a.kv, first_seq, i, lane);
+                page = first_pages.at(i);
             } else {
                 if (i - pages.base >= 64) pages.load(a.kv, seq, i, lane);
                 page = pages.at(i);
@@ -221,7 +227,9 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
         return u;
     };
     bool odd = false;
-    auto work = [&](Unit& f, const int key0, auto after_scores) {
+    auto work = [&](Unit& f, const int u, auto after_scores) {
+        const int key0 = steps.at(u) * UK;
+        const bool first = TWO && u < steps.first;
         f32x4 sc[NT][KT];
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
@@ -240,7 +248,9 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
         after_scores();
         __builtin_amdgcn_sched_barrier(0);
         // some rows do not see all of the unit; some of its keys are behind the sequence's end
-        const bool edge = key0 + UK - 1 > from || (SEES >= KV_WINDOW && SEES != KV_SHARED && key0 < low_last && key0 + UK > sinks);
+        bool edge = key0 + UK - 1 > from;
+        if constexpr (SEES == KV_WINDOW || SEES == KV_OWN) edge = edge || (key0 < low_last && key0 + UK > sinks);
+        if constexpr (SEES == KV_BOTH) edge = edge || (first ? key0 + UK > low : key0 < low);
         float vs[KT][4];
         if constexpr (L::Q8)
 #pragma unroll
@@ -255,7 +265,7 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
                 for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        if (hidden(key0 + score_key<C>(kt, 4 * g + j), t)) sc[t][kt][j] = -INFINITY;
+                        if (hidden(key0 + score_key<C>(kt, 4 * g + j), t, first)) sc[t][kt][j] = -INFINITY;
             }
             float cm = sc[t][0][0];
 #pragma unroll
@@ -280,7 +290,7 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
                     if constexpr (L::Q8) {
                         pr[kt][j] = e * vs[kt][j];
                         // (an unwritten scale may be anything)
-                        if (edge && hidden(key0 + score_key<C>(kt, 4 * g + j), t)) pr[kt][j] = 0.f;
+                        if (edge && hidden(key0 + score_key<C>(kt, 4 * g + j), t, first)) pr[kt][j] = 0.f;
                     }
                 }
             // the probabilities as operands: lane group g holds, in order, the keys of its V^T pieces
@@ -303,6 +313,7 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
             // what is behind the end, or no row sees, is cleared: 0 times whatever lies there must be 0
             int cut = 0, n_keys = s.len - key0;
             if constexpr (SEES == KV_OWN) cut = low - key0;
+            if constexpr (SEES == KV_BOTH) { if (first) n_keys = low - key0; else cut = low - key0; }
             if constexpr (SEES == KV_WINDOW) {
                 if (key0 >= sinks) cut = low - key0;
                 if (key0 + UK <= low) n_keys = min(n_keys, sinks - key0);
@@ -313,7 +324,7 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
                         uint32_t keep = kv_kept<C>(n_keys, ks, g, x);
-                        if constexpr (SEES == KV_OWN || SEES == KV_WINDOW) keep &= ~kv_kept<C>(cut, ks, g, x);
+                        if constexpr (SEES != KV_ALL && SEES != KV_SHARED) keep &= ~kv_kept<C>(cut, ks, g, x);
 #pragma unroll
                         for (int ht = 0; ht < HT; ++ht) f.v[ht][ks][x] &= keep;
                     }
@@ -355,7 +366,7 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
             const int un = next(unit + 4);
             if (un < u_end) ask(then);
             __builtin_amdgcn_sched_barrier(0);
-            work(now, steps.at(unit) * UK, [] {});
+            work(now, unit, [] {});
             unit = un;
         };
         if (unit < u_end) ask(f0);
@@ -369,7 +380,7 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
         if (unit < u_end) { ask_k(f, at_k); ask_v(f, at_v); }
         while (unit < u_end) {
             const int un = next(unit + 4);
-            work(f, steps.at(unit) * UK, [&] { if (un < u_end) ask_k(f, at_k); });
+            work(f, unit, [&] { if (un < u_end) ask_k(f, at_k); });
             __builtin_amdgcn_sched_barrier(0);
             if (un < u_end) ask_v(f, at_v);
             __builtin_amdgcn_sched_barrier(0);
@@ -407,10 +418,11 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
             if (sh.odd) {                                // what the row sees among the item's keys, but for units that all rows see
                 const int end = SEES == KV_SHARED ? from : base + token, row_low = SEES == KV_WINDOW ? end - window + 1 : low;
                 const int main0 = (max(low_last, 0) + UK - 1) / UK * UK, main1 = (from + 1) / UK * UK;
-                const int first_key = steps.at(max(u_begin, steps.sinks)) * UK, last_key = min(end, (u_end + steps.skip) * UK - 1);
+                const int first_key = steps.at(max(u_begin, steps.first)) * UK, last_key = min(end, (u_end + steps.skip) * UK - 1);
                 for (int j = 0; j < 4; ++j) {
                     v[j] += kv_odd_sum<C, H>(a.kv, seq, kvh, first_key, last_key, d + j, row_low, sinks, main0, main1);
-                    if (SEES == KV_WINDOW && u_begin < steps.sinks) v[j] += kv_odd_sum<C, H>(a.kv, seq, kvh, u_begin * UK, min(min(end, sinks - 1), u_end * UK - 1), d + j);
+                    if (TWO && u_begin < steps.first)
+                        v[j] += kv_odd_sum<C, H>(a.kv, first_seq, kvh, u_begin * UK, min(min(end, (SEES == KV_BOTH ? low : sinks) - 1), u_end * UK - 1), d + j, 0, 0, 0, SEES == KV_BOTH ? low / UK * UK : 0);
                 }
             }
             if (it.whole) {
@@ -486,17 +498,19 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
         window = a.window; sinks = a.sinks;
         low = from - window + 1; low_last = last - window + 1; my_low = my_from - window + 1; my_low_last = my_last - window + 1;
     }
-    if constexpr (SEES == KV_OWN) low = low_last = my_low = my_low_last = s.low;
-    auto hidden = [&](int key, int t) {
+    if constexpr (SEES >= KV_OWN) low = low_last = my_low = my_low_last = s.low;
+    auto hidden = [&](int key, int t, bool first) {      // first: of the first steps
         bool h = key > pos[t];
         if constexpr (SEES == KV_WINDOW) h = h || (key <= pos[t] - window && key >= sinks);
         if constexpr (SEES == KV_OWN) h = h || key < low;
+        if constexpr (SEES == KV_BOTH) h = h || (key < low) != first;
         return h;
     };
     // Steps of one chunk: those of the workgroup's run, those that all its rows see whole
     const KvSteps steps = kv_steps<SEES>(a, low, 64);
     const int c0 = it.split * per, c_end = min((last + 64) / 64 - steps.skip, c0 + per);
     const int main0 = max((max(low_last, 0) + 63) / 64 - steps.skip, c0), main1 = min(c_end, (from + 1) / 64 - steps.skip);
+    const int first_main = SEES == KV_BOTH ? min(low / 64, c_end) : 0;                    // ... and the first ones (of the shared keys)
     f32x4 o[NT][HT];
     float mx[NT], l[NT];
 #pragma unroll
@@ -507,12 +521,14 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
     }
     bool odd = false;                                    // this lane has taken a value out of V
     if (c_end > c0) {
-        // The page of the chunk asked for next: the table's entries lie in the wave's lanes, those of the first keys apart from the others
+        // The page of the chunk asked for next: the table's entries lie in the wave's lanes, those of the first steps apart from the others
+        constexpr bool TWO = SEES == KV_WINDOW || SEES == KV_BOTH;
         const int cpp = a.kv.page_tokens / 64, r0 = steps.at(c0);
         int page_i = r0 / cpp, in_page = r0 % cpp;
         KvPages pages, later;
-        pages.load(a.kv, seq, page_i, lane);
-        if constexpr (SEES == KV_WINDOW) if (c0 < steps.sinks) later.load(a.kv, seq, (steps.sinks + steps.skip) / cpp, lane);
+        const int first_seq = SEES == KV_BOTH ? s.lead : seq;
+        pages.load(a.kv, TWO && c0 < steps.first ? first_seq : seq, page_i, lane);
+        if constexpr (TWO) if (c0 < steps.first && c_end > steps.first) later.load(a.kv, seq, (steps.first + steps.skip) / cpp, lane);
         uint32_t gone = 0;                               // bit c % 32: the chunk of step c has no page
         bool lost = false;
         int asked = c0;                                  // chunk whose K is asked for next
@@ -533,8 +549,8 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
                 gone = page >= 0 ? gone & ~(1u << (asked & 31)) : gone | 1u << (asked & 31);
                 lost |= page < 0;
                 if (++in_page == cpp) { in_page = 0; ++page_i; }
-                if constexpr (SEES == KV_WINDOW) if (asked + 1 == steps.sinks) {
-                    page_i = (steps.sinks + steps.skip) / cpp; in_page = (steps.sinks + steps.skip) % cpp;
+                if constexpr (TWO) if (asked + 1 == steps.first) {
+                    page_i = (steps.first + steps.skip) / cpp; in_page = (steps.first + steps.skip) % cpp;
                     pages = later;
                 }
             }
@@ -553,7 +569,7 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
         ask_k(); ask_v(src, n_bytes); ask_k();           // K, V^T of the first chunk, K of the next
         auto turn = [&]() {
             if (page_i - pages.base >= 62) {             // (once in 62 pages: the ring runs dry for a moment)
-                pages.load(a.kv, seq, page_i, lane);
+                pages.load(a.kv, TWO && asked < steps.first ? first_seq : seq, page_i, lane);
                 wait_vm<0, false>();
             }
             wait_vm<LH + X, true>();                     // the K of the next chunk may still be on its way
@@ -562,6 +578,9 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
             __builtin_amdgcn_sched_barrier(0);
         };
         auto ask = [&]() { ask_v(src, n_bytes); ask_k(); };      // V^T of the next chunk, K of the one behind it
+        // the written keys that belong to step c: first_key .. last_key - 1
+        auto first_key = [&](int c) { return SEES == KV_OWN || (SEES == KV_BOTH && c >= steps.first) ? low : 0; };
+        auto last_key = [&](int c) { return SEES == KV_BOTH && c < steps.first ? low : s.len; };
         // step c, chunk r: one that this wave has products for; edge: some of its rows do not see all of it
         auto work = [&](const int c, const int r, auto is_edge) {
             constexpr bool edge = decltype(is_edge)::value;
@@ -610,13 +629,13 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
                     for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
-                            if (hidden(r * 64 + score_key<C>(kt, 4 * g + j), t)) sc[t][kt][j] = -INFINITY;
+                            if (hidden(r * 64 + score_key<C>(kt, 4 * g + j), t, TWO && c < steps.first)) sc[t][kt][j] = -INFINITY;
                 if constexpr (L::Q8) {                   // (an unwritten scale may be anything)
-                    const int n_keys = s.len - r * 64, cut = SEES == KV_OWN ? low - r * 64 : 0;
+                    const int n_keys = last_key(c) - r * 64, cut = first_key(c) - r * 64;
 #pragma unroll
                     for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) if (score_key<C>(kt, 4 * g + j) >= n_keys || (SEES == KV_OWN && score_key<C>(kt, 4 * g + j) < cut)) vs[kt][j] = 0.f;
+                        for (int j = 0; j < 4; ++j) if (score_key<C>(kt, 4 * g + j) >= n_keys || (SEES >= KV_OWN && score_key<C>(kt, 4 * g + j) < cut)) vs[kt][j] = 0.f;
                 }
             }
             u32x4 pf[NT][PS];
@@ -675,8 +694,8 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
             __builtin_amdgcn_s_setprio(0);
         };
         // A chunk with an edge: keys behind the end and values that are not finite leave V^T (see kv_clean); each wave cleans what it has asked for
-        auto clean = [&](const int r) {
-            const int n_keys = s.len - r * 64, cut = SEES == KV_OWN ? low - r * 64 : 0;
+        auto clean = [&](const int c, const int r) {
+            const int n_keys = last_key(c) - r * 64, cut = first_key(c) - r * 64;
             uint32_t hit = 0;
 #pragma unroll 1
             for (int q = 0; q < LH; ++q) {
@@ -686,7 +705,7 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     f[x] &= kv_kept<C>(n_keys, j % KST, g, x);
-                    if constexpr (SEES == KV_OWN) f[x] &= ~kv_kept<C>(cut, j % KST, g, x);
+                    if constexpr (SEES >= KV_OWN) f[x] &= ~kv_kept<C>(cut, j % KST, g, x);
                     hit |= kv_odd<C>(f[x]);
                     f[x] = kv_clean<C>(f[x]);
                 }
@@ -705,15 +724,15 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
         // Chunks that all rows of the workgroup see run in a loop of their own, without masks; those with an edge, or without a page, one by one
         int c = c0;
         for (;;) {
-            for (; c >= main0 && c < main1 && gone == 0; ++c) {
+            for (const int stop = c < first_main ? first_main : c >= main0 ? main1 : c; c < stop && gone == 0; ++c) {
                 turn();
-                work(c, c + steps.skip, std::false_type{});
+                work(c, steps.at(c), std::false_type{});
                 done();
             }
             if (c >= c_end) break;
             turn();
             const int r = steps.at(c);
-            if (c < main0 || c >= main1) clean(r);       // (beside a missing page: what all rows see goes through the products)
+            if (c >= first_main && (c < main0 || c >= main1)) clean(c, r);       // (beside a missing page: what all rows see goes through the products)
             bool mine = r * 64 <= my_last;
             if constexpr (SEES == KV_WINDOW) mine = mine && (r * 64 + 63 >= my_low || r * 64 < sinks);
             if (mine && !((gone >> (c & 31)) & 1u)) work(c, r, std::true_type{}); else ask();
@@ -753,9 +772,10 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
         if (odd) {                                       // (each lane changes what it has stored)
             for (int d = 0; d < H / 4; ++d) {
                 const int dim = d / 4 * 16 + 4 * g + d % 4;
-                float x = kv_odd_sum<C, H>(a.kv, seq, kvh, steps.at(max(c0, steps.sinks)) * 64, min(pos[t], (c_end + steps.skip) * 64 - 1), dim,
+                float x = kv_odd_sum<C, H>(a.kv, seq, kvh, steps.at(max(c0, steps.first)) * 64, min(pos[t], (c_end + steps.skip) * 64 - 1), dim,
                                            SEES == KV_WINDOW ? pos[t] - window + 1 : low, sinks, (main0 + steps.skip) * 64, (main1 + steps.skip) * 64);
-                if (SEES == KV_WINDOW && c0 < steps.sinks) x += kv_odd_sum<C, H>(a.kv, seq, kvh, c0 * 64, min(min(pos[t], sinks - 1), c_end * 64 - 1), dim);
+                if ((SEES == KV_WINDOW || SEES == KV_BOTH) && c0 < steps.first)
+                    x += kv_odd_sum<C, H>(a.kv, SEES == KV_BOTH ? s.lead : seq, kvh, c0 * 64, min(min(pos[t], (SEES == KV_BOTH ? low : sinks) - 1), c_end * 64 - 1), dim, 0, 0, 0, first_main * 64);
                 if (finite(x)) continue;                 // (nothing of its own row's to add)
                 if (it.whole) out[dim] = BF16::from_f32(BF16::to_f32(out[dim]) + x); else a.o_part[at * H + dim] += x;
             }

@@ -14,7 +14,7 @@ struct AttendPlan {
     size_t o_bytes, bytes;
 };
 // walk(R): the chunks that tiles of R rows walk at most
-template <class F> AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b, F walk) {
+template <class F> AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b, F walk, bool large_tiles = true) {
     AttendPlan p{};
     const int group = s->n_heads / s->n_kv_heads;
     const int64_t rows = (int64_t)b->max_new * group;
@@ -34,7 +34,9 @@ template <class F> AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_ba
     // 4000 in all, 64 / 8 heads x 128: 187 us against 269; 8 bits 142 against 135), and codes widened for fp32 products in a batch that fills the card
     // (four prompts of 500, 32 / 32 heads x 128: 186 against 224; with 8 / 8 heads, just below the border, the rule's 63 against 57).
     p.nt = rows <= 16 ? 1 : bf16 ? (!q8 && chunks >= 8 ? 2 : 1) : (q8 && (int64_t)b->n_rows * s->n_heads / 32 >= 2 * units() ? 2 : 1);
+    if (!large_tiles) p.rows = false;
     if (p.rows) p.nt = 8;
+    if (!large_tiles) p.nt = 1;
     p.max_tiles = (int32_t)tiles(p.nt);
     chunks = walk(16 * p.nt);
     // Keys are cut into about four items per compute unit (48 sequences of 500 to 8192 tokens: 90 us, with two 100, with eight 97), but not

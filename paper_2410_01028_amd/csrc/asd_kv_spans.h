@@ -34,6 +34,49 @@ __device__ __forceinline__ void kv_place_item(KvItem& it, int local, int64_t fir
     it.part = first + (int64_t)(it.split * n_tiles + it.tile) * n_kv + it.kvh;
 }
 
+// What the join of 16 rows for a KV head has to know, written by the work item that has their first run: the join itself then looks nothing up but this (with the
+// search for its rows and runs, as kv_join_kernel has it, 64 sequences in two parts took 20 us).
+struct KvNote {
+    int32_t r0, row0, left, kvh;                        // the sequence's first row, the first of these rows x heads, how many
+    int32_t n_own, own, own_step, own_row;              // runs; the item of the first, to the next; the first row's place in it
+    int32_t n_front, front, front_step, front_row;      // the same of the shared keys; the first row's place among the group's
+};
+struct KvNotes {
+    int32_t n, pad[15];
+    KvNote at[1];
+};
+template <class A, int H>
+__global__ __launch_bounds__(256) void kv_parts_kernel(const KvAttendArgs a, const KvNotes* notes, const float* front_o, const float* front_ml, int front_rows) {
+    const int n = notes->n;
+    const KvNote k = notes->at[blockIdx.x];             // (the notes have room for every block)
+    if ((int)blockIdx.x >= n) return;
+    const KvSeq s{uniform(k.r0), 0, 0};
+    kv_join_rows<A, H>(a, s, uniform(k.kvh), uniform(k.row0), uniform(k.left), uniform(k.n_own + k.n_front), [&](int i, int r) {
+        if (i < k.n_own) {
+            const int64_t p = (int64_t)(k.own + i * k.own_step) * a.tile_rows + k.own_row + r;
+            return KvPartial{a.o_part + p * H, a.ml_part + p * 2};
+        }
+        const uint32_t row = (uint32_t)(k.front_row + r), tile = row / (uint32_t)front_rows;
+        const int64_t p = (int64_t)(k.front + (i - k.n_own) * k.front_step + (int)tile * a.kv.n_kv) * front_rows + row % (uint32_t)front_rows;
+        return KvPartial{front_o + p * H, front_ml + p * 2};
+    });
+}
+// The notes on a tile's rows, by one wave of its first run; k: what concerns all of them.  before: 16-row blocks of the sequences in front that are joined
+__device__ __forceinline__ void kv_write_notes(KvNotes* notes, const KvAttendArgs& a, const KvItem& it, int n_tiles, int64_t before, int lane, KvNote k) {
+    const int row = it.tile * a.tile_rows + lane * 16, left = it.s.n * a.kv.group - row;
+    if (lane * 16 >= a.tile_rows || left <= 0) return;
+    k.r0 = it.s.r0; k.row0 = row; k.left = min(left, 16); k.kvh = it.kvh;
+    k.own = (int)it.part; k.own_step = n_tiles * a.kv.n_kv; k.own_row = lane * 16;
+    k.front_row += row;
+    notes->at[(before + row / 16) * a.kv.n_kv + it.kvh] = k;
+}
+
+// how many there are
+template <class Lanes, class F> __device__ __forceinline__ void kv_count_notes(KvNotes* notes, const KvArgs& a, const Lanes& all, int lane, F joined) {
+    const int64_t n = kv_items_before(a, all, a.n_seqs, lane, joined);
+    if (lane == 0) notes->n = (int)(n * a.n_kv);
+}
+
 // ---------------------------------------------------------------- a sliding window and the first tokens
 // The chunks that the tiles of R rows of a sequence walk at most: those of the first tokens, and those from the first row's window on to the last row
 __device__ __forceinline__ int kv_window_chunks(const KvWindowArgs& a, const KvSeq& v, int R) {
@@ -45,7 +88,7 @@ __device__ __forceinline__ int kv_window_chunks(const KvWindowArgs& a, const KvS
     const int tokens = min(v.n, R % group ? (R + group - 2) / group + 1 : R / group);
     return min(whole, sink + (a.window + tokens + 125) / 64);
 }
-template <int R, class F> __device__ __forceinline__ bool kv_window_item(const KvWindowArgs& a, KvItem& it, F) {
+template <int R, class F> __device__ __forceinline__ bool kv_window_item(const KvWindowArgs& a, KvNotes* notes, KvItem& it, F) {
     const int lane = threadIdx.x & 63, n_kv = a.kv.n_kv;
     int local;
     int64_t first;
@@ -54,43 +97,28 @@ template <int R, class F> __device__ __forceinline__ bool kv_window_item(const K
     all.load(a.kv, 0, lane, check);
     auto chunks = [&](const KvSeq& v) { return kv_window_chunks(a, v, R); };
     const int run = kv_run_all(a, all, lane, R, chunks);
+    auto joined = [&](const KvSeq& v) { return kv_splits(chunks(v), run) > 1 ? kv_tiles_of(a.kv, v, 16) : 0; };
+    if (check && a.cut) kv_count_notes(notes, a.kv, all, lane, joined);
     if (!kv_find(a.kv, all, blockIdx.x, lane, check, [&](const KvSeq& v) { return kv_tiles_of(a.kv, v, R) * kv_splits(chunks(v), run) * n_kv; }, &it.seq, &local, &first, &it.s)) return false;
-    const int n_splits = kv_splits(chunks(it.s), run);
-    kv_place_item(it, local, first, kv_tiles_of(a.kv, it.s, R), n_kv, F::value);
+    const int n_splits = kv_splits(chunks(it.s), run), n_tiles = kv_tiles_of(a.kv, it.s, R);
+    kv_place_item(it, local, first, n_tiles, n_kv, F::value);
     it.per = kv_per_split(chunks(it.s), n_splits);
     it.whole = n_splits == 1;
+    if (!it.whole && it.split == 0 && threadIdx.x >= 192) kv_write_notes(notes, a, it, n_tiles, kv_items_before(a.kv, all, it.seq, lane, joined), lane, KvNote{.n_own = n_splits});
     return true;
 }
 template <class A, class C, int H, int NT>
-__global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_window_kernel(const KvWindowArgs a) {
+__global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_window_kernel(const KvWindowArgs a, KvNotes* notes) {
     __shared__ KvFewLds<H> lds;
     KvItem it;
-    if (kv_window_item<16 * NT>(a, it, std::false_type{})) kv_few_rows<A, C, H, NT, KV_WINDOW>(a, it, lds);
+    if (kv_window_item<16 * NT>(a, notes, it, std::false_type{})) kv_few_rows<A, C, H, NT, KV_WINDOW>(a, it, lds);
 }
 template <class C, int H, int NT, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void kv_window_rows_kernel(const KvWindowArgs a) {
+__global__ __launch_bounds__(64 * NW, 2) void kv_window_rows_kernel(const KvWindowArgs a, KvNotes* notes) {
     __shared__ u32x4 mem[KV_RING<C, H>];
     KvItem it;
-    if (kv_window_item<16 * NT * NW>(a, it, std::true_type{})) kv_many_rows<C, H, NT, NW, KV_WINDOW>(a, it, mem);
+    if (kv_window_item<16 * NT * NW>(a, notes, it, std::true_type{})) kv_many_rows<C, H, NT, NW, KV_WINDOW>(a, it, mem);
 }
-template <class A, int H>
-__global__ __launch_bounds__(256) void kv_window_join_kernel(const KvWindowArgs a) {
-    const int lane = threadIdx.x & 63, n_kv = a.kv.n_kv, group = a.kv.group, R = a.tile_rows;
-    int seq, local;
-    int64_t first;
-    KvSeq s;
-    KvLanes all;
-    all.load(a.kv, 0, lane, false);
-    auto chunks = [&](const KvSeq& v) { return kv_window_chunks(a, v, R); };
-    const int run = kv_run_all(a, all, lane, R, chunks);
-    // 16 rows of a cut sequence and KV head
-    if (!kv_find(a.kv, all, blockIdx.x, lane, false, [&](const KvSeq& v) { return kv_splits(chunks(v), run) > 1 ? kv_tiles_of(a.kv, v, 16) * n_kv : 0; }, &seq, &local, &first, &s)) return;
-    const int64_t item0 = kv_items_before(a.kv, all, seq, lane, [&](const KvSeq& v) { return (int64_t)kv_tiles_of(a.kv, v, R) * kv_splits(chunks(v), run) * n_kv; });
-    const int n_splits = kv_splits(chunks(s), run), n_tiles = kv_tiles_of(a.kv, s, R), kvh = local % n_kv, row0 = local / n_kv * 16;
-    const int64_t step = (int64_t)n_tiles * n_kv * R, at = (item0 + (int64_t)(row0 / R) * n_kv + kvh) * R + row0 % R;
-    kv_join_rows<A, H>(a, s, kvh, row0, min(s.n * group - row0, 16), n_splits, [&](int i, int r) { const int64_t p = at + r + i * step; return KvPartial{a.o_part + p * H, a.ml_part + p * 2}; });
-}
-
 // ---------------------------------------------------------------- sequences that begin with the same tokens
 // The keys that a group shares are read once for the rows of all its sequences: these lie one behind the other, so that a group is to its shared keys what a
 // sequence is to its own, all rows seeing all of them.  The keys behind them are each sequence's own.  Every row's sums come in two
@@ -98,7 +126,7 @@ __global__ __launch_bounds__(256) void kv_window_join_kernel(const KvWindowArgs 
 struct KvSharedArgs : KvAttendArgs {                    // (o_part .. cut: of the own keys)
     const int32_t *group_start, *shared_len;
     int32_t n_groups;
-    int32_t front_target, front_cut, front_rows;
+    int32_t front_target, front_cut, front_rows, front_grid;
     float *front_o, *front_ml;
     __device__ __forceinline__ KvAttendArgs front() const {
         KvAttendArgs f = *this;
@@ -119,21 +147,36 @@ struct KvGroupLanes {
     const KvSharedArgs* a;
     KvSeq v;
     int f0, f1, top_f = 0, top_h = 0;
+    int s0, s1, len;                                    // what the arrays say
     __device__ __forceinline__ KvGroupLanes(const KvSharedArgs& args) : a(&args) {}
     __device__ __forceinline__ int entries(const KvArgs&) const { return a->n_groups; }
-    __device__ __forceinline__ void load(const KvArgs& kv, int g0, int lane, bool check) {
-        const int g = g0 + lane;
-        const bool on = g < a->n_groups;
-        const int s0 = on ? a->group_start[g] : 0, s1 = on ? a->group_start[g + 1] : 0, len = on ? a->shared_len[g] : 0;
-        const int before = kv_max_before(min(max(s1, 0), kv.n_seqs), top_f, lane);
+    __device__ __forceinline__ void ask(int g0, int lane) {
+        const int g = min(g0 + lane, a->n_groups - 1);
+        s0 = a->group_start[g]; s1 = a->group_start[g + 1]; len = a->shared_len[g];
+    }
+    // begin(s), of all lanes at once: row_start[s]
+    template <class F> __device__ __forceinline__ void take(const KvArgs& kv, int g0, int lane, bool check, F begin) {
+        const bool on = g0 + lane < a->n_groups;
+        const int before = kv_max_before(on ? min(max(s1, 0), kv.n_seqs) : 0, top_f, lane);
         const bool order = s0 >= before && s1 >= s0 && s1 <= kv.n_seqs;
         f0 = !on ? 0x7fffffff : order ? s0 : before;
         f1 = on && order ? s1 : f0;
-        v = KvSeq{0, 0, min(max(len, 0), kv.cap)};
-        int end = 0;
-        if (f1 > f0) { v.r0 = min(max(kv.row_start[f0], 0), kv.n_rows); end = min(max(kv.row_start[f1], 0), kv.n_rows); }
+        const int shared = min(max(len, 0), kv.cap), r0 = begin(f1 > f0 ? f0 : 0), r1 = begin(f1 > f0 ? f1 : 0);
+        v = KvSeq{f1 > f0 ? min(max(r0, 0), kv.n_rows) : 0, 0, shared};
+        const int end = f1 > f0 ? min(max(r1, 0), kv.n_rows) : 0;
         v.n = v.r0 >= kv_max_before(end, top_h, lane) ? max(end - v.r0, 0) : 0;
-        if (check && on && (!order || v.len != len)) kv_flag(kv, ASD_KV_BAD_GROUP);
+        if (check && on && (!order || shared != len)) kv_flag(kv, ASD_KV_BAD_GROUP);
+    }
+    __device__ __forceinline__ void load(const KvArgs& kv, int g0, int lane, bool check) {
+        ask(g0, lane);
+        take(kv, g0, lane, check, [&](int s) { return kv.row_start[s]; });
+    }
+    // the first 64; with up to 64 sequences their beginnings are asked for along with the groups
+    __device__ __forceinline__ void begin(const KvArgs& kv, int lane, bool check) {
+        ask(0, lane);
+        if (kv.n_seqs > 64) return take(kv, 0, lane, check, [&](int s) { return kv.row_start[s]; });
+        const int s = min(lane, kv.n_seqs - 1), r0 = kv.row_start[s], r1 = kv.row_start[s + 1];
+        take(kv, 0, lane, check, [&](int at) { const int x = __shfl(r0, min(at, 63)), y = __shfl(r1, max(at - 1, 0)); return at < kv.n_seqs ? x : y; });
     }
 };
 // The sequences, with the first key of their own (v.low): 0 where a sequence is in no group, or has a new row that does not lie behind the shared tokens
@@ -150,7 +193,7 @@ struct KvOwnLanes : KvLanes {
 #pragma unroll
                 for (int step = 32; step > 0; step >>= 1) if (__shfl(g.f0, at + step) <= s) at += step;
             const int f0 = __shfl(g.f0, at), f1 = __shfl(g.f1, at), r0 = __shfl(g.v.r0, at), rows = __shfl(g.v.n, at), len = __shfl(g.v.len, at);
-            if (s >= f0 && s < f1 && v.n > 0 && v.r0 >= r0 && v.r0 + v.n <= r0 + rows && v.len - v.n >= len) v.low = len;
+            if (s >= f0 && s < f1 && v.n > 0 && v.r0 >= r0 && v.r0 + v.n <= r0 + rows && v.len - v.n >= len) { v.low = len; v.lead = f0; }
             g0 += 64;
             if (g0 >= n) break;
             g.load(kv, g0, lane, false);
@@ -159,6 +202,10 @@ struct KvOwnLanes : KvLanes {
 };
 __device__ __forceinline__ int kv_front_chunks(const KvSeq& v) { return (v.len + 63) / 64; }
 __device__ __forceinline__ int kv_own_chunks(const KvSeq& v) { return (v.len + 63) / 64 - v.low / 64; }
+__device__ __forceinline__ int kv_both_chunks(const KvSeq& v) { return (v.len + 63) / 64 + (v.low % 64 != 0); }
+__device__ __forceinline__ int kv_front_items(const KvSharedArgs& a, const KvSeq& v, int rows, int run) {
+    return v.len > 0 ? kv_tiles_of(a.kv, v, rows) * kv_splits(kv_front_chunks(v), run) * a.kv.n_kv : 0;
+}
 // work item `item` of the shared keys
 template <int R, class F> __device__ __forceinline__ bool kv_front_item(const KvSharedArgs& a, int64_t item, KvItem& it, F) {
     const int lane = threadIdx.x & 63, n_kv = a.kv.n_kv;
@@ -166,9 +213,9 @@ template <int R, class F> __device__ __forceinline__ bool kv_front_item(const Kv
     int64_t first;
     const bool check = item == 0 && threadIdx.x < 64;
     KvGroupLanes all(a);
-    all.load(a.kv, 0, lane, check);
+    all.begin(a.kv, lane, check);
     const int run = kv_run_all(a.front(), all, lane, R, kv_front_chunks);
-    auto count = [&](const KvSeq& v) { return v.len > 0 ? kv_tiles_of(a.kv, v, R) * kv_splits(kv_front_chunks(v), run) * n_kv : 0; };
+    auto count = [&](const KvSeq& v) { return kv_front_items(a, v, R, run); };
     if (!kv_find(a.kv, all, item, lane, check, count, &group, &local, &first, &it.s)) return false;
     it.seq = a.group_start[group];
     kv_place_item(it, local, first, kv_tiles_of(a.kv, it.s, R), n_kv, F::value);
@@ -176,97 +223,77 @@ template <int R, class F> __device__ __forceinline__ bool kv_front_item(const Kv
     it.whole = false;
     return true;
 }
-// work item `item` of the own keys
-template <int R, class F> __device__ __forceinline__ bool kv_own_item(const KvSharedArgs& a, int64_t item, KvItem& it, F) {
+// where the sums of the sequence's rows over the shared keys are
+__device__ __forceinline__ void kv_front_note(const KvSharedArgs& a, KvGroupLanes groups, const KvItem& it, int lane, KvNote& k) {
+    const int n_kv = a.kv.n_kv, R = a.front_rows, run = kv_run_all(a.front(), groups, lane, R, kv_front_chunks);
+    int64_t before = 0;
+    for (int g0 = 0; g0 < a.n_groups; g0 += 64) {
+        if (g0) groups.load(a.kv, g0, lane, false);
+        const int c = kv_front_items(a, groups.v, R, run);
+        const unsigned long long mine = __ballot(groups.f0 == it.s.lead && groups.f1 > groups.f0);
+        const int l = uniform(mine ? __ffsll(mine) - 1 : 64);
+        before += wave_sum(lane < l ? c : 0);
+        if (!mine) continue;
+        const KvSeq g{from_lane(groups.v.r0, l), from_lane(groups.v.n, l), from_lane(groups.v.len, l)};
+        k.n_front = kv_splits(kv_front_chunks(g), run);
+        k.front = (int)before + it.kvh;
+        k.front_step = kv_tiles_of(a.kv, g, R) * n_kv;
+        k.front_row = (it.s.r0 - g.r0) * a.kv.group;
+        return;
+    }
+}
+// work item `item` of the own keys; BOTH: of all keys of a sequence, the shared ones in front
+template <int R, bool BOTH, class F> __device__ __forceinline__ bool kv_own_item(const KvSharedArgs& a, KvNotes* notes, int64_t item, KvItem& it, F) {
     const int lane = threadIdx.x & 63, n_kv = a.kv.n_kv;
     int local;
     int64_t first;
     const bool check = item == 0 && threadIdx.x < 64;
     KvGroupLanes groups(a);
-    groups.load(a.kv, 0, lane, false);
+    groups.begin(a.kv, lane, BOTH && check);
     KvOwnLanes all(groups);
     all.load(a.kv, 0, lane, check);
-    const int run = kv_run_all(a, all, lane, R, kv_own_chunks);
-    auto count = [&](const KvSeq& v) { return kv_tiles_of(a.kv, v, R) * kv_splits(kv_own_chunks(v), run) * n_kv; };
+    auto chunks = [](const KvSeq& v) { return BOTH ? kv_both_chunks(v) : kv_own_chunks(v); };
+    const int run = kv_run_all(a, all, lane, R, chunks);
+    auto count = [&](const KvSeq& v) { return kv_tiles_of(a.kv, v, R) * kv_splits(chunks(v), run) * n_kv; };
+    auto joined = [&](const KvSeq& v) { return kv_splits(chunks(v), run) > 1 || (!BOTH && v.low > 0) ? kv_tiles_of(a.kv, v, 16) : 0; };
+    if (check && (!BOTH || a.cut)) kv_count_notes(notes, a.kv, all, lane, joined);
+    if (BOTH && check && a.n_groups > 64) for (int g0 = 64; g0 < a.n_groups; g0 += 64) groups.load(a.kv, g0, lane, true);
     if (!kv_find(a.kv, all, item, lane, check, count, &it.seq, &local, &first, &it.s)) return false;
-    const int n_splits = kv_splits(kv_own_chunks(it.s), run);
-    kv_place_item(it, local, first, kv_tiles_of(a.kv, it.s, R), n_kv, F::value);
-    it.per = kv_per_split(kv_own_chunks(it.s), n_splits);
-    it.whole = n_splits == 1 && it.s.low == 0;
+    const int n_splits = kv_splits(chunks(it.s), run), n_tiles = kv_tiles_of(a.kv, it.s, R);
+    kv_place_item(it, local, first, n_tiles, n_kv, F::value);
+    it.per = kv_per_split(chunks(it.s), n_splits);
+    it.whole = n_splits == 1 && (BOTH || it.s.low == 0);
+    if (!it.whole && it.split == 0 && threadIdx.x >= 192) {
+        KvNote k{.n_own = n_splits};
+        if (!BOTH && it.s.low > 0) kv_front_note(a, groups, it, lane, k);
+        kv_write_notes(notes, a, it, n_tiles, kv_items_before(a.kv, all, it.seq, lane, joined), lane, k);
+    }
     return true;
 }
-template <class A, class C, int H, int NT>
-__global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_front_kernel(const KvSharedArgs a) {
-    __shared__ KvFewLds<H> lds;
+// Both parts in one launch, the shared keys' items first: tiles of 16 * FNT rows (128: FNT = 8), the own ones of 16
+template <class A, class C, int H, int FNT>
+__global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_apart_kernel(const KvSharedArgs a, KvNotes* notes) {
+    using Ring = u32x4[KV_RING<C, H>];
+    constexpr size_t RING = FNT == 8 ? sizeof(Ring) : 0;
+    __shared__ __align__(16) char mem[RING > sizeof(KvFewLds<H>) ? RING : sizeof(KvFewLds<H>)];
     KvItem it;
-    if (kv_front_item<16 * NT>(a, blockIdx.x, it, std::false_type{})) kv_few_rows<A, C, H, NT, KV_SHARED>(a.front(), it, lds);
-}
-template <class A, class C, int H, int NT>
-__global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_own_kernel(const KvSharedArgs a) {
-    __shared__ KvFewLds<H> lds;
-    KvItem it;
-    if (kv_own_item<16 * NT>(a, blockIdx.x, it, std::false_type{})) kv_few_rows<A, C, H, NT, KV_OWN>(a, it, lds);
-}
-template <class C, int H, int NT, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void kv_front_rows_kernel(const KvSharedArgs a) {
-    __shared__ u32x4 mem[KV_RING<C, H>];
-    KvItem it;
-    if (kv_front_item<16 * NT * NW>(a, blockIdx.x, it, std::false_type{})) kv_many_rows<C, H, NT, NW, KV_SHARED>(a.front(), it, mem);
-}
-template <class C, int H, int NT, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void kv_own_rows_kernel(const KvSharedArgs a) {
-    __shared__ u32x4 mem[KV_RING<C, H>];
-    KvItem it;
-    if (kv_own_item<16 * NT * NW>(a, blockIdx.x, it, std::true_type{})) kv_many_rows<C, H, NT, NW, KV_OWN>(a, it, mem);
-}
-// Puts the parts of every row together
-template <class A, int H>
-__global__ __launch_bounds__(256) void kv_shared_join_kernel(const KvSharedArgs a) {
-    const int lane = threadIdx.x & 63, n_kv = a.kv.n_kv, rows_each = a.kv.group, R = a.tile_rows, FR = a.front_rows;
-    int seq, local;
-    int64_t first;
-    KvSeq s;
-    KvGroupLanes groups(a);
-    groups.load(a.kv, 0, lane, false);
-    KvOwnLanes all(groups);
-    all.load(a.kv, 0, lane, false);
-    const int run = kv_run_all(a, all, lane, R, kv_own_chunks);
-    // 16 rows of a sequence with more than one part and KV head
-    if (!kv_find(a.kv, all, blockIdx.x, lane, false, [&](const KvSeq& v) { return kv_splits(kv_own_chunks(v), run) > 1 || v.low > 0 ? kv_tiles_of(a.kv, v, 16) * n_kv : 0; },
-                 &seq, &local, &first, &s)) return;
-    const int64_t item0 = kv_items_before(a.kv, all, seq, lane, [&](const KvSeq& v) { return (int64_t)kv_tiles_of(a.kv, v, R) * kv_splits(kv_own_chunks(v), run) * n_kv; });
-    const int n_own = kv_splits(kv_own_chunks(s), run), n_tiles = kv_tiles_of(a.kv, s, R), kvh = local % n_kv, row0 = local / n_kv * 16;
-    const int64_t step = (int64_t)n_tiles * n_kv * R, at = (item0 + (int64_t)(row0 / R) * n_kv + kvh) * R + row0 % R;
-    // the group of the sequence, its first item, and the sequence's first row among the group's
-    int n_front = 0, front_tiles = 0;
-    int64_t front0 = 0, front_row = 0;
-    if (s.low > 0) {
-        const int front_run = kv_run_all(a.front(), groups, lane, FR, kv_front_chunks);
-        for (int g0 = 0;;) {
-            const int64_t c = groups.v.len > 0 ? (int64_t)kv_tiles_of(a.kv, groups.v, FR) * kv_splits(kv_front_chunks(groups.v), front_run) * n_kv : 0;
-            const unsigned long long mine = __ballot(seq >= groups.f0 && seq < groups.f1);
-            const int l = uniform(mine ? __ffsll(mine) - 1 : 64);
-            front0 += wave_sum(lane < l ? c : 0);
-            if (mine) {
-                const KvSeq g{from_lane(groups.v.r0, l), from_lane(groups.v.n, l), from_lane(groups.v.len, l)};
-                n_front = kv_splits(kv_front_chunks(g), front_run);
-                front_tiles = kv_tiles_of(a.kv, g, FR);
-                front_row = (int64_t)(s.r0 - g.r0) * rows_each + row0;
-                break;
-            }
-            g0 += 64;
-            if (g0 >= a.n_groups) break;
-            groups.load(a.kv, g0, lane, false);
-        }
+    if (blockIdx.x >= (unsigned)a.front_grid) {
+        if (kv_own_item<16, false>(a, notes, blockIdx.x - a.front_grid, it, std::false_type{})) kv_few_rows<A, C, H, 1, KV_OWN>(a, it, *(KvFewLds<H>*)mem);
+    } else if (kv_front_item<16 * FNT>(a, blockIdx.x, it, std::false_type{})) {
+        if constexpr (FNT == 8) kv_many_rows<C, H, 2, 4, KV_SHARED>(a.front(), it, *(Ring*)mem);
+        else kv_few_rows<A, C, H, FNT, KV_SHARED>(a.front(), it, *(KvFewLds<H>*)mem);
     }
-    kv_join_rows<A, H>(a, s, kvh, row0, min(s.n * rows_each - row0, 16), n_own + n_front, [&](int i, int r) {
-        const float *o = a.o_part, *ml = a.ml_part;
-        int64_t p = at + r + i * step;
-        if (i >= n_own) {
-            const int64_t row = front_row + r;
-            p = (front0 + ((int64_t)(i - n_own) * front_tiles + row / FR) * n_kv + kvh) * FR + row % FR;
-            o = a.front_o; ml = a.front_ml;
-        }
-        return KvPartial{o + p * H, ml + p * 2};
-    });
+}
+// All keys of a sequence, the shared ones through the page table of the group's first
+template <class A, class C, int H, int NT>
+__global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_both_kernel(const KvSharedArgs a, KvNotes* notes) {
+    __shared__ KvFewLds<H> lds;
+    KvItem it;
+    if (kv_own_item<16 * NT, true>(a, notes, blockIdx.x, it, std::false_type{})) kv_few_rows<A, C, H, NT, KV_BOTH>(a, it, lds);
+}
+template <class C, int H, int NT, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void kv_both_rows_kernel(const KvSharedArgs a, KvNotes* notes) {
+    __shared__ u32x4 mem[KV_RING<C, H>];
+    KvItem it;
+    if (kv_own_item<16 * NT * NW, true>(a, notes, blockIdx.x, it, std::true_type{})) kv_many_rows<C, H, NT, NW, KV_BOTH>(a, it, mem);
 }

@@ -310,6 +310,6 @@ def test_refusals_of_the_binding():
         with pytest.raises(asd.AsdError):
             p.cache.attend_shared(b, groups, bad)
     with pytest.raises(asd.AsdError):
-        p.cache.attend_shared(b, groups, q, workspace=torch.empty(256, dtype=torch.uint8, device=DEV)[:16])
+        p.cache.attend_shared(b, groups, q, workspace=torch.empty(256, dtype=torch.uint8))
     with pytest.raises(AttributeError):
         groups.shared_len = i32([4])
