@@ -499,13 +499,6 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
         low = from - window + 1; low_last = last - window + 1; my_low = my_from - window + 1; my_low_last = my_last - window + 1;
     }
     if constexpr (SEES >= KV_OWN) low = low_last = my_low = my_low_last = s.low;
-    auto hidden = [&](int key, int t, bool first) {      // first: of the first steps
-        bool h = key > pos[t];
-        if constexpr (SEES == KV_WINDOW) h = h || (key <= pos[t] - window && key >= sinks);
-        if constexpr (SEES == KV_OWN) h = h || key < low;
-        if constexpr (SEES == KV_BOTH) h = h || (key < low) != first;
-        return h;
-    };
     // Steps of one chunk: those of the workgroup's run, those that all its rows see whole
     const KvSteps steps = kv_steps<SEES>(a, low, 64);
     const int c0 = it.split * per, c_end = min((last + 64) / 64 - steps.skip, c0 + per);
@@ -541,7 +534,7 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
 #pragma unroll
             for (int q = 0; q < LH; ++q) frag_to_lds(from_ + (w + NW * q) * 1024, bytes, mem + slot * HF * 64 + (w + NW * q) * 64, lane);
         };
-        auto ask_k = [&]() {                             // past the end: the last chunk again
+        auto ask_k = [&]() {                             // past the end: nothing, the requests are only counted
             if (asked < c_end) {
                 const int page = pages.at(page_i);
                 src = a.kv.pages + (((size_t)max(page, 0) * n_kv + kvh) * cpp + in_page) * L::CHUNK;
@@ -553,6 +546,8 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
                     page_i = (steps.first + steps.skip) / cpp; in_page = (steps.first + steps.skip) % cpp;
                     pages = later;
                 }
+            } else {
+                n_bytes = 0;
             }
             half(src, n_bytes, slot_k);
             if constexpr (L::Q8)
@@ -581,6 +576,12 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
         // the written keys that belong to step c: first_key .. last_key - 1
         auto first_key = [&](int c) { return SEES == KV_OWN || (SEES == KV_BOTH && c >= steps.first) ? low : 0; };
         auto last_key = [&](int c) { return SEES == KV_BOTH && c < steps.first ? low : s.len; };
+        auto cleaned = [&]() {
+            asm volatile("" ::: "memory");
+            wait_vm<63, true>();                         // (the ring's requests go on)
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
         // step c, chunk r: one that this wave has products for; edge: some of its rows do not see all of it
         auto work = [&](const int c, const int r, auto is_edge) {
             constexpr bool edge = decltype(is_edge)::value;
@@ -598,7 +599,9 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
 #pragma unroll
             for (int hp = 0; hp < HP; ++hp) {
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt) f[(hp + 1) & 1][kt] = hp + 1 < HP ? kp[(kt * HP + hp + 1) * 64] : vp[kt * 64];
+                for (int kt = 0; kt < 4; ++kt)
+                    if (hp + 1 < HP) f[(hp + 1) & 1][kt] = kp[(kt * HP + hp + 1) * 64];
+                    else if (!edge) f[(hp + 1) & 1][kt] = vp[kt * 64];
 #pragma unroll
                 for (int u = 0; u < US; ++u)
 #pragma unroll
@@ -623,19 +626,38 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
 #pragma unroll
                     for (int j = 0; j < 4; ++j) vs[kt][j] = q8_scale((ve[kt] >> (8 * j)) & 255u);
             if constexpr (edge) {
+                // Masks by the places of a row's first and last key in the chunk, and only on the side on which some row of the wave does not see all of it (a lane's
+                // keys: those of lane group 0, at constants, and `at` on)
+                const bool first = TWO && c < steps.first;
+                const int at = r * 64 + score_key<C>(0, 4 * g), end = first ? (SEES == KV_WINDOW ? sinks : low) - 1 : 0x7fffffff;
+                if (r * 64 + 63 > min(my_from, end)) {
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                    for (int t = 0; t < NT; ++t) {
+                        const int most = min(pos[t], end) - at;
 #pragma unroll
-                    for (int kt = 0; kt < 4; ++kt)
+                        for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (hidden(r * 64 + score_key<C>(kt, 4 * g + j), t, TWO && c < steps.first)) sc[t][kt][j] = -INFINITY;
+                            for (int j = 0; j < 4; ++j) if (score_key<C>(kt, j) > most) sc[t][kt][j] = -INFINITY;
+                    }
+                }
+                if constexpr (SEES == KV_WINDOW || SEES >= KV_OWN) if (!first && r * 64 < my_low_last) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const int least = (SEES == KV_WINDOW ? pos[t] - window + 1 : low) - at, after = SEES == KV_WINDOW ? max(sinks - at, -64) : -64;      // (hidden: after .. least - 1)
+                        const uint32_t gap = (uint32_t)max(least - after, 0);
+#pragma unroll
+                        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) if ((uint32_t)(score_key<C>(kt, j) - after) < gap) sc[t][kt][j] = -INFINITY;
+                    }
+                }
                 if constexpr (L::Q8) {                   // (an unwritten scale may be anything)
                     const int n_keys = last_key(c) - r * 64, cut = first_key(c) - r * 64;
+                    if (n_keys < 64 || cut > 0)
 #pragma unroll
-                    for (int kt = 0; kt < 4; ++kt)
+                        for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) if (score_key<C>(kt, 4 * g + j) >= n_keys || (SEES >= KV_OWN && score_key<C>(kt, 4 * g + j) < cut)) vs[kt][j] = 0.f;
+                            for (int j = 0; j < 4; ++j) if (score_key<C>(kt, 4 * g + j) >= n_keys || (SEES >= KV_OWN && score_key<C>(kt, 4 * g + j) < cut)) vs[kt][j] = 0.f;
                 }
             }
             u32x4 pf[NT][PS];
@@ -670,6 +692,11 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
                 }
                 l[t] += sum[0] + sum[1];
             }
+            if constexpr (edge) {
+                cleaned();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f[HP & 1][j] = vp[j * 64];
+            }
             __builtin_amdgcn_s_setprio(1);
             constexpr int HG = 4 / KST;                  // output tiles of a step
 #pragma unroll
@@ -693,29 +720,36 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
             }
             __builtin_amdgcn_s_setprio(0);
         };
-        // A chunk with an edge: keys behind the end and values that are not finite leave V^T (see kv_clean); each wave cleans what it has asked for
+        // A chunk with an edge: keys behind the end and values that are not finite leave V^T (see kv_clean) before its products; each wave cleans what it has
+        // asked for, behind `cleaned` it has been done
         auto clean = [&](const int c, const int r) {
             const int n_keys = last_key(c) - r * 64, cut = first_key(c) - r * 64;
+            const bool part = n_keys < 64 || cut > 0;
+            u32x4* p = mem + (use_v * HF + w) * 64 + lane;
+            u32x4 f[LH];
             uint32_t hit = 0;
-#pragma unroll 1
-            for (int q = 0; q < LH; ++q) {
-                const int j = w + NW * q;
-                u32x4* p = mem + (use_v * HF + j) * 64 + lane;
-                u32x4 f = *p;
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    f[x] &= kv_kept<C>(n_keys, j % KST, g, x);
-                    if constexpr (SEES >= KV_OWN) f[x] &= ~kv_kept<C>(cut, j % KST, g, x);
-                    hit |= kv_odd<C>(f[x]);
-                    f[x] = kv_clean<C>(f[x]);
+            for (int q = 0; q < LH; ++q) f[q] = p[NW * q * 64];
+            if (part)
+#pragma unroll
+                for (int q = 0; q < LH; ++q)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        f[q][x] &= kv_kept<C>(n_keys, (w + NW * q) % KST, g, x);
+                        if constexpr (SEES >= KV_OWN) f[q][x] &= ~kv_kept<C>(cut, (w + NW * q) % KST, g, x);
+                    }
+#pragma unroll
+            for (int q = 0; q < LH; ++q)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) hit |= kv_odd<C>(f[q][x]);
+            if (part || __any(hit != 0))
+#pragma unroll
+                for (int q = 0; q < LH; ++q) {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) f[q][x] = kv_clean<C>(f[q][x]);
+                    p[NW * q * 64] = f[q];
                 }
-                *p = f;
-            }
             odd |= hit != 0;
-            asm volatile("" ::: "memory");
-            wait_vm<63, true>();                         // (the ring's requests go on)
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
         };
         auto done = [&]() {
             use_k = use_k + 2 >= SLOTS ? use_k + 2 - SLOTS : use_k + 2;
@@ -735,7 +769,7 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
             if (c >= first_main && (c < main0 || c >= main1)) clean(c, r);       // (beside a missing page: what all rows see goes through the products)
             bool mine = r * 64 <= my_last;
             if constexpr (SEES == KV_WINDOW) mine = mine && (r * 64 + 63 >= my_low || r * 64 < sinks);
-            if (mine && !((gone >> (c & 31)) & 1u)) work(c, r, std::true_type{}); else ask();
+            if (mine && !((gone >> (c & 31)) & 1u)) work(c, r, std::true_type{}); else { ask(); cleaned(); }
             done();
             gone &= ~(1u << (c & 31));
             ++c;
@@ -744,11 +778,11 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
         wait_vm<0, true>();                              // no request may outlive the workgroup's LDS
         __syncthreads();
         int* any = (int*)mem;                            // the ring is free: what one lane has taken out concerns all
-        if (tid == 0) *any = 0;
+        const bool found = __any(odd);
+        if (lane == 0) any[w] = found;
         __syncthreads();
-        if (odd) *any = 1;
-        __syncthreads();
-        odd = *any != 0;
+        odd = any[lane % NW] != 0;
+        odd = __any(odd);
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {

@@ -126,11 +126,11 @@ __global__ __launch_bounds__(64 * NW, 2) void kv_window_rows_kernel(const KvWind
 struct KvSharedArgs : KvAttendArgs {                    // (o_part .. cut: of the own keys)
     const int32_t *group_start, *shared_len;
     int32_t n_groups;
-    int32_t front_target, front_cut, front_rows, front_grid;
+    int32_t front_target, front_min_run, front_cut, front_rows, front_grid;
     float *front_o, *front_ml;
     __device__ __forceinline__ KvAttendArgs front() const {
         KvAttendArgs f = *this;
-        f.o_part = front_o; f.ml_part = front_ml; f.target = front_target; f.cut = front_cut;
+        f.o_part = front_o; f.ml_part = front_ml; f.target = front_target; f.min_run = front_min_run; f.cut = front_cut;
         return f;
     }
 };

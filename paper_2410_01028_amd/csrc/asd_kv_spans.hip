@@ -143,7 +143,7 @@ int asd_kv_attend_shared(const asd_kv_shape* s, const asd_kv_batch* b, const asd
     KvNotes* notes = (KvNotes*)workspace;
     a.front_o = (float*)((char*)workspace + p.front_at); a.front_ml = (float*)((char*)a.front_o + p.front.o_bytes);
     a.o_part = (float*)((char*)workspace + p.own_at); a.ml_part = (float*)((char*)a.o_part + p.own.o_bytes);
-    a.front_target = p.front.target; a.front_cut = p.front.join; a.front_rows = 16 * p.front.nt; a.front_grid = (int32_t)p.front.grid;
+    a.front_target = p.front.target; a.front_min_run = p.front.min_run; a.front_cut = p.front.join; a.front_rows = 16 * p.front.nt; a.front_grid = (int32_t)p.front.grid;
     a.target = p.own.target; a.cut = p.own.join; a.min_run = p.own.min_run; a.tile_rows = 16 * p.own.nt;
     const hipStream_t stream = (hipStream_t)hip_stream;
     by_shape(s, [&](auto t, auto c, auto h) {
