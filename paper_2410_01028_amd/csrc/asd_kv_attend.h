@@ -13,6 +13,7 @@ struct KvAttendArgs {
     int32_t target;                 // work items to cut the batch into
     int32_t min_run;                // chunks that are worth a run
     int32_t cut;                    // 0: every tile's keys stay together
+    int32_t tail;                   // > 0: those of the last round's tiles are cut, into this many runs at most (asd_kv_spans.h)
     int32_t tile_rows;              // rows of a tile
 };
 // What the rows of a tile see.  KV_ALL: the keys 0 .. position of their sequence.  KV_WINDOW: of those the last `window` and the first `sinks`.  Sequences that
@@ -478,17 +479,6 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
     const int seq = it.seq, kvh = it.kvh, tile = it.tile, per = it.per, n_kv = a.kv.n_kv;
     const KvSeq s = it.s;
     const int rows = s.n * a.kv.group, base = s.len - s.n, row0 = (tile * NW + w) * NT * 16;
-    int pos[NT];
-    u32x4 qf[NT][QS];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int row = row0 + t * 16 + m, token = row / a.kv.group, head = kvh * a.kv.group + row % a.kv.group;
-        const bool on = row < rows;
-        pos[t] = on ? SEES == KV_SHARED ? s.len - 1 : base + token : -1;
-        const uint16_t* qp = (const uint16_t*)a.q + (s.r0 + (int64_t)token) * a.q_stride + head * H;
-#pragma unroll
-        for (int i = 0; i < QS; ++i) qf[t][i] = on ? *(const u32x4*)(qp + i / US * 4 * KK + g * KK + i % US * AE) : u32x4{0u, 0u, 0u, 0u};
-    }
     // last key of row `row`'s token
     auto reach = [&](int row) { return SEES == KV_SHARED ? s.len - 1 : base + row / a.kv.group; };
     const int from = reach(tile * RT * 16), last = reach(min((tile + 1) * 16 * RT, rows) - 1);                 // ... of the workgroup's first and last row
@@ -504,6 +494,27 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
     const int c0 = it.split * per, c_end = min((last + 64) / 64 - steps.skip, c0 + per);
     const int main0 = max((max(low_last, 0) + 63) / 64 - steps.skip, c0), main1 = min(c_end, (from + 1) / 64 - steps.skip);
     const int first_main = SEES == KV_BOTH ? min(low / 64, c_end) : 0;                    // ... and the first ones (of the shared keys)
+    // The page of the chunk asked for next: the table's entries lie in the wave's lanes, those of the first steps apart from the others.  (Asked for ahead of the
+    // queries: the first chunk's request waits for them alone.)
+    constexpr bool TWO = SEES == KV_WINDOW || SEES == KV_BOTH;
+    const int cpp = a.kv.page_tokens / 64, r0 = steps.at(c0), first_seq = SEES == KV_BOTH ? s.lead : seq;
+    int page_i = r0 / cpp, in_page = r0 % cpp;
+    KvPages pages, later;
+    if (c_end > c0) {
+        pages.load(a.kv, TWO && c0 < steps.first ? first_seq : seq, page_i, lane);
+        if constexpr (TWO) if (c0 < steps.first && c_end > steps.first) later.load(a.kv, seq, (steps.first + steps.skip) / cpp, lane);
+    }
+    int pos[NT];
+    u32x4 qf[NT][QS];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int row = row0 + t * 16 + m, token = row / a.kv.group, head = kvh * a.kv.group + row % a.kv.group;
+        const bool on = row < rows;
+        pos[t] = on ? SEES == KV_SHARED ? s.len - 1 : base + token : -1;
+        const uint16_t* qp = (const uint16_t*)a.q + (s.r0 + (int64_t)token) * a.q_stride + head * H;
+#pragma unroll
+        for (int i = 0; i < QS; ++i) qf[t][i] = on ? *(const u32x4*)(qp + i / US * 4 * KK + g * KK + i % US * AE) : u32x4{0u, 0u, 0u, 0u};
+    }
     f32x4 o[NT][HT];
     float mx[NT], l[NT];
 #pragma unroll
@@ -514,14 +525,6 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
     }
     bool odd = false;                                    // this lane has taken a value out of V
     if (c_end > c0) {
-        // The page of the chunk asked for next: the table's entries lie in the wave's lanes, those of the first steps apart from the others
-        constexpr bool TWO = SEES == KV_WINDOW || SEES == KV_BOTH;
-        const int cpp = a.kv.page_tokens / 64, r0 = steps.at(c0);
-        int page_i = r0 / cpp, in_page = r0 % cpp;
-        KvPages pages, later;
-        const int first_seq = SEES == KV_BOTH ? s.lead : seq;
-        pages.load(a.kv, TWO && c0 < steps.first ? first_seq : seq, page_i, lane);
-        if constexpr (TWO) if (c0 < steps.first && c_end > steps.first) later.load(a.kv, seq, (steps.first + steps.skip) / cpp, lane);
         uint32_t gone = 0;                               // bit c % 32: the chunk of step c has no page
         bool lost = false;
         int asked = c0;                                  // chunk whose K is asked for next
@@ -560,8 +563,8 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
             slot_v = slot_v + 2 >= SLOTS ? slot_v + 2 - SLOTS : slot_v + 2;
         };
         int use_k = 0, use_v = 1;                        // slots of the chunk at hand
-        wait_vm<0, true>();                              // from here on only the ring's requests count
         ask_k(); ask_v(src, n_bytes); ask_k();           // K, V^T of the first chunk, K of the next
+        wait_vm<3 * LH + 2 * X, true>();                 // the queries are there: from here on only the ring's requests count
         auto turn = [&]() {
             if (page_i - pages.base >= 62) {             // (once in 62 pages: the ring runs dry for a moment)
                 pages.load(a.kv, TWO && asked < steps.first ? first_seq : seq, page_i, lane);

@@ -11,10 +11,15 @@ struct AttendPlan {
     int32_t target, max_tiles, min_run;
     int64_t grid;                  // most work items
     bool join;                     // some sequence's keys may be cut
+    int32_t tail;                  // > 0: only the tiles of the last, partly filled round are, into this many runs at most
+    int64_t join_blocks;           // 16-row blocks that may be joined
     size_t o_bytes, bytes;
 };
+// What differs between the forms of attention.  PLAN_CAUSAL: asd_kv_attend, whose sums stay as they are.  PLAN_EVEN: tiles of a batch walk about as many chunks each (a
+// window).  PLAN_BOTH: as causal attention.  PLAN_SMALL: tiles of 16 rows only.
+enum PlanForm { PLAN_CAUSAL, PLAN_EVEN, PLAN_BOTH, PLAN_SMALL };
 // walk(R): the chunks that tiles of R rows walk at most
-template <class F> AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b, F walk, bool large_tiles = true) {
+template <class F> AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b, F walk, PlanForm form = PLAN_CAUSAL) {
     AttendPlan p{};
     const int group = s->n_heads / s->n_kv_heads;
     const int64_t rows = (int64_t)b->max_new * group;
@@ -34,9 +39,9 @@ template <class F> AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_ba
     // 4000 in all, 64 / 8 heads x 128: 187 us against 269; 8 bits 142 against 135), and codes widened for fp32 products in a batch that fills the card
     // (four prompts of 500, 32 / 32 heads x 128: 186 against 224; with 8 / 8 heads, just below the border, the rule's 63 against 57).
     p.nt = rows <= 16 ? 1 : bf16 ? (!q8 && chunks >= 8 ? 2 : 1) : (q8 && (int64_t)b->n_rows * s->n_heads / 32 >= 2 * units() ? 2 : 1);
-    if (!large_tiles) p.rows = false;
+    if (form == PLAN_SMALL) p.rows = false;
     if (p.rows) p.nt = 8;
-    if (!large_tiles) p.nt = 1;
+    if (form == PLAN_SMALL) p.nt = 1;
     p.max_tiles = (int32_t)tiles(p.nt);
     chunks = walk(16 * p.nt);
     // Keys are cut into about four items per compute unit (48 sequences of 500 to 8192 tokens: 90 us, with two 100, with eight 97), but not
@@ -46,10 +51,29 @@ template <class F> AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_ba
     // and 221.  128 tokens behind 400 .. 8192 and the 512 rows: 402 and 428, behind 400 .. 16384 734 and 703)
     p.min_run = 16;
     p.target = 4 * units();
-    const int64_t whole = (int64_t)p.max_tiles * s->n_kv_heads, full = (int64_t)b->n_rows * group / (16 * p.nt) * s->n_kv_heads;
+    const int64_t whole = (int64_t)p.max_tiles * s->n_kv_heads;
+    // Fewer tiles than compute units: runs of four chunks are worth their join (a token of one sequence of 8192, window 4096, 32 / 32 heads x 128, bf16 pages: 20 us against 23.5)
+    if ((form == PLAN_EVEN || form == PLAN_BOTH) && whole < units()) { p.min_run = 4; p.target = units(); }
+    const int64_t full = (int64_t)b->n_rows * group / (16 * p.nt) * s->n_kv_heads;
     const int64_t most = (chunks + p.min_run / 2) / p.min_run;      // runs of the longest sequence
     p.join = most > 1 && !(p.rows && (full >= p.target || (whole >= p.target && chunks < 128)));
+    // kv_many_rows' tiles are few and long beside the two that a compute unit works on at a time.  Those that fill whole rounds stay whole; the rest are cut so that they fill
+    // one more (512 rows behind 8195 tokens and 260 behind 2665, 64 / 8 heads, 8 bits, window 2048, 392 tiles: 110 us with all tiles cut, 92 so; 24 questions behind system
+    // prompts of 4000, 2756 and 2976 tokens, 2.2 rounds: 307 us with none cut, 272 so).
+    if (p.rows && (form == PLAN_EVEN || (form == PLAN_BOTH && !p.join))) {
+        p.target = 2 * units();
+        p.tail = (int32_t)(chunks / 8 < 1 ? 1 : chunks / 8 < p.target ? chunks / 8 : p.target);
+        p.join = p.tail > 1;
+        p.grid = whole + (p.join ? p.target : 0);
+        p.join_blocks = (whole < p.target / 2 ? whole : p.target / 2) * p.nt;
+        if (p.join) {
+            p.o_bytes = ((size_t)p.target * 16 * p.nt * s->head_dim * 4 + 255) / 256 * 256;
+            p.bytes = p.o_bytes + (size_t)p.target * 16 * p.nt * 8;
+        }
+        return p;
+    }
     p.grid = p.join ? whole + p.target : whole;
+    p.join_blocks = tiles(1) * s->n_kv_heads;
     if (p.join && whole * most < p.grid) p.grid = whole * most;
     if (p.join) {
         p.o_bytes = ((size_t)p.grid * 16 * p.nt * s->head_dim * 4 + 255) / 256 * 256;

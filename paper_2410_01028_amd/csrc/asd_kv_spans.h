@@ -49,7 +49,7 @@ template <class A, int H>
 __global__ __launch_bounds__(256) void kv_parts_kernel(const KvAttendArgs a, const KvNotes* notes, const float* front_o, const float* front_ml, int front_rows) {
     const int n = notes->n;
     const KvNote k = notes->at[blockIdx.x];             // (the notes have room for every block)
-    if ((int)blockIdx.x >= n) return;
+    if ((int)blockIdx.x >= n || k.left == 0) return;
     const KvSeq s{uniform(k.r0), 0, 0};
     kv_join_rows<A, H>(a, s, uniform(k.kvh), uniform(k.row0), uniform(k.left), uniform(k.n_own + k.n_front), [&](int i, int r) {
         if (i < k.n_own) {
@@ -77,6 +77,30 @@ template <class Lanes, class F> __device__ __forceinline__ void kv_count_notes(K
     if (lane == 0) notes->n = (int)(n * a.n_kv);
 }
 
+// Item `item` where only the last round's tiles are cut (attend_plan): of all tiles and KV heads those that fill whole rounds of a.target come first, whole, then the others
+// in k runs each.  The notes on the latter lie tile by tile.
+template <int R, class Lanes, class F> __device__ __forceinline__ bool kv_tail_item(const KvAttendArgs& a, KvNotes* notes, const Lanes& all, int64_t item, int lane, bool check, KvItem& it, F chunks) {
+    const int n_kv = a.kv.n_kv;
+    auto tiles = [&](const KvSeq& v) { return kv_tiles_of(a.kv, v, R) * n_kv; };
+    const int total = (int)kv_items_before(a.kv, all, all.entries(a.kv), lane, tiles), rest = total % a.target, full = total - rest;
+    const int k = rest ? max(1, min(a.target / rest, a.tail)) : 1;
+    if (check && a.tail > 1 && lane == 0) notes->n = k > 1 ? rest * (R / 16) : 0;
+    const int over = max((int)item - full, 0), th = min((int)item, full) + over / k;
+    int local;
+    int64_t first;
+    if (!kv_find(a.kv, all, th, lane, check, tiles, &it.seq, &local, &first, &it.s)) return false;
+    kv_place_item(it, local, 0, kv_tiles_of(a.kv, it.s, R), n_kv, true);
+    it.split = over % k;
+    it.per = kv_per_split(chunks(it.s), th < full ? 1 : k);
+    it.whole = th < full || k == 1;
+    it.part = over;
+    if (!it.whole && it.split == 0 && threadIdx.x >= 192 && lane < R / 16) {
+        const int row = it.tile * R + lane * 16;
+        notes->at[(th - full) * (R / 16) + lane] = KvNote{it.s.r0, row, max(min(it.s.n * a.kv.group - row, 16), 0), it.kvh, k, over, 1, lane * 16};
+    }
+    return true;
+}
+
 // ---------------------------------------------------------------- a sliding window and the first tokens
 // The chunks that the tiles of R rows of a sequence walk at most: those of the first tokens, and those from the first row's window on to the last row
 __device__ __forceinline__ int kv_window_chunks(const KvWindowArgs& a, const KvSeq& v, int R) {
@@ -96,6 +120,7 @@ template <int R, class F> __device__ __forceinline__ bool kv_window_item(const K
     KvLanes all;
     all.load(a.kv, 0, lane, check);
     auto chunks = [&](const KvSeq& v) { return kv_window_chunks(a, v, R); };
+    if constexpr (F::value) return kv_tail_item<R>(a, notes, all, blockIdx.x, lane, check, it, chunks);
     const int run = kv_run_all(a, all, lane, R, chunks);
     auto joined = [&](const KvSeq& v) { return kv_splits(chunks(v), run) > 1 ? kv_tiles_of(a.kv, v, 16) : 0; };
     if (check && a.cut) kv_count_notes(notes, a.kv, all, lane, joined);
@@ -253,11 +278,12 @@ template <int R, bool BOTH, class F> __device__ __forceinline__ bool kv_own_item
     KvOwnLanes all(groups);
     all.load(a.kv, 0, lane, check);
     auto chunks = [](const KvSeq& v) { return BOTH ? kv_both_chunks(v) : kv_own_chunks(v); };
+    if (BOTH && check && a.n_groups > 64) for (int g0 = 64; g0 < a.n_groups; g0 += 64) groups.load(a.kv, g0, lane, true);
+    if (F::value && a.tail) return kv_tail_item<R>(a, notes, all, item, lane, check, it, chunks);
     const int run = kv_run_all(a, all, lane, R, chunks);
     auto count = [&](const KvSeq& v) { return kv_tiles_of(a.kv, v, R) * kv_splits(chunks(v), run) * n_kv; };
     auto joined = [&](const KvSeq& v) { return kv_splits(chunks(v), run) > 1 || (!BOTH && v.low > 0) ? kv_tiles_of(a.kv, v, 16) : 0; };
     if (check && (!BOTH || a.cut)) kv_count_notes(notes, a.kv, all, lane, joined);
-    if (BOTH && check && a.n_groups > 64) for (int g0 = 64; g0 < a.n_groups; g0 += 64) groups.load(a.kv, g0, lane, true);
     if (!kv_find(a.kv, all, item, lane, check, count, &it.seq, &local, &first, &it.s)) return false;
     const int n_splits = kv_splits(chunks(it.s), run), n_tiles = kv_tiles_of(a.kv, it.s, R);
     kv_place_item(it, local, first, n_tiles, n_kv, F::value);

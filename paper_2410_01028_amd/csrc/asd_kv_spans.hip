@@ -39,18 +39,15 @@ void attend_args(KvAttendArgs* a, const asd_kv_shape* s, const asd_kv_batch* b, 
 }
 
 int32_t at_most(int32_t x, int32_t most) { return x < most ? x : most; }
-// room for the notes on the rows that may be joined: 16-row blocks of all sequences and KV heads
-unsigned join_blocks(const asd_kv_shape* s, const asd_kv_batch* b) {
-    return (unsigned)(((int64_t)b->n_rows * (s->n_heads / s->n_kv_heads) / 16 + at_most(b->n_seqs, b->n_rows)) * s->n_kv_heads);
-}
-size_t notes_bytes(const asd_kv_shape* s, const asd_kv_batch* b) { return (64 + (size_t)join_blocks(s, b) * sizeof(KvNote) + 255) / 256 * 256; }
+// the notes on the rows that may be joined, in front of the partial sums
+size_t notes_bytes(const AttendPlan& p) { return (64 + (size_t)p.join_blocks * sizeof(KvNote) + 255) / 256 * 256; }
 AttendPlan window_plan(const asd_kv_shape* s, const asd_kv_batch* b, int32_t window, int32_t sinks) {
     const int64_t cap = kv_args(s, b).cap, chunks = (cap + 63) / 64, group = s->n_heads / s->n_kv_heads;
     return attend_plan(s, b, [=](int rows) {           // as kv_window_chunks
         const int64_t most = rows % group ? (rows + group - 2) / group + 1 : rows / group, tokens = most < b->max_new ? most : b->max_new;
         const int64_t n = ((int64_t)at_most(sinks, (int32_t)cap) + 63) / 64 + (at_most(window, (int32_t)cap) + tokens + 125) / 64;
         return n < chunks ? n : chunks;
-    });
+    }, PLAN_EVEN);
 }
 // Groups either way: `apart`, the shared keys read once for the rows of all sequences of a group, and each sequence's own; or, with `own` alone, each
 // sequence's tiles walk both.
@@ -64,22 +61,22 @@ SharedPlan shared_plan(const asd_kv_shape* s, const asd_kv_batch* b, const asd_k
     const int64_t chunks = (kv_args(s, b).cap + 63) / 64, group = s->n_heads / s->n_kv_heads;
     p.apart = (int64_t)b->n_rows * group <= 32 * (int64_t)b->n_seqs;
     if (!p.apart) {
-        p.own = attend_plan(s, b, [=](int) { return chunks + 1; });      // (the chunk in which the shared tokens end comes twice)
-        p.bytes = p.own.join ? notes_bytes(s, b) + p.own.bytes : 0;
-        p.own_at = notes_bytes(s, b);
+        p.own = attend_plan(s, b, [=](int) { return chunks + 1; }, PLAN_BOTH);      // (the chunk in which the shared tokens end comes twice)
+        p.bytes = p.own.join ? notes_bytes(p.own) + p.own.bytes : 0;
+        p.own_at = notes_bytes(p.own);
         return p;
     }
     asd_kv_batch rows = *b;                             // a group is one sequence to its shared keys
     rows.n_seqs = g->n_groups;
     rows.max_new = b->n_rows;
     p.front = attend_plan(s, &rows, [=](int) { return chunks; });
-    p.own = attend_plan(s, b, [=](int) { return chunks; }, false);
+    p.own = attend_plan(s, b, [=](int) { return chunks; }, PLAN_SMALL);
     // every tile has a place, cut or not
     for (AttendPlan* x : {&p.front, &p.own}) {
         x->o_bytes = ((size_t)x->grid * 16 * x->nt * s->head_dim * 4 + 255) / 256 * 256;
         x->bytes = (x->o_bytes + (size_t)x->grid * 16 * x->nt * 8 + 255) / 256 * 256;
     }
-    p.front_at = notes_bytes(s, b);
+    p.front_at = notes_bytes(p.own);
     p.own_at = p.front_at + p.front.bytes;
     p.bytes = p.own_at + p.own.bytes;
     return p;
@@ -92,7 +89,7 @@ extern "C" {
 size_t asd_kv_attend_window_workspace(const asd_kv_shape* s, const asd_kv_batch* b, int32_t window, int32_t sinks) {
     if (shape_fault(s) || batch_fault(s, b) || window_fault(window, sinks)) return 0;
     const AttendPlan p = window_plan(s, b, window, sinks);
-    return p.join ? notes_bytes(s, b) + p.bytes : 0;
+    return p.join ? notes_bytes(p) + p.bytes : 0;
 }
 
 int asd_kv_attend_window(const asd_kv_shape* s, const asd_kv_batch* b, int32_t window, int32_t sinks, const void* q, int64_t q_stride, void* out,
@@ -102,13 +99,13 @@ int asd_kv_attend_window(const asd_kv_shape* s, const asd_kv_batch* b, int32_t w
     if (!why) why = window_fault(window, sinks);
     if (why) return refuse(ASD_E_INVAL, "%s: %s", name, why);
     const AttendPlan p = window_plan(s, b, window, sinks);
-    if (const int rc = room(name, p.join ? notes_bytes(s, b) + p.bytes : 0, workspace, workspace_bytes)) return rc;
-    if (p.grid > MOST_GROUPS) return refuse(ASD_E_INVAL, "%s: the batch is too large", name);
+    if (const int rc = room(name, p.join ? notes_bytes(p) + p.bytes : 0, workspace, workspace_bytes)) return rc;
+    if (p.grid > MOST_GROUPS || p.join_blocks > MOST_GROUPS) return refuse(ASD_E_INVAL, "%s: the batch is too large", name);
     KvWindowArgs a{};
     attend_args(&a, s, b, q, q_stride, out, out_stride, scale);
     KvNotes* notes = (KvNotes*)workspace;
-    a.o_part = (float*)((char*)workspace + notes_bytes(s, b)); a.ml_part = (float*)((char*)a.o_part + p.o_bytes);
-    a.target = p.target; a.cut = p.join; a.min_run = p.min_run; a.tile_rows = 16 * p.nt;
+    a.o_part = (float*)((char*)workspace + notes_bytes(p)); a.ml_part = (float*)((char*)a.o_part + p.o_bytes);
+    a.target = p.target; a.cut = p.join; a.tail = p.tail; a.min_run = p.min_run; a.tile_rows = 16 * p.nt;
     a.window = at_most(window, a.kv.cap); a.sinks = at_most(sinks, a.kv.cap);
     const hipStream_t stream = (hipStream_t)hip_stream;
     by_shape(s, [&](auto t, auto c, auto h) {
@@ -118,7 +115,7 @@ int asd_kv_attend_window(const asd_kv_shape* s, const asd_kv_batch* b, int32_t w
         if (p.nt == 1) kv_window_kernel<T, C, h.value, 1><<<(unsigned)p.grid, 256, 0, stream>>>(a, notes);
         if constexpr (bf16 != q8) { if (p.nt == 2) kv_window_kernel<T, C, h.value, 2><<<(unsigned)p.grid, 256, 0, stream>>>(a, notes); }
         if constexpr (bf16 && h.value >= 64) { if (p.nt == 8) kv_window_rows_kernel<C, h.value, 2, 4><<<(unsigned)p.grid, 256, 0, stream>>>(a, notes); }
-        if (p.join) kv_parts_kernel<T, h.value><<<join_blocks(s, b), 256, 0, stream>>>(a, notes, nullptr, nullptr, 16);
+        if (p.join) kv_parts_kernel<T, h.value><<<(unsigned)p.join_blocks, 256, 0, stream>>>(a, notes, nullptr, nullptr, 16);
     });
     return launched(name);
 }
@@ -136,7 +133,7 @@ int asd_kv_attend_shared(const asd_kv_shape* s, const asd_kv_batch* b, const asd
     if (why) return refuse(ASD_E_INVAL, "%s: %s", name, why);
     const SharedPlan p = shared_plan(s, b, g);
     if (const int rc = room(name, p.bytes, workspace, workspace_bytes)) return rc;
-    if (p.front.grid + p.own.grid > MOST_GROUPS) return refuse(ASD_E_INVAL, "%s: the batch is too large", name);
+    if (p.front.grid + p.own.grid > MOST_GROUPS || p.own.join_blocks > MOST_GROUPS) return refuse(ASD_E_INVAL, "%s: the batch is too large", name);
     KvSharedArgs a{};
     attend_args(&a, s, b, q, q_stride, out, out_stride, scale);
     a.group_start = g->group_start; a.shared_len = g->shared_len; a.n_groups = g->n_groups;
@@ -144,7 +141,7 @@ int asd_kv_attend_shared(const asd_kv_shape* s, const asd_kv_batch* b, const asd
     a.front_o = (float*)((char*)workspace + p.front_at); a.front_ml = (float*)((char*)a.front_o + p.front.o_bytes);
     a.o_part = (float*)((char*)workspace + p.own_at); a.ml_part = (float*)((char*)a.o_part + p.own.o_bytes);
     a.front_target = p.front.target; a.front_min_run = p.front.min_run; a.front_cut = p.front.join; a.front_rows = 16 * p.front.nt; a.front_grid = (int32_t)p.front.grid;
-    a.target = p.own.target; a.cut = p.own.join; a.min_run = p.own.min_run; a.tile_rows = 16 * p.own.nt;
+    a.target = p.own.target; a.cut = p.own.join; a.tail = p.own.tail; a.min_run = p.own.min_run; a.tile_rows = 16 * p.own.nt;
     const hipStream_t stream = (hipStream_t)hip_stream;
     by_shape(s, [&](auto t, auto c, auto h) {
         using T = decltype(t);
@@ -161,7 +158,7 @@ int asd_kv_attend_shared(const asd_kv_shape* s, const asd_kv_batch* b, const asd
             if constexpr (bf16 != q8) { if (p.own.nt == 2) kv_both_kernel<T, C, h.value, 2><<<grid, 256, 0, stream>>>(a, notes); }
             if constexpr (bf16 && h.value >= 64) { if (p.own.nt == 8) kv_both_rows_kernel<C, h.value, 2, 4><<<grid, 256, 0, stream>>>(a, notes); }
         }
-        if (p.apart || p.own.join) kv_parts_kernel<T, h.value><<<join_blocks(s, b), 256, 0, stream>>>(a, notes, a.front_o, a.front_ml, a.front_rows);
+        if (p.apart || p.own.join) kv_parts_kernel<T, h.value><<<(unsigned)p.own.join_blocks, 256, 0, stream>>>(a, notes, a.front_o, a.front_ml, a.front_rows);
     });
     return launched(name);
 }
