@@ -125,23 +125,23 @@ template <int H> struct alignas(16) KvFewLds {
     float o[4][16][H], ml[4][16][2];
     int odd;
 };
-// 16 * NT rows against a run of chunks, in units: the keys of one step of V^T pieces (16 fp32, 32 bf16, 64 codes).  Four waves, wave w
-// the units w, w + 4, ... of the run with a running maximum and sum per row, merged through LDS at the end.  Scores S[key][row] = K q^T and the output O[dim][row] = V^T P are matrix-core products with the rows as
+// 16 * NT rows against a run of chunks, in units: the keys of one step of V^T pieces (16 fp32, 32 bf16, 64 codes).  W waves (4, or 1: each has an item of its own), wave w
+// the units w, w + W, ... of the run with a running maximum and sum per row, merged through LDS at the end.  Scores S[key][row] = K q^T and the output O[dim][row] = V^T P are matrix-core products with the rows as
 // columns (see asd_attn.h); a unit's fragments go from memory into registers ahead of their use: memory-bound while the rows are few.
 // 8 bits: K is widened with its scale, V without: V's scales go into the probabilities, one value per key.
 // One token of 48 sequences of 500 to 8192 tokens, 64 / 8 heads x 128, 8 bits: 85 us, with the join 5.5 TB/s.  A batch too small for memory to
 // bound it waits for its loads, 1.7 us for each unit of a wave: five rows of eight sequences of up to 1031 tokens, 40 heads, 16 us.
-template <class A, class C, int H, int NT, int SEES, class Args> __device__ __forceinline__ void kv_few_rows(const Args& a, const KvItem& item, KvFewLds<H>& sh) {
+template <class A, class C, int H, int NT, int SEES, int W, class Args> __device__ __forceinline__ void kv_few_rows(const Args& a, const KvItem& item, KvFewLds<H>& sh) {
     using L = KvLayout<C, H>;
     using E = typename A::elem;
     constexpr int AE = A::KE, KK = L::KK, HP = L::HP, US = KK / AE, QS = HP * US;      // operand steps of a K piece, of a row
     constexpr int HT = L::HT, KST = L::KST, VS = L::KV / AE;                           // ... of a V^T piece
     constexpr int UPC = KV_UNITS(C), UK = 64 / UPC, KT = 4 / UPC, KSU = KST / UPC, PS = KSU * VS;      // units of a chunk; keys, score tiles, V^T pieces, steps of a unit
-    const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), g = lane >> 4, m = lane & 15;
+    const int tid = threadIdx.x, lane = tid & 63, w = W == 1 ? 0 : uniform(tid >> 6), g = lane >> 4, m = lane & 15;
     const KvItem it = item.scalar();
     const int seq = it.seq, kvh = it.kvh, tile = it.tile, split = it.split, per = it.per, n_kv = a.kv.n_kv;
     const KvSeq s = it.s;
-    if (tid == 0) sh.odd = 0;
+    if (W > 1 && tid == 0) sh.odd = 0;
     const int rows = s.n * a.kv.group, base = s.len - s.n;
     int pos[NT];                                        // last key of this lane's rows (-1: no such row, or none)
     u32x4 qf[NT][QS];
@@ -209,7 +209,7 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
     // the first unit from u on that has a page, and where it is; one without counts as hidden
     const char *at_k = nullptr, *at_v = nullptr;
     auto next = [&](int u) {
-        for (; u < u_end; u += 4) {
+        for (; u < u_end; u += W) {
             const int r = steps.at(u), c = r / UPC, i = c / cpp;
             int page;
             if (TWO && u < steps.first) {
@@ -364,7 +364,7 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
         Unit f0, f1;
         auto ask = [&](Unit& f) { ask_k(f, at_k); ask_v(f, at_v); };
         auto turn = [&](Unit& now, Unit& then) {
-            const int un = next(unit + 4);
+            const int un = next(unit + W);
             if (un < u_end) ask(then);
             __builtin_amdgcn_sched_barrier(0);
             work(now, unit, [] {});
@@ -380,7 +380,7 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
         Unit f;
         if (unit < u_end) { ask_k(f, at_k); ask_v(f, at_v); }
         while (unit < u_end) {
-            const int un = next(unit + 4);
+            const int un = next(unit + W);
             work(f, unit, [&] { if (un < u_end) ask_k(f, at_k); });
             __builtin_amdgcn_sched_barrier(0);
             if (un < u_end) ask_v(f, at_v);
@@ -389,6 +389,42 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
         }
     }
 
+    // four dims of row r of column block t, unnormalised: the row's maximum and sum of weights; found: something was taken out of V
+    auto put = [&](int t, int r, int d, float (&v)[4], float top, float sum, float inv, bool found) {
+        const int row = (tile * NT + t) * 16 + r, token = row / a.kv.group, head = kvh * a.kv.group + row % a.kv.group;
+        if (row >= rows) return;
+        if (found) {                                     // what the row sees among the item's keys, but for units that all rows see
+            const int end = SEES == KV_SHARED ? from : base + token, row_low = SEES == KV_WINDOW ? end - window + 1 : low;
+            const int main0 = (max(low_last, 0) + UK - 1) / UK * UK, main1 = (from + 1) / UK * UK;
+            const int first_key = steps.at(max(u_begin, steps.first)) * UK, last_key = min(end, (u_end + steps.skip) * UK - 1);
+            for (int j = 0; j < 4; ++j) {
+                v[j] += kv_odd_sum<C, H>(a.kv, seq, kvh, first_key, last_key, d + j, row_low, sinks, main0, main1);
+                if (TWO && u_begin < steps.first)
+                    v[j] += kv_odd_sum<C, H>(a.kv, first_seq, kvh, u_begin * UK, min(min(end, (SEES == KV_BOTH ? low : sinks) - 1), u_end * UK - 1), d + j, 0, 0, 0, SEES == KV_BOTH ? low / UK * UK : 0);
+            }
+        }
+        if (it.whole) {
+            v[0] *= inv; v[1] *= inv; v[2] *= inv; v[3] *= inv;
+            store4<A>((E*)a.out + (s.r0 + (int64_t)token) * a.out_stride + head * H + d, v);
+        } else {
+            const size_t at = (size_t)it.part * (16 * NT) + t * 16 + r;
+            *(float4*)(a.o_part + at * H + d) = float4{v[0], v[1], v[2], v[3]};
+            if (d == 0) { a.ml_part[at * 2] = top; a.ml_part[at * 2 + 1] = sum; }
+        }
+    };
+    if constexpr (W == 1) {                              // an item to each wave: nothing to merge
+        const bool found = __any(odd);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const float sum = groups_sum(l[t]), inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+            for (int ht = 0; ht < HT; ++ht) {
+                float v[4] = {o[t][ht][0], o[t][ht][1], o[t][ht][2], o[t][ht][3]};
+                put(t, m, ht * 16 + 4 * g, v, mx[t], sum, inv, found);
+            }
+        }
+        return;
+    }
     // ---- the waves' results, 16 rows at a time, wave order
     __syncthreads();                                    // (sh.odd is cleared)
     if (odd && lane == 0) sh.odd = 1;
@@ -400,7 +436,7 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
 #pragma unroll
         for (int ht = 0; ht < HT; ++ht) *(f32x4*)&sh.o[w][m][ht * 16 + 4 * g] = o[t][ht];
         __syncthreads();
-        const int r = tid & 15, row = (tile * NT + t) * 16 + r, token = row / a.kv.group, head = kvh * a.kv.group + row % a.kv.group;
+        const int r = tid & 15;
         float top = -INFINITY, sum = 0.f, wt[4];
 #pragma unroll
         for (int ww = 0; ww < 4; ++ww) top = fmaxf(top, sh.ml[ww][r][0]);
@@ -415,25 +451,7 @@ template <class A, class C, int H, int NT, int SEES, class Args> __device__ __fo
                 const f32x4 x = *(const f32x4*)&sh.o[ww][r][d];
                 v[0] += x[0] * wt[ww]; v[1] += x[1] * wt[ww]; v[2] += x[2] * wt[ww]; v[3] += x[3] * wt[ww];
             }
-            if (row >= rows) continue;
-            if (sh.odd) {                                // what the row sees among the item's keys, but for units that all rows see
-                const int end = SEES == KV_SHARED ? from : base + token, row_low = SEES == KV_WINDOW ? end - window + 1 : low;
-                const int main0 = (max(low_last, 0) + UK - 1) / UK * UK, main1 = (from + 1) / UK * UK;
-                const int first_key = steps.at(max(u_begin, steps.first)) * UK, last_key = min(end, (u_end + steps.skip) * UK - 1);
-                for (int j = 0; j < 4; ++j) {
-                    v[j] += kv_odd_sum<C, H>(a.kv, seq, kvh, first_key, last_key, d + j, row_low, sinks, main0, main1);
-                    if (TWO && u_begin < steps.first)
-                        v[j] += kv_odd_sum<C, H>(a.kv, first_seq, kvh, u_begin * UK, min(min(end, (SEES == KV_BOTH ? low : sinks) - 1), u_end * UK - 1), d + j, 0, 0, 0, SEES == KV_BOTH ? low / UK * UK : 0);
-                }
-            }
-            if (it.whole) {
-                v[0] *= inv; v[1] *= inv; v[2] *= inv; v[3] *= inv;
-                store4<A>((E*)a.out + (s.r0 + (int64_t)token) * a.out_stride + head * H + d, v);
-            } else {
-                const size_t at = (size_t)it.part * (16 * NT) + t * 16 + r;
-                *(float4*)(a.o_part + at * H + d) = float4{v[0], v[1], v[2], v[3]};
-                if (d == 0) { a.ml_part[at * 2] = top; a.ml_part[at * 2 + 1] = sum; }
-            }
+            put(t, r, d, v, top, sum, inv, sh.odd != 0);
         }
     }
 }
@@ -456,7 +474,7 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(cons
     it.per = kv_per_split(chunks(it.s), n_splits);
     it.whole = n_splits == 1;
     it.part = blockIdx.x;
-    kv_few_rows<A, C, H, NT, KV_ALL>(a, it, lds);
+    kv_few_rows<A, C, H, NT, KV_ALL, 4>(a, it, lds);
 }
 
 // Many rows (bf16): NW waves with 16 * NT rows each walk a run of chunks together, their fragments in LDS once for all of them.  They come by

@@ -16,8 +16,8 @@ struct AttendPlan {
     size_t o_bytes, bytes;
 };
 // What differs between the forms of attention.  PLAN_CAUSAL: asd_kv_attend, whose sums stay as they are.  PLAN_EVEN: tiles of a batch walk about as many chunks each (a
-// window).  PLAN_BOTH: as causal attention.  PLAN_SMALL: tiles of 16 rows only.
-enum PlanForm { PLAN_CAUSAL, PLAN_EVEN, PLAN_BOTH, PLAN_SMALL };
+// window).  PLAN_BOTH: as causal attention.  PLAN_FRONT: keys that groups share, for the rows of a group.  PLAN_WAVE: an item is a wave's, of 16 rows.
+enum PlanForm { PLAN_CAUSAL, PLAN_EVEN, PLAN_BOTH, PLAN_FRONT, PLAN_WAVE };
 // walk(R): the chunks that tiles of R rows walk at most
 template <class F> AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_batch* b, F walk, PlanForm form = PLAN_CAUSAL) {
     AttendPlan p{};
@@ -39,9 +39,12 @@ template <class F> AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_ba
     // 4000 in all, 64 / 8 heads x 128: 187 us against 269; 8 bits 142 against 135), and codes widened for fp32 products in a batch that fills the card
     // (four prompts of 500, 32 / 32 heads x 128: 186 against 224; with 8 / 8 heads, just below the border, the rule's 63 against 57).
     p.nt = rows <= 16 ? 1 : bf16 ? (!q8 && chunks >= 8 ? 2 : 1) : (q8 && (int64_t)b->n_rows * s->n_heads / 32 >= 2 * units() ? 2 : 1);
-    if (form == PLAN_SMALL) p.rows = false;
+    // Shared keys are read from memory once either way: 128 rows as soon as they are more than two tiles, and the work more than a chunk or two for each compute unit (64 / 8
+    // heads, 8 bits, one token of 64 sequences behind 1000 shared ones: 24 us against 30, behind 4000 32 against 48; five of 8 sequences behind 1000: 19.4 against 17.6)
+    if (form == PLAN_FRONT) p.rows = bf16 && s->head_dim >= 64 && rows > 32 && work * chunks > 12 * (int64_t)units();
+    if (form == PLAN_WAVE) p.rows = false;
     if (p.rows) p.nt = 8;
-    if (form == PLAN_SMALL) p.nt = 1;
+    if (form == PLAN_WAVE) p.nt = 1;
     p.max_tiles = (int32_t)tiles(p.nt);
     chunks = walk(16 * p.nt);
     // Keys are cut into about four items per compute unit (48 sequences of 500 to 8192 tokens: 90 us, with two 100, with eight 97), but not
@@ -54,6 +57,14 @@ template <class F> AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_ba
     const int64_t whole = (int64_t)p.max_tiles * s->n_kv_heads;
     // Fewer tiles than compute units: runs of four chunks are worth their join (a token of one sequence of 8192, window 4096, 32 / 32 heads x 128, bf16 pages: 20 us against 23.5)
     if ((form == PLAN_EVEN || form == PLAN_BOTH) && whole < units()) { p.min_run = 4; p.target = units(); }
+    // Shared keys: runs of 8 chunks (128 rows: 16), shorter ones as long as there are fewer than compute units (sixteen samples of a prompt of 2048 tokens, 32 / 32 heads, bf16
+    // pages: 28.4 us with 16, 25.8 with 8; one token of 16 sequences behind 16000, 64 / 8 heads, 8 bits: 38 with 15, 30 with 8)
+    if (form == PLAN_FRONT) {
+        const int64_t base = p.rows ? 16 : 8, tile = 16 * p.nt, fill = (rows + tile - 1) / tile * seqs * s->n_kv_heads * chunks / units();
+        p.min_run = (int32_t)(fill >= base ? base : fill > 4 ? fill : 4);
+    }
+    // An item that is a wave's: about eight to a compute unit, two chunks each if they are short (the sixteen samples' own 512 tokens and less: 35 us with 16 chunks, 26 with 2)
+    if (form == PLAN_WAVE) { p.min_run = 2; p.target = 8 * units(); }
     const int64_t full = (int64_t)b->n_rows * group / (16 * p.nt) * s->n_kv_heads;
     const int64_t most = (chunks + p.min_run / 2) / p.min_run;      // runs of the longest sequence
     p.join = most > 1 && !(p.rows && (full >= p.target || (whole >= p.target && chunks < 128)));

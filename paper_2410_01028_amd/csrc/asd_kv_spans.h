@@ -136,7 +136,7 @@ template <class A, class C, int H, int NT>
 __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_window_kernel(const KvWindowArgs a, KvNotes* notes) {
     __shared__ KvFewLds<H> lds;
     KvItem it;
-    if (kv_window_item<16 * NT>(a, notes, it, std::false_type{})) kv_few_rows<A, C, H, NT, KV_WINDOW>(a, it, lds);
+    if (kv_window_item<16 * NT>(a, notes, it, std::false_type{})) kv_few_rows<A, C, H, NT, KV_WINDOW, 4>(a, it, lds);
 }
 template <class C, int H, int NT, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void kv_window_rows_kernel(const KvWindowArgs a, KvNotes* notes) {
@@ -289,7 +289,7 @@ template <int R, bool BOTH, class F> __device__ __forceinline__ bool kv_own_item
     kv_place_item(it, local, first, n_tiles, n_kv, F::value);
     it.per = kv_per_split(chunks(it.s), n_splits);
     it.whole = n_splits == 1 && (BOTH || it.s.low == 0);
-    if (!it.whole && it.split == 0 && threadIdx.x >= 192) {
+    if (!it.whole && it.split == 0 && (!BOTH || threadIdx.x >= 192)) {     // (own items are a wave's each)
         KvNote k{.n_own = n_splits};
         if (!BOTH && it.s.low > 0) kv_front_note(a, groups, it, lane, k);
         kv_write_notes(notes, a, it, n_tiles, kv_items_before(a.kv, all, it.seq, lane, joined), lane, k);
@@ -304,10 +304,11 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_apart_kernel(const
     __shared__ __align__(16) char mem[RING > sizeof(KvFewLds<H>) ? RING : sizeof(KvFewLds<H>)];
     KvItem it;
     if (blockIdx.x >= (unsigned)a.front_grid) {
-        if (kv_own_item<16, false>(a, notes, blockIdx.x - a.front_grid, it, std::false_type{})) kv_few_rows<A, C, H, 1, KV_OWN>(a, it, *(KvFewLds<H>*)mem);
+        const int64_t item = (int64_t)(blockIdx.x - a.front_grid) * 4 + uniform(threadIdx.x >> 6);
+        if (kv_own_item<16, false>(a, notes, item, it, std::false_type{})) kv_few_rows<A, C, H, 1, KV_OWN, 1>(a, it, *(KvFewLds<H>*)mem);
     } else if (kv_front_item<16 * FNT>(a, blockIdx.x, it, std::false_type{})) {
         if constexpr (FNT == 8) kv_many_rows<C, H, 2, 4, KV_SHARED>(a.front(), it, *(Ring*)mem);
-        else kv_few_rows<A, C, H, FNT, KV_SHARED>(a.front(), it, *(KvFewLds<H>*)mem);
+        else kv_few_rows<A, C, H, FNT, KV_SHARED, 4>(a.front(), it, *(KvFewLds<H>*)mem);
     }
 }
 // All keys of a sequence, the shared ones through the page table of the group's first
@@ -315,7 +316,7 @@ template <class A, class C, int H, int NT>
 __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_both_kernel(const KvSharedArgs a, KvNotes* notes) {
     __shared__ KvFewLds<H> lds;
     KvItem it;
-    if (kv_own_item<16 * NT, true>(a, notes, blockIdx.x, it, std::false_type{})) kv_few_rows<A, C, H, NT, KV_BOTH>(a, it, lds);
+    if (kv_own_item<16 * NT, true>(a, notes, blockIdx.x, it, std::false_type{})) kv_few_rows<A, C, H, NT, KV_BOTH, 4>(a, it, lds);
 }
 template <class C, int H, int NT, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void kv_both_rows_kernel(const KvSharedArgs a, KvNotes* notes) {

@@ -59,7 +59,11 @@ struct SharedPlan {
 SharedPlan shared_plan(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_groups* g) {
     SharedPlan p{};
     const int64_t chunks = (kv_args(s, b).cap + 63) / 64, group = s->n_heads / s->n_kv_heads;
-    p.apart = (int64_t)b->n_rows * group <= 32 * (int64_t)b->n_seqs;
+    // Apart costs a second launch, and is worth it where the sequences' tiles are not full by themselves (64 rows on average) and, walking both, would read much more than
+    // there is (64 / 8 heads, 8 bits, one token of 64 sequences behind 4000 shared ones: 32 us, walking both 62; of 4 behind 1000: 14.7 and 13.1; 130 rows of 24
+    // sequences: 309 and 272).
+    const int64_t cap = kv_args(s, b).cap, read = b->n_seqs * cap * (int64_t)(asd_kv_page_bytes(s) / s->page_tokens);
+    p.apart = b->n_seqs / 2 >= g->n_groups && b->n_rows * group <= 64 * (int64_t)b->n_seqs && ((cap >= 512 && read >= 40 << 20) || read >= 256 << 20);
     if (!p.apart) {
         p.own = attend_plan(s, b, [=](int) { return chunks + 1; }, PLAN_BOTH);      // (the chunk in which the shared tokens end comes twice)
         p.bytes = p.own.join ? notes_bytes(p.own) + p.own.bytes : 0;
@@ -68,9 +72,9 @@ SharedPlan shared_plan(const asd_kv_shape* s, const asd_kv_batch* b, const asd_k
     }
     asd_kv_batch rows = *b;                             // a group is one sequence to its shared keys
     rows.n_seqs = g->n_groups;
-    rows.max_new = b->n_rows;
-    p.front = attend_plan(s, &rows, [=](int) { return chunks; });
-    p.own = attend_plan(s, b, [=](int) { return chunks; }, PLAN_SMALL);
+    rows.max_new = (b->n_rows + g->n_groups - 1) / g->n_groups;      // (on average: a rule's, no bound)
+    p.front = attend_plan(s, &rows, [=](int) { return chunks; }, PLAN_FRONT);
+    p.own = attend_plan(s, b, [=](int) { return chunks; }, PLAN_WAVE);
     // every tile has a place, cut or not
     for (AttendPlan* x : {&p.front, &p.own}) {
         x->o_bytes = ((size_t)x->grid * 16 * x->nt * s->head_dim * 4 + 255) / 256 * 256;
@@ -148,7 +152,7 @@ int asd_kv_attend_shared(const asd_kv_shape* s, const asd_kv_batch* b, const asd
         using C = decltype(c);
         constexpr bool bf16 = T::KE == 8, q8 = sizeof(typename C::elem) == 1;
         if (p.apart) {
-            const unsigned grid = (unsigned)(p.front.grid + p.own.grid);
+            const unsigned grid = (unsigned)(p.front.grid + (p.own.grid + 3) / 4);
             if (p.front.nt == 1) kv_apart_kernel<T, C, h.value, 1><<<grid, 256, 0, stream>>>(a, notes);
             if constexpr (bf16 != q8) { if (p.front.nt == 2) kv_apart_kernel<T, C, h.value, 2><<<grid, 256, 0, stream>>>(a, notes); }
             if constexpr (bf16 && h.value >= 64) { if (p.front.nt == 8) kv_apart_kernel<T, C, h.value, 8><<<grid, 256, 0, stream>>>(a, notes); }

@@ -1,4 +1,7 @@
-"""Attention of sequences that begin with the same tokens (KVCache.attend_shared) against 64 bits; tolerances: kv_spans_reference.py."""
+"""Attention of sequences that begin with the same tokens (KVCache.attend_shared) against 64 bits; tolerances: kv_spans_reference.py.
+
+`wide`: page tables with room for long sequences (entries that are no pages), for which the shared keys are read apart from the own ones.
+"""
 import math
 
 import pytest
@@ -15,16 +18,27 @@ def i32(x):
     return torch.tensor(x, dtype=torch.int32, device=DEV)
 
 
+def widen(p):
+    """Room for so many tokens that reading all of them for every sequence would be much."""
+    each = asd.kv_page_bytes(p.cache.n_heads, p.cache.n_kv_heads, p.h, p.page, *p.cache._key[4:])
+    n = len(p.lens)
+    width = min(2 ** 24 // p.page, (2 ** 28 // n + each - 1) // each + 1)
+    p.d_table = torch.cat([p.d_table, torch.full((n, max(0, width - p.d_table.shape[1])), -1, dtype=torch.int32, device=DEV)], 1).contiguous()
+    p.cap = p.d_table.shape[1] * p.page
+
+
 class Family:
     """Groups of sequences: (shared tokens, [(new rows, tokens) of its sequences]).  A group's first sequence holds the shared tokens; the others have pages of their
     own from the one on in which these end, with nothing but their own tokens written there."""
 
-    def __init__(self, dtype, kv, heads, kv_heads, h, page, groups, seed=0, spread=0, max_len=None):
+    def __init__(self, dtype, kv, heads, kv_heads, h, page, groups, seed=0, spread=0, max_len=None, wide=False):
         self.news, self.total = [n for _, g in groups for n, _ in g], [t for _, g in groups for _, t in g]
         self.shared, self.first = [s for s, g in groups for _ in g], []
         for _, g in groups:
             self.first += [len(self.first)] * len(g)
         p = self.p = Pool(dtype, kv, heads, kv_heads, h, page, list(zip(self.news, self.total)), seed=seed, max_len=max_len)
+        if wide:
+            widen(p)
         for i, f in enumerate(self.first):
             if f != i:
                 p.d_table[i, :self.shared[i] // page] = p.d_table[f, :self.shared[i] // page]
@@ -66,11 +80,12 @@ FAMILIES = {
 }
 
 
+@pytest.mark.parametrize("wide", [False, True], ids=["", "wide"])
 @pytest.mark.parametrize("dtype,kv", COMBOS)
 @pytest.mark.parametrize("kind", list(FAMILIES))
 @pytest.mark.parametrize("h,heads,kv_heads,page", [(128, 8, 1, 64), (128, 4, 4, 192), (64, 15, 5, 64), (32, 6, 2, 128)])
-def test_families(dtype, kv, kind, h, heads, kv_heads, page):
-    f = Family(dtype, kv, heads, kv_heads, h, page, FAMILIES[kind], seed=h)
+def test_families(dtype, kv, kind, h, heads, kv_heads, page, wide):
+    f = Family(dtype, kv, heads, kv_heads, h, page, FAMILIES[kind], seed=h, wide=wide)
     rows = sum(f.news)
     q = f.p.normal(rows + 2, heads + 3, h, scale=2.0)[:, 1:heads + 1]
     out = torch.full((rows + 2, heads, h), 7.0, dtype=f.p.t, device=DEV)
@@ -78,6 +93,20 @@ def test_families(dtype, kv, kind, h, heads, kv_heads, page):
     f.p.cache.attend_shared(b, f.groups, q, out=out)
     b.check()
     assert bool((out[rows:] == 7.0).all())
+    f.check(q, out)
+
+
+@pytest.mark.parametrize("dtype,kv", COMBOS)
+@pytest.mark.parametrize("h,heads,kv_heads,groups", [(128, 64, 8, [(1000, [(1 + i % 5, 1007 + 11 * i) for i in range(20)]), (2111, [(3, 2114)] * 9)]),
+                                                     (64, 40, 40, [(1500, [(1, 1501)] * 3 + [(4, 1700)] * 20)]), (64, 64, 4, [(65, [(1, 66)]), (3000, [(2, 3002 + i) for i in range(70)])])])
+def test_rows_of_many_sequences_share_a_chunk(dtype, kv, h, heads, kv_heads, groups):
+    """Groups whose rows fill tiles of 128 that go over the borders of sequences."""
+    f = Family(dtype, kv, heads, kv_heads, h, 64, groups, seed=h, wide=True, spread=1013)
+    q = f.p.normal(sum(f.news), heads, h, scale=2.0)
+    b = f.p.batch(f.news, f.total)
+    assert f.p.cache.attend_shared_workspace(b, f.groups) > 0
+    out = f.p.cache.attend_shared(b, f.groups, q)
+    b.check()
     f.check(q, out)
 
 
@@ -109,10 +138,11 @@ def test_long_beginnings(kv, groups):
     f.check(q, out)
 
 
+@pytest.mark.parametrize("wide", [False, True], ids=["", "wide"])
 @pytest.mark.parametrize("dtype,kv", COMBOS)
 @pytest.mark.parametrize("kv_heads,kind", [(2, "samples"), (2, "drafts"), (2, "requests"), (64, "requests")])
-def test_values_that_are_not_finite_stay_where_they_are_seen(dtype, kv, kv_heads, kind):
-    f = Family(dtype, kv, 2 * kv_heads, kv_heads, 64, 64, FAMILIES[kind], seed=2, spread=23)
+def test_values_that_are_not_finite_stay_where_they_are_seen(dtype, kv, kv_heads, kind, wide):
+    f = Family(dtype, kv, 2 * kv_heads, kv_heads, 64, 64, FAMILIES[kind], seed=2, spread=23, wide=wide)
     q = f.p.normal(sum(f.news), 2 * kv_heads, 64)
     b = f.p.batch(f.news, f.total)
     out = f.p.cache.attend_shared(b, f.groups, q)
@@ -120,10 +150,11 @@ def test_values_that_are_not_finite_stay_where_they_are_seen(dtype, kv, kv_heads
     f.check(q, out)
 
 
-def test_more_groups_and_sequences_than_a_wave_looks_at():
-    groups = [((g * 37) % 200, [(1 + (g + i) % 2, (g * 37) % 200 + 2 + (i * 13) % 90) for i in range(g % 5)]) for g in range(150)]
-    f = Family("bf16", "fp8", 4, 2, 64, 64, groups, seed=4)
-    assert len(f.news) > 256
+@pytest.mark.parametrize("wide", [False, True], ids=["", "wide"])
+def test_more_groups_and_sequences_than_a_wave_looks_at(wide):
+    groups = [((g * 37) % 200, [(1 + (g + i) % 2, (g * 37) % 200 + 2 + (i * 13) % 90) for i in range(g % 6)]) for g in range(150)]
+    f = Family("bf16", "fp8", 4, 2, 64, 64, groups, seed=4, wide=wide)
+    assert len(f.news) > 2 * len(groups)
     q = f.p.normal(sum(f.news), 4, 64)
     b = f.p.batch(f.news, f.total)
     out = f.p.cache.attend_shared(b, f.groups, q)
@@ -131,8 +162,9 @@ def test_more_groups_and_sequences_than_a_wave_looks_at():
     f.check(q, out)
 
 
-def test_one_group_of_more_sequences_than_a_wave_looks_at():
-    f = Family("bf16", "bf16", 8, 2, 64, 64, [(70, [(1, 71)] * 3), (500, [(1, 501 + i) for i in range(200)]), (90, [(2, 200)] * 70)], seed=5)
+@pytest.mark.parametrize("wide", [False, True], ids=["", "wide"])
+def test_one_group_of_more_sequences_than_a_wave_looks_at(wide):
+    f = Family("bf16", "bf16", 8, 2, 64, 64, [(70, [(1, 71)] * 3), (500, [(1, 501 + i) for i in range(200)]), (90, [(2, 200)] * 70)], seed=5, wide=wide)
     q = f.p.normal(sum(f.news), 8, 64)
     b = f.p.batch(f.news, f.total)
     out = f.p.cache.attend_shared(b, f.groups, q)
@@ -140,12 +172,13 @@ def test_one_group_of_more_sequences_than_a_wave_looks_at():
     f.check(q, out)
 
 
-def test_sequences_in_no_group():
+@pytest.mark.parametrize("wide", [False, True], ids=["", "wide"])
+def test_sequences_in_no_group(wide):
     """Groups of a few of the sequences: the others in front, between and behind take their own pages."""
-    f = Family("bf16", "fp8", 8, 2, 64, 64, [(100, [(1, 130)]), (200, [(2, 202), (1, 300)]), (50, [(3, 80)]), (64, [(1, 90), (1, 70)])], seed=6)
+    f = Family("bf16", "fp8", 8, 2, 64, 64, [(100, [(1, 130)]), (200, [(2, 202), (1, 300)]), (50, [(3, 80)]), (64, [(1, 90), (1, 70)])], seed=6, wide=wide)
     q = f.p.normal(sum(f.news), 8, 64)
     b = f.p.batch(f.news, f.total)
-    for start, shared in (([1, 3], [200]), ([1, 3, 3, 3], [200, 9, 7]), ([1, 3, 4, 6], [200, 50, 64])):
+    for start, shared in (([1, 3], [200]), ([1, 3, 3], [200, 9]), ([1, 3, 3, 3], [200, 9, 7]), ([1, 3, 4, 6], [200, 50, 64])):
         out = f.p.cache.attend_shared(b, asd.KVGroups(i32(start), i32(shared)), q)
         b.check()
         rows = slice(1, 4)
@@ -161,12 +194,15 @@ BAD = {"descends": ([0, 4, 2, 6], [130, 130, 130]), "begins in front": ([-3, 2, 
        "claimed twice": ([0, 6, 0, 6], [130, 130, 130]), "far away": ([2 ** 31 - 1, -2 ** 31, 2, 4], [130, 130, 130]), "lengths": ([0, 2, 4, 6], [-5, 2 ** 31 - 1, 130])}
 
 
+@pytest.mark.parametrize("wide", [False, True], ids=["", "wide"])
 @pytest.mark.parametrize("dtype,kv", [("bf16", "fp8"), ("f32", "f32")])
 @pytest.mark.parametrize("kind", list(BAD))
-def test_groups_out_of_range_are_cut_and_reported(kind, dtype, kv):
+def test_groups_out_of_range_are_cut_and_reported(kind, dtype, kv, wide):
     """Sequences that hold all their tokens in pages of their own: whatever the groups say, each sequence's answer is that of its tokens."""
     lens = [(1, 200), (2, 300), (1, 131), (3, 400), (1, 150), (2, 170)]
     p = Pool(dtype, kv, 8, 2, 64, 64, lens, seed=7)
+    if wide:
+        widen(p)
     news, total = [a for a, _ in lens], [b for _, b in lens]
     k, v = p.normal(400, 2, 64), p.normal(400, 2, 64)
     own = [p.normal(300, 2, 64) for _ in range(12)]
@@ -186,10 +222,11 @@ def test_groups_out_of_range_are_cut_and_reported(kind, dtype, kv):
 
 @pytest.mark.parametrize("start,lens", [([0, 3, 1, 6, 8], [200, 210, 220, 230]), ([0, 2, 4, 6, 2 ** 31 - 1], [200, 200, 200, 200]), ([-9, 2, 4, 6, 8], [200, 200, 200, 200]),
                                         ([0, 8, 0, 8, 8], [200, 200, 200, 200]), ([0, 2, 4, 6, 8], [2 ** 31 - 1, 1, -3, 200]), ([5, 4, 3, 2, 1], [200, 200, 200, 200])])
-def test_rows_out_of_range_are_cut_and_reported(start, lens):
+@pytest.mark.parametrize("wide", [False, True], ids=["", "wide"])
+def test_rows_out_of_range_are_cut_and_reported(start, lens, wide):
     """Rows that are claimed twice, cut or out of range beside groups: every answer is finite, rows that belong to no sequence stay as they are."""
-    f = Family("bf16", "fp8", 8, 2, 64, 64, [(130, [(2, 200), (2, 200)]), (64, [(2, 200), (2, 200)])], seed=8)
-    b = asd.KVBatch(f.p.d_table, i32(start), i32(lens), 8, 3, 200)
+    f = Family("bf16", "fp8", 8, 2, 64, 64, [(130, [(2, 200), (2, 200)]), (64, [(2, 200), (2, 200)])], seed=8, wide=wide)
+    b = asd.KVBatch(f.p.d_table, i32(start), i32(lens), 8, 3, f.p.cap if wide else 200)
     q = f.p.normal(8, 8, 64)
     ref = f.p.cache.attend(b, q, out=torch.full_like(q, 7.0))
     out = f.p.cache.attend_shared(b, f.groups, q, out=torch.full_like(q, 7.0))
@@ -198,8 +235,9 @@ def test_rows_out_of_range_are_cut_and_reported(start, lens):
     assert torch.equal((out == 7.0).all(-1), (ref == 7.0).all(-1))
 
 
-def test_pages_out_of_range_are_hidden_and_reported():
-    f = Family("bf16", "bf16", 4, 2, 64, 64, [(200, [(1, 201), (2, 300), (1, 270)])], seed=9)
+@pytest.mark.parametrize("wide", [False, True], ids=["", "wide"])
+def test_pages_out_of_range_are_hidden_and_reported(wide):
+    f = Family("bf16", "bf16", 4, 2, 64, 64, [(200, [(1, 201), (2, 300), (1, 270)])], seed=9, wide=wide)
     q = f.p.normal(4, 4, 64)
     b = f.p.batch(f.news, f.total)
     for seq, page, hidden in ((0, 1, [0, 1, 2]), (1, 4, [1])):
@@ -219,11 +257,14 @@ def test_pages_out_of_range_are_hidden_and_reported():
         f.p.d_table[seq, page] = keep
 
 
-def test_a_fork_inside_a_page_goes_on_by_itself():
+@pytest.mark.parametrize("wide", [False, True], ids=["", "wide"])
+def test_a_fork_inside_a_page_goes_on_by_itself(wide):
     """A conversation is continued three ways: each way writes its own tokens from inside the page in which the common ones end, attends, and grows; the common
     tokens stay as they are.  In the end drafts for all of them are verified together."""
     h, heads, kv_heads, common = 64, 8, 2, 100
     p = Pool("bf16", "fp8", heads, kv_heads, h, 64, [(common, 300), (1, 300), (1, 300)], seed=10)
+    if wide:
+        widen(p)
     p.d_table[1:, :1] = p.d_table[0, :1]
     k, v = [p.normal(common, kv_heads, h)], [p.normal(common, kv_heads, h)]
     prompt = p.batch([common, 0, 0], [common, 0, 0])
@@ -246,18 +287,20 @@ def test_a_fork_inside_a_page_goes_on_by_itself():
             at += n
 
 
-@pytest.mark.parametrize("kind", ["tokens", "drafts", "many"])
-def test_a_captured_call_follows_lengths_and_groups(kind):
+@pytest.mark.parametrize("kind,wide", [("tokens", False), ("tokens", True), ("drafts", False), ("drafts", True), ("many", False)])
+def test_a_captured_call_follows_lengths_and_groups(kind, wide):
     """Captured once, replayed with other lengths, groups and shared tokens, with eager work between: the eager call's bits; the answer in the queries' place."""
     news, heads, kv_heads = {"tokens": ([1] * 6, 16, 2), "drafts": ([6, 5, 1, 5, 2, 6], 8, 2), "many": ([130, 70, 1, 30, 40, 90], 64, 64)}[kind]
     longest = 2500
     p = Pool("bf16", "fp8", heads, kv_heads, 64, 64, [(n, longest) for n in news], seed=13)
     k, v = p.fill()
+    if wide:
+        widen(p)
     p.d_table[1:, :15] = p.d_table[0, :15]
     k, v = ([torch.cat([x[0][:960], y[960:]]) for y in x] for x in (k, v))
     b, groups = p.batch(news, news), asd.KVGroups(i32([0, 6, 6]), i32([0, 0]))
     q = p.normal(sum(news), heads, 64)
-    ws = torch.empty(p.cache.attend_shared_workspace(b, groups), dtype=torch.uint8, device=DEV)
+    ws = torch.empty(max(p.cache.attend_shared_workspace(b, groups), 256), dtype=torch.uint8, device=DEV)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
