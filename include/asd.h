@@ -485,8 +485,8 @@ int asd_kv_attend_window(const asd_kv_shape* s, const asd_kv_batch* b, int32_t w
  * prompt): these keys are read once for all rows of a group.  Group g is the sequences group_start[g] .. group_start[g+1]-1; sequences may be in no
  * group.  The keys 0 .. shared_len[g]-1 of its sequences are those of its FIRST sequence, read through that one's page table; the keys behind
  * them are each sequence's own, read through its own.  So a sequence can leave a common beginning anywhere, inside a page too: its
- * page there holds its own tokens only, and nothing is copied.  A sequence of which some new row does not lie behind the shared tokens
- * (kv_len - new rows < shared_len) is read through its own table altogether, as is one in no group.
+ * page there holds its own tokens only, and nothing is copied.  A sequence is read through its own table altogether where it is in no group, where some new row
+ * does not lie behind the shared tokens (kv_len - new rows < shared_len), and where the group's first sequence has fewer tokens than them.
  * group_start outside 0 .. n_seqs or descending: no sequence belongs to two groups, a group that begins in front of the end of an earlier one has none
  * (ASD_KV_BAD_GROUP).  A group whose rows are not in order (ASD_KV_BAD_ROWS) may be taken as if its sequences were in none.
  */

@@ -71,7 +71,7 @@ template <class F> AttendPlan attend_plan(const asd_kv_shape* s, const asd_kv_ba
     // kv_many_rows' tiles are few and long beside the two that a compute unit works on at a time.  Those that fill whole rounds stay whole; the rest are cut so that they fill
     // one more (512 rows behind 8195 tokens and 260 behind 2665, 64 / 8 heads, 8 bits, window 2048, 392 tiles: 110 us with all tiles cut, 92 so; 24 questions behind system
     // prompts of 4000, 2756 and 2976 tokens, 2.2 rounds: 307 us with none cut, 272 so).
-    if (p.rows && (form == PLAN_EVEN || (form == PLAN_BOTH && !p.join))) {
+    if (p.rows && ((form == PLAN_EVEN && chunks < 128) || ((form == PLAN_EVEN || form == PLAN_BOTH) && !p.join))) {
         p.target = 2 * units();
         p.tail = (int32_t)(chunks / 8 < 1 ? 1 : chunks / 8 < p.target ? chunks / 8 : p.target);
         p.join = p.tail > 1;

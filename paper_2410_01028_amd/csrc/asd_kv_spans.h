@@ -120,7 +120,7 @@ template <int R, class F> __device__ __forceinline__ bool kv_window_item(const K
     KvLanes all;
     all.load(a.kv, 0, lane, check);
     auto chunks = [&](const KvSeq& v) { return kv_window_chunks(a, v, R); };
-    if constexpr (F::value) return kv_tail_item<R>(a, notes, all, blockIdx.x, lane, check, it, chunks);
+    if (F::value && a.tail) return kv_tail_item<R>(a, notes, all, blockIdx.x, lane, check, it, chunks);
     const int run = kv_run_all(a, all, lane, R, chunks);
     auto joined = [&](const KvSeq& v) { return kv_splits(chunks(v), run) > 1 ? kv_tiles_of(a.kv, v, 16) : 0; };
     if (check && a.cut) kv_count_notes(notes, a.kv, all, lane, joined);
@@ -179,32 +179,33 @@ struct KvGroupLanes {
         const int g = min(g0 + lane, a->n_groups - 1);
         s0 = a->group_start[g]; s1 = a->group_start[g + 1]; len = a->shared_len[g];
     }
-    // begin(s), of all lanes at once: row_start[s]
-    template <class F> __device__ __forceinline__ void take(const KvArgs& kv, int g0, int lane, bool check, F begin) {
+    // begin(s), tokens(s), of all lanes at once: row_start[s], kv_len[s]
+    template <class F, class G> __device__ __forceinline__ void take(const KvArgs& kv, int g0, int lane, bool check, F begin, G tokens) {
         const bool on = g0 + lane < a->n_groups;
         const int before = kv_max_before(on ? min(max(s1, 0), kv.n_seqs) : 0, top_f, lane);
         const bool order = s0 >= before && s1 >= s0 && s1 <= kv.n_seqs;
         f0 = !on ? 0x7fffffff : order ? s0 : before;
         f1 = on && order ? s1 : f0;
-        const int shared = min(max(len, 0), kv.cap), r0 = begin(f1 > f0 ? f0 : 0), r1 = begin(f1 > f0 ? f1 : 0);
-        v = KvSeq{f1 > f0 ? min(max(r0, 0), kv.n_rows) : 0, 0, shared};
+        const int shared = min(max(len, 0), kv.cap), r0 = begin(f1 > f0 ? f0 : 0), r1 = begin(f1 > f0 ? f1 : 0), held = tokens(f1 > f0 ? f0 : 0);
+        v = KvSeq{f1 > f0 ? min(max(r0, 0), kv.n_rows) : 0, 0, held < shared ? 0 : shared};      // (the first one has to hold them)
         const int end = f1 > f0 ? min(max(r1, 0), kv.n_rows) : 0;
         v.n = v.r0 >= kv_max_before(end, top_h, lane) ? max(end - v.r0, 0) : 0;
         if (check && on && (!order || shared != len)) kv_flag(kv, ASD_KV_BAD_GROUP);
     }
     __device__ __forceinline__ void load(const KvArgs& kv, int g0, int lane, bool check) {
         ask(g0, lane);
-        take(kv, g0, lane, check, [&](int s) { return kv.row_start[s]; });
+        take(kv, g0, lane, check, [&](int s) { return kv.row_start[s]; }, [&](int s) { return kv.kv_len[s]; });
     }
     // the first 64; with up to 64 sequences their beginnings are asked for along with the groups
     __device__ __forceinline__ void begin(const KvArgs& kv, int lane, bool check) {
         ask(0, lane);
-        if (kv.n_seqs > 64) return take(kv, 0, lane, check, [&](int s) { return kv.row_start[s]; });
-        const int s = min(lane, kv.n_seqs - 1), r0 = kv.row_start[s], r1 = kv.row_start[s + 1];
-        take(kv, 0, lane, check, [&](int at) { const int x = __shfl(r0, min(at, 63)), y = __shfl(r1, max(at - 1, 0)); return at < kv.n_seqs ? x : y; });
+        if (kv.n_seqs > 64) return take(kv, 0, lane, check, [&](int s) { return kv.row_start[s]; }, [&](int s) { return kv.kv_len[s]; });
+        const int s = min(lane, kv.n_seqs - 1), r0 = kv.row_start[s], r1 = kv.row_start[s + 1], n = kv.kv_len[s];
+        take(kv, 0, lane, check, [&](int at) { const int x = __shfl(r0, min(at, 63)), y = __shfl(r1, max(at - 1, 0)); return at < kv.n_seqs ? x : y; }, [&](int at) { return __shfl(n, at); });
     }
 };
-// The sequences, with the first key of their own (v.low): 0 where a sequence is in no group, or has a new row that does not lie behind the shared tokens
+// The sequences, with the first key of their own (v.low): 0 where a sequence is in no group, or has a new row that does not lie behind the shared tokens, or
+// where the group's first sequence does not hold them
 struct KvOwnLanes : KvLanes {
     KvGroupLanes groups;                                // (the first 64)
     __device__ __forceinline__ KvOwnLanes(const KvGroupLanes& g) : groups(g) {}
@@ -282,13 +283,14 @@ template <int R, bool BOTH, class F> __device__ __forceinline__ bool kv_own_item
     if (F::value && a.tail) return kv_tail_item<R>(a, notes, all, item, lane, check, it, chunks);
     const int run = kv_run_all(a, all, lane, R, chunks);
     auto count = [&](const KvSeq& v) { return kv_tiles_of(a.kv, v, R) * kv_splits(chunks(v), run) * n_kv; };
-    auto joined = [&](const KvSeq& v) { return kv_splits(chunks(v), run) > 1 || (!BOTH && v.low > 0) ? kv_tiles_of(a.kv, v, 16) : 0; };
+    // (Apart, all rows are joined: one that shares nothing may lie in a tile of those that do, whose queries must not change while the tile is at work: `out` may be `q`.)
+    auto joined = [&](const KvSeq& v) { return !BOTH || kv_splits(chunks(v), run) > 1 ? kv_tiles_of(a.kv, v, 16) : 0; };
     if (check && (!BOTH || a.cut)) kv_count_notes(notes, a.kv, all, lane, joined);
     if (!kv_find(a.kv, all, item, lane, check, count, &it.seq, &local, &first, &it.s)) return false;
     const int n_splits = kv_splits(chunks(it.s), run), n_tiles = kv_tiles_of(a.kv, it.s, R);
     kv_place_item(it, local, first, n_tiles, n_kv, F::value);
     it.per = kv_per_split(chunks(it.s), n_splits);
-    it.whole = n_splits == 1 && (BOTH || it.s.low == 0);
+    it.whole = BOTH && n_splits == 1;
     if (!it.whole && it.split == 0 && (!BOTH || threadIdx.x >= 192)) {     // (own items are a wave's each)
         KvNote k{.n_own = n_splits};
         if (!BOTH && it.s.low > 0) kv_front_note(a, groups, it, lane, k);

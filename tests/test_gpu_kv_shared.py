@@ -190,6 +190,32 @@ def test_sequences_in_no_group(wide):
         assert bool(out[rows].isfinite().all())
 
 
+@pytest.mark.parametrize("wide", [False, True], ids=["", "wide"])
+def test_rows_that_share_nothing_beside_others_and_answers_in_place(wide):
+    """A group of sequences some of which do not reach behind the shared tokens, one whose first sequence does not hold them; the answer takes the queries' place, twice over: the
+    same bits."""
+    lens = [(2, 900), (1, 700), (1, 901), (5, 640), (2, 1000), (1, 100), (1, 800), (2, 650)]
+    p = Pool("bf16", "fp8", 64, 8, 64, 64, lens, seed=15)
+    if wide:
+        widen(p)
+    k, v = p.fill()
+    p.d_table[1:5, :10] = p.d_table[0, :10]
+    k, v = ([x[0]] + [torch.cat([x[0][:640], y[640:]]) for y in x[1:5]] + list(x[5:]) for x in (k, v))
+    news, total = [a for a, _ in lens], [b for _, b in lens]
+    b, groups = p.batch(news, total), asd.KVGroups(i32([0, 5, 8]), i32([640, 640]))
+    q = p.normal(sum(news), 64, 64, scale=2.0)
+    apart = p.cache.attend_shared(b, groups, q)
+    at = 0
+    for i, (n, t) in enumerate(lens):
+        check("bf16", q[at:at + n], apart[at:at + n], k[i], v[i], in_window(torch.arange(t - n, t, device=DEV), t, 2 ** 30, 0), 0.125, f"sequence {i}")
+        at += n
+    for _ in range(4):
+        mine = q.clone()
+        assert p.cache.attend_shared(b, groups, mine, out=mine) is mine
+        assert torch.equal(mine, apart)
+    b.check()
+
+
 BAD = {"descends": ([0, 4, 2, 6], [130, 130, 130]), "begins in front": ([-3, 2, 4, 6], [130, 130, 130]), "ends behind": ([0, 2, 4, 2 ** 31 - 1], [130, 130, 130]),
        "claimed twice": ([0, 6, 0, 6], [130, 130, 130]), "far away": ([2 ** 31 - 1, -2 ** 31, 2, 4], [130, 130, 130]), "lengths": ([0, 2, 4, 6], [-5, 2 ** 31 - 1, 130])}
 
