@@ -698,7 +698,8 @@ class KVCache(_Fixed):
     def attend_window(self, batch: KVBatch, q, window: int, sinks: int = 0, out=None, scale: float | None = None, workspace=None):
         """attend() with a sliding window (asd_kv_attend_window): a row sees the last `window` tokens up to its own, and the first `sinks` tokens of
         its sequence.  Pages that hold neither are not read.  workspace: attend_window_workspace(batch, window, sinks) bytes."""
-        _fits(window=window, sinks=sinks)
+        if not (0 < window < 1 << 31 and 0 <= sinks < 1 << 31):
+            raise AsdError(E_INVAL, f"window {window}, sinks {sinks}: a positive number and one of 0 or more, of 31 bits")
         return self._attend(self._lib.asd_kv_attend_window, self._lib.asd_kv_attend_window_workspace, batch, (window, sinks), (self._key, window, sinks), q, out, scale, workspace)
 
     def attend_window_workspace(self, batch: KVBatch, window: int, sinks: int = 0) -> int:

@@ -268,3 +268,60 @@ def test_refusals_of_the_binding():
     for bad in (q.float(), q[:1], q.cpu()):
         with pytest.raises(asd.AsdError):
             p.cache.attend_window(b, bad, 4)
+
+
+@pytest.mark.parametrize("dtype,kv", COMBOS)
+def test_a_long_conversation_in_a_few_pages(dtype, kv):
+    """Prompt, drafts and tokens appended and attended to with a window, the pages behind it given to the tokens that come: five pages hold two conversations that would
+    take sixteen."""
+    h, heads, kv_heads, page, window, sinks = 64, 8, 2, 64, 70, 5
+    args = (heads, kv_heads, h, page, asd.DT_BF16 if dtype == "bf16" else asd.DT_F32, {"f32": asd.DT_F32, "bf16": asd.DT_BF16, "fp8": asd.DT_FP8}[kv])
+    cache = asd.KVCache(torch.full((10 * asd.kv_page_bytes(*args),), 0x7F, dtype=torch.uint8, device=DEV), *args)
+    t = cache.torch_dtype
+    gen = torch.Generator(DEV).manual_seed(3)
+    normal = lambda *shape: torch.randn(*shape, generator=gen, device=DEV).to(t)      # noqa: E731
+    table = torch.full((2, 16), -1, dtype=torch.int32, device=DEV)
+    rope = asd.rope_table(h, 1024)
+    free, mine, lens, kept = [[0, 1, 2, 3, 4], [5, 6, 7, 8, 9]], [{}, {}], [0, 0], [([], []), ([], [])]
+    for news in [[90, 33]] + [[5, 1], [1, 5]] * 30 + [[64, 100]] + [[1, 1]] * 40 + [[128, 100]]:
+        for i in range(2):
+            first = max(0, lens[i] - window + 1)        # the first key of the next row's window
+            for j in [j for j in mine[i] if j and (j + 1) * page <= first]:
+                free[i].append(mine[i].pop(j))
+                table[i, j] = -1
+            lens[i] += news[i]
+            for j in range((lens[i] + page - 1) // page):
+                if j not in mine[i] and (j + 1) * page > lens[i] - news[i]:
+                    mine[i][j] = free[i].pop(0)
+                    table[i, j] = mine[i][j]
+        b = asd.KVBatch(table, torch.tensor([0, news[0], sum(news)], dtype=torch.int32, device=DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), sum(news), max(news), 1024)
+        q = cache.append(b, normal(sum(news), heads, h), normal(sum(news), kv_heads, h), normal(sum(news), kv_heads, h), rope=rope, rot_dim=h)
+        got = cache.read(b)
+        out = cache.attend_window(b, q, window, sinks)
+        b.check()
+        at = 0
+        for i, n in enumerate(news):
+            for x, y in zip(kept[i], got):
+                x.append(y[at:at + n])
+            k, v = (torch.cat(x) for x in kept[i])
+            pos = torch.arange(lens[i] - n, lens[i], device=DEV)
+            check(dtype, q[at:at + n], out[at:at + n], k, v, in_window(pos, lens[i], window, sinks), h ** -0.5, f"conversation {i} at {lens[i]}")
+            at += n
+    assert min(lens) > 400 and max(len(x) for x in mine) <= 5
+
+
+def test_an_engines_cache():
+    """New rows attend to a window of what an engine's prompt pass has left in its pages."""
+    import asd_inputs as si
+    tiny = si.SHAPES["tiny"]
+    eng = asd.Engine(asd.make_config(tiny, 256, page_tokens=64)).init_synthetic(0)
+    eng.prefill(si.prompt(0, 200, tiny.vocab))
+    k, v = (torch.from_numpy(x).cuda() for x in eng.get_kv(1, 0, 200))
+    cache, table = eng.kv_cache(1)
+    b = asd.KVBatch(table, torch.tensor([0, 3], dtype=torch.int32, device=DEV), torch.tensor([200], dtype=torch.int32, device=DEV), 3, 3, 256)
+    q = torch.randn(3, tiny.n_heads, tiny.head_dim, generator=torch.Generator(DEV).manual_seed(1), device=DEV)
+    out = cache.attend_window(b, q, 50, 4)
+    b.check()
+    pos = torch.arange(197, 200, device=DEV)
+    check("f32", q, out, k.view(200, tiny.n_kv_heads, -1), v.view(200, tiny.n_kv_heads, -1), in_window(pos, 200, 50, 4), tiny.head_dim ** -0.5, "engine")
+    eng.close()
