@@ -62,7 +62,7 @@ struct KvPages {
 };
 // How a batch is cut.  The rows of a sequence and KV head are its new tokens x the heads of the group; a tile is 16 * NT of
 // them.  With `cut`, all tiles' key ranges are cut into runs of `run` chunks, the same for every sequence, so that about `target` items come out
-// whatever the lengths are: one long conversation among short ones is spread over the card.  (attend_plan in asd_kv.hip says which batches are cut.)
+// whatever the lengths are: one long conversation among short ones is spread over the card.  (attend_plan in asd_kv_plan.h says which batches are cut.)
 template <int NT> __device__ __forceinline__ int kv_tiles(const KvArgs& a, const KvSeq& v) { return (int)(((uint32_t)v.n * a.group + 16 * NT - 1) / (16 * NT)); }      // (n_rows * n_h is below 2^31)
 __device__ __forceinline__ int kv_run_of(const KvAttendArgs& a, int64_t t) {      // t: chunks of all tiles of a KV head
     const int run = (int)fminf((float)(t * a.kv.n_kv) / (float)a.target, 1e8f) + 1;
@@ -129,8 +129,11 @@ template <int H> struct alignas(16) KvFewLds {
 // the units w, w + W, ... of the run with a running maximum and sum per row, merged through LDS at the end.  Scores S[key][row] = K q^T and the output O[dim][row] = V^T P are matrix-core products with the rows as
 // columns (see asd_attn.h); a unit's fragments go from memory into registers ahead of their use: memory-bound while the rows are few.
 // 8 bits: K is widened with its scale, V without: V's scales go into the probabilities, one value per key.
-// One token of 48 sequences of 500 to 8192 tokens, 64 / 8 heads x 128, 8 bits: 85 us, with the join 5.5 TB/s.  A batch too small for memory to
-// bound it waits for its loads, 1.7 us for each unit of a wave: five rows of eight sequences of up to 1031 tokens, 40 heads, 16 us.
+// One token of 48 sequences of 500 to 8192 tokens, 64 / 8 heads x 128, 8 bits: 84 us, with the join 5.6 TB/s.  A batch too small for memory to
+// bound it waits for its loads, 1.7 us for each unit of a wave: five rows of eight sequences of up to 1031 tokens, 40 heads, 16 us.  Around them about 5 us: a launch,
+// 1.7 us until a wave knows its item (lengths, sums over them), 1 for the pages, 2 for the merge.
+// With a window (KV_WINDOW) that is all that is left of the length: the 48 sequences with the last 1024 tokens and the first 4 27 us (bf16 pages 40, 5.0 TB/s).
+// A wave to an item (W = 1) leaves the merge and its LDS out, for short runs beside other work (the own keys of sequences that share the others).
 template <class A, class C, int H, int NT, int SEES, int W, class Args> __device__ __forceinline__ void kv_few_rows(const Args& a, const KvItem& item, KvFewLds<H>& sh) {
     using L = KvLayout<C, H>;
     using E = typename A::elem;
@@ -481,10 +484,14 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(cons
 // direct loads into a ring of five half-chunks (K, V^T, K, ..): one barrier per chunk c, behind which K and V^T of c have landed
 // and the slots of c - 1 may be asked for anew (V^T of c + 1, K of c + 2).  A SIMD has two waves.
 // (Prompts of 1035 to 2048 tokens, 32 heads x 128, bf16 pages, took 160 us so at the step when four waves of 16 rows took 199 and two waves with the
-// next product's fragments in registers 200, both spilling.)  Bound by products and exponentials (in 8 bits the widening, too, which each
-// wave does for itself) one after the other: the vector unit issues in 53 % of the busy cycles (8 bits 73), the matrix cores are at work in 38 (37),
-// little of it at the same time; and by what each tile takes once.  These prompts now take 137 to 143 us (8-bit pages 156), 720 to 750 TFLOP/s,
-// one of 8192 tokens 1001 TFLOP/s (944); 512 rows behind 8195 tokens and 260 behind 2665 in 8 bits, 64 / 8 heads, 214 us with the join.
+// next product's fragments in registers 200, both spilling.)  Bound by products, exponentials (in 8 bits the widening, too, which each wave does for itself) and the
+// fragments' way out of LDS, each of them about 2000 cycles of a compute unit for a step of two workgroups (bf16 pages), which takes 2900 (8 bits 3400 to 4000; one
+// workgroup alone 3300): the vector unit issues in 48 to 53 % of the busy cycles (8 bits 73 to 76), the matrix cores are at work in 33 to 38.  And by what each tile takes
+// once, about 10000 cycles in front (its item, the page table, queries, first fragments) and 4000 behind; a step with an edge takes 5000: the chunk's V^T is looked
+// through, and rows are masked on the side on which some see less.  (7600 with a mask of three comparisons per score and V^T written back always, behind a barrier of its own:
+// prompts of 4096, 3575, 2070 and 2547 tokens, window 1024: 325 us, 281 to 300 so.)
+// The prompts above now take 134 to 137 us (8-bit pages 154), 750 TFLOP/s, one of 8192 tokens 1058 TFLOP/s (967); 512 rows behind 8195 tokens and 260 behind 2665 in 8
+// bits, 64 / 8 heads, 211 us with the join, with a window of 2048 92 us.
 template <class C, int H> constexpr int KV_RING = 5 * KvLayout<C, H>::K_BYTES / 16 + (KvLayout<C, H>::Q8 ? 4 * 8 : 0);       // (bf16 at head dim 128: two of them are a unit's whole LDS)
 template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __forceinline__ void kv_many_rows(const Args& a, const KvItem& item, u32x4 (&mem)[KV_RING<C, H>]) {
     using A = BF16;
