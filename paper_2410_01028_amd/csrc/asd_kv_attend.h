@@ -403,7 +403,7 @@ template <class A, class C, int H, int NT, int SEES, int W, class Args> __device
             for (int j = 0; j < 4; ++j) {
                 v[j] += kv_odd_sum<C, H>(a.kv, seq, kvh, first_key, last_key, d + j, row_low, sinks, main0, main1);
                 if (TWO && u_begin < steps.first)
-                    v[j] += kv_odd_sum<C, H>(a.kv, first_seq, kvh, u_begin * UK, min(min(end, (SEES == KV_BOTH ? low : sinks) - 1), u_end * UK - 1), d + j, 0, 0, 0, SEES == KV_BOTH ? low / UK * UK : 0);
+                    v[j] += kv_odd_sum<C, H>(a.kv, first_seq, kvh, u_begin * UK, min(min(end, (SEES == KV_BOTH ? low : sinks) - 1), u_end * UK - 1), d + j, 0, 0, 0, (SEES == KV_BOTH ? low : sinks) / UK * UK);
             }
         }
         if (it.whole) {
@@ -489,7 +489,7 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(cons
 // workgroup alone 3300): the vector unit issues in 48 to 53 % of the busy cycles (8 bits 73 to 76), the matrix cores are at work in 33 to 38.  And by what each tile takes
 // once, about 10000 cycles in front (its item, the page table, queries, first fragments) and 4000 behind; a step with an edge takes 5000: the chunk's V^T is looked
 // through, and rows are masked on the side on which some see less.  (7600 with a mask of three comparisons per score and V^T written back always, behind a barrier of its own:
-// prompts of 4096, 3575, 2070 and 2547 tokens, window 1024: 325 us, 281 to 300 so.)
+// prompts of 4096, 3575, 2070 and 4062 tokens, window 1024: 325 us, 281 to 300 so.)
 // The prompts above now take 134 to 137 us (8-bit pages 154), 750 TFLOP/s, one of 8192 tokens 1058 TFLOP/s (967); 512 rows behind 8195 tokens and 260 behind 2665 in 8
 // bits, 64 / 8 heads, 211 us with the join, with a window of 2048 92 us.
 template <class C, int H> constexpr int KV_RING = 5 * KvLayout<C, H>::K_BYTES / 16 + (KvLayout<C, H>::Q8 ? 4 * 8 : 0);       // (bf16 at head dim 128: two of them are a unit's whole LDS)
@@ -518,7 +518,7 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
     const KvSteps steps = kv_steps<SEES>(a, low, 64);
     const int c0 = it.split * per, c_end = min((last + 64) / 64 - steps.skip, c0 + per);
     const int main0 = max((max(low_last, 0) + 63) / 64 - steps.skip, c0), main1 = min(c_end, (from + 1) / 64 - steps.skip);
-    const int first_main = SEES == KV_BOTH ? min(low / 64, c_end) : 0;                    // ... and the first ones (of the shared keys)
+    const int first_main = SEES == KV_BOTH ? min(low / 64, c_end) : SEES == KV_WINDOW && steps.first ? min(sinks / 64, c_end) : 0;      // ... and the first ones
     // The page of the chunk asked for next: the table's entries lie in the wave's lanes, those of the first steps apart from the others.  (Asked for ahead of the
     // queries: the first chunk's request waits for them alone.)
     constexpr bool TWO = SEES == KV_WINDOW || SEES == KV_BOTH;

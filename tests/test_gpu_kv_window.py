@@ -325,3 +325,28 @@ def test_an_engines_cache():
     pos = torch.arange(197, 200, device=DEV)
     check("f32", q, out, k.view(200, tiny.n_kv_heads, -1), v.view(200, tiny.n_kv_heads, -1), in_window(pos, 200, 50, 4), tiny.head_dim ** -0.5, "engine")
     eng.close()
+
+
+@pytest.mark.parametrize("kv", ["fp8", "bf16"])
+def test_many_first_tokens(kv):
+    """First tokens of many chunks, whole ones among them, with values that are not finite in all of them, in front of windows of many rows and of few; a page of them missing."""
+    news, total = [200, 3, 130], [3000, 2500, 2600]
+    p = Pool("bf16", kv, 40, 40, 64, 64, list(zip(news, total)), seed=31)
+    k, v = p.normal(sum(total), 40, 64), p.normal(sum(total), 40, 64)
+    for i, key in enumerate(list(range(5, 1500, 97)) + [3000 + x for x in range(7, 1400, 111)] + [5500 + 640, 5500 + 700, 5500 + 1279]):
+        v[key, i % 40, i % 64] = (math.nan, math.inf, -math.inf)[i % 3]
+    whole = p.batch(total, total)
+    p.cache.append(whole, None, k, v)
+    k, v = (torch.split(x, total) for x in p.cache.read(whole))
+    b, q = p.batch(news, total), p.normal(sum(news), 40, 64)
+    for window, sinks in ((300, 1280), (500, 1300), (64, 1279)):
+        out = p.cache.attend_window(b, q, window, sinks)
+        b.check()
+        check_window(p, news, total, q, out, k, v, 0.125, window, sinks)
+    p.d_table[2, 7] = -1
+    out = p.cache.attend_window(b, q, 300, 1280)
+    with pytest.raises(asd.AsdError, match="pages"):
+        b.check()
+    seen = in_window(torch.arange(2470, 2600, device=DEV), 2600, 300, 1280)
+    seen[:, 448:512] = False
+    check("bf16", q[203:], out[203:], k[2], v[2], seen, 0.125, "a page of the first tokens is missing")
