@@ -689,22 +689,33 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
                 }
             }
             u32x4 pf[NT][PS];
+            // The reference of a row's exponents need not be its maximum: it moves only when a weight would pass 2^8 (one branch for all column blocks, so that their chains run
+            // side by side)
+            float cm[NT];
+            bool past = false;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                float cm = sc[t][0][0];
+                cm[t] = sc[t][0][0];
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) cm = fmaxf(cm, sc[t][kt][j]);
-                cm = groups_max(cm);
-                // The reference of a row's exponents need not be its maximum: it moves only when a weight would pass 2^8
-                if (__any((cm - mx[t]) * a.c2 > 8.f)) {
-                    const float mn = fmaxf(mx[t], cm), alpha = mn == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mx[t] - mn) * a.c2);
+                    for (int j = 0; j < 4; ++j) cm[t] = fmaxf(cm[t], sc[t][kt][j]);
+                cm[t] = groups_max(cm[t]);
+                past = past || (cm[t] - mx[t]) * a.c2 > 8.f;
+            }
+            if (__any(past)) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    if (!__any((cm[t] - mx[t]) * a.c2 > 8.f)) continue;
+                    const float mn = fmaxf(mx[t], cm[t]), alpha = mn == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mx[t] - mn) * a.c2);
                     mx[t] = mn;
                     l[t] *= alpha;
 #pragma unroll
                     for (int ht = 0; ht < HT; ++ht) { o[t][ht][0] *= alpha; o[t][ht][1] *= alpha; o[t][ht][2] *= alpha; o[t][ht][3] *= alpha; }
                 }
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
                 const float off = mx[t] == -INFINITY ? 0.f : -mx[t] * a.c2;
                 float sum[2] = {0.f, 0.f};
 #pragma unroll
@@ -715,7 +726,7 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
                     if constexpr (L::Q8)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) e[j] *= vs[kt][j];
-                    pf[t][kt / 2][kt % 2 * 2] = bf16_pair(e[0], e[1]);      // as V is: see kv_attend_kernel
+                    pf[t][kt / 2][kt % 2 * 2] = bf16_pair(e[0], e[1]);      // as V is: see kv_few_rows
                     pf[t][kt / 2][kt % 2 * 2 + 1] = bf16_pair(e[2], e[3]);
                 }
                 l[t] += sum[0] + sum[1];
