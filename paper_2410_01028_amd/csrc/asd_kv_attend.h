@@ -146,6 +146,27 @@ template <class A, class C, int H, int NT, int SEES, int W, class Args> __device
     const KvSeq s = it.s;
     if (W > 1 && tid == 0) sh.odd = 0;
     const int rows = s.n * a.kv.group, base = s.len - s.n;
+    // last keys of the tile's last and first row; first keys of their windows (KV_OWN: of all rows)
+    const int last = SEES == KV_SHARED ? s.len - 1 : base + (min((tile + 1) * NT * 16, rows) - 1) / a.kv.group;
+    const int from = SEES == KV_SHARED ? s.len - 1 : base + tile * NT * 16 / a.kv.group;
+    int window = 0, sinks = 0, low = 0, low_last = 0;
+    if constexpr (SEES == KV_WINDOW) { window = a.window; sinks = a.sinks; low = from - window + 1; low_last = last - window + 1; }
+    if constexpr (SEES >= KV_OWN) low = low_last = s.low;
+    const KvSteps steps = kv_steps<SEES>(a, low, UK);
+    const int u_begin = split * per * UPC, u_end = min((last + UK) / UK - steps.skip, (split + 1) * per * UPC);      // (nothing to do where last is negative)
+    // The pages lie in the wave's lanes, those of the first steps apart from the others: a look-up in memory per unit would wait
+    // for every fragment asked for before it.  (Asked for ahead of the queries, which nothing waits for before the first scores.)
+    constexpr bool TWO = SEES == KV_WINDOW || SEES == KV_BOTH;
+    const int cpp = a.kv.page_tokens / 64, first_seq = SEES == KV_BOTH ? s.lead : seq, u_first = u_begin + w;
+    KvPages pages, first_pages;
+    if (u_first < u_end) {
+        if (TWO && u_first < steps.first) {
+            first_pages.load(a.kv, first_seq, u_first / UPC / cpp, lane);
+            if (u_end > steps.first) pages.load(a.kv, seq, (steps.first + steps.skip) / UPC / cpp, lane);
+        } else {
+            pages.load(a.kv, seq, steps.at(u_first) / UPC / cpp, lane);
+        }
+    }
     int pos[NT];                                        // last key of this lane's rows (-1: no such row, or none)
     u32x4 qf[NT][QS];
 #pragma unroll
@@ -157,14 +178,6 @@ template <class A, class C, int H, int NT, int SEES, int W, class Args> __device
 #pragma unroll
         for (int i = 0; i < QS; ++i) qf[t][i] = on ? *(const u32x4*)(qp + i / US * 4 * KK + g * KK + i % US * AE) : u32x4{0u, 0u, 0u, 0u};
     }
-    // last keys of the tile's last and first row; first keys of their windows (KV_OWN: of all rows)
-    const int last = SEES == KV_SHARED ? s.len - 1 : base + (min((tile + 1) * NT * 16, rows) - 1) / a.kv.group;
-    const int from = SEES == KV_SHARED ? s.len - 1 : base + tile * NT * 16 / a.kv.group;
-    int window = 0, sinks = 0, low = 0, low_last = 0;
-    if constexpr (SEES == KV_WINDOW) { window = a.window; sinks = a.sinks; low = from - window + 1; low_last = last - window + 1; }
-    if constexpr (SEES >= KV_OWN) low = low_last = s.low;
-    const KvSteps steps = kv_steps<SEES>(a, low, UK);
-    const int u_begin = split * per * UPC, u_end = min((last + UK) / UK - steps.skip, (split + 1) * per * UPC);      // (nothing to do where last is negative)
     auto hidden = [&](int key, int t, bool first) {      // first: of the first steps
         bool h = key > pos[t];
         if constexpr (SEES == KV_WINDOW) h = h || (key <= pos[t] - window && key >= sinks);
@@ -199,16 +212,6 @@ template <class A, class C, int H, int NT, int SEES, int W, class Args> __device
             for (int ks = 0; ks < KSU; ++ks) f.v[ht][ks] = __builtin_nontemporal_load((const u32x4*)(p + ((ht * KST + ks) * 64 + lane) * 16));
         if constexpr (L::Q8) f.ve = *(const u32x4*)(p + L::K_BYTES + 64 + 16 * g);
     };
-    // The pages lie in the wave's lanes, those of the first steps apart from the others: a look-up in memory per unit would wait
-    // for every fragment asked for before it
-    const int cpp = a.kv.page_tokens / 64;
-    constexpr bool TWO = SEES == KV_WINDOW || SEES == KV_BOTH;
-    const int first_seq = SEES == KV_BOTH ? s.lead : seq;
-    KvPages pages, first_pages;
-    if constexpr (TWO) if (u_begin < steps.first) {
-        if (u_end > steps.first) pages.load(a.kv, seq, (steps.first + steps.skip) / UPC / cpp, lane);
-        first_pages.load(a.kv, first_seq, u_begin / UPC / cpp, lane);
-    }
     // the first unit from u on that has a page, and where it is; one without counts as hidden
     const char *at_k = nullptr, *at_v = nullptr;
     auto next = [&](int u) {
@@ -491,7 +494,7 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(cons
 // through, and rows are masked on the side on which some see less.  (7600 with a mask of three comparisons per score and V^T written back always, behind a barrier of its own:
 // prompts of 4096, 3575, 2070 and 4062 tokens, window 1024: 325 us, 281 to 300 so.)
 // The prompts above now take 134 to 137 us (8-bit pages 154), 750 TFLOP/s, one of 8192 tokens 1058 TFLOP/s (967); 512 rows behind 8195 tokens and 260 behind 2665 in 8
-// bits, 64 / 8 heads, 211 us with the join, with a window of 2048 92 us.
+// bits, 64 / 8 heads, 209 us with the join, with a window of 2048 92 us.
 template <class C, int H> constexpr int KV_RING = 5 * KvLayout<C, H>::K_BYTES / 16 + (KvLayout<C, H>::Q8 ? 4 * 8 : 0);       // (bf16 at head dim 128: two of them are a unit's whole LDS)
 template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __forceinline__ void kv_many_rows(const Args& a, const KvItem& item, u32x4 (&mem)[KV_RING<C, H>]) {
     using A = BF16;
