@@ -655,7 +655,10 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) vs[kt][j] = q8_scale((ve[kt] >> (8 * j)) & 255u);
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t e = (ve[kt] >> (8 * j)) & 255u;
+                        vs[kt][j] = q8_scale(edge ? min(e, 254u) : e);      // (a key that no row sees may have any scale: its weight, 0, times a finite one is 0; written ones are below)
+                    }
             if constexpr (edge) {
                 // Masks by the places of a row's first and last key in the chunk, and only on the side on which some row of the wave does not see all of it (a lane's
                 // keys: those of lane group 0, at constants, and `at` on)
@@ -681,14 +684,6 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
 #pragma unroll
                             for (int j = 0; j < 4; ++j) if ((uint32_t)(score_key<C>(kt, j) - after) < gap) sc[t][kt][j] = -INFINITY;
                     }
-                }
-                if constexpr (L::Q8) {                   // (an unwritten scale may be anything)
-                    const int n_keys = last_key(c) - r * 64, cut = first_key(c) - r * 64;
-                    if (n_keys < 64 || cut > 0)
-#pragma unroll
-                        for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) if (score_key<C>(kt, 4 * g + j) >= n_keys || (SEES >= KV_OWN && score_key<C>(kt, 4 * g + j) < cut)) vs[kt][j] = 0.f;
                 }
             }
             u32x4 pf[NT][PS];
