@@ -211,22 +211,24 @@ struct KvGroupLanes {
 // The sequences, with the first key of their own (v.low): 0 where a sequence is in no group, or has a new row that does not lie behind the shared tokens, or
 // where the group's first sequence does not hold them
 struct KvOwnLanes : KvLanes {
-    KvGroupLanes groups;                                // (the first 64)
-    __device__ __forceinline__ KvOwnLanes(const KvGroupLanes& g) : groups(g) {}
+    KvGroupLanes groups;                                // 64 of them, from g0 on
+    int g0 = 0;
+    __device__ __forceinline__ KvOwnLanes(const KvGroupLanes& first) : groups(first) {}
     __device__ __forceinline__ void load(const KvArgs& kv, int s0, int lane, bool check) {
         KvLanes::load(kv, s0, lane, check);
         const int s = s0 + lane, n = groups.entries(kv);
-        KvGroupLanes g = groups;
-        for (int g0 = 0;;) {
+        for (;;) {
             int at = 0;                                 // the last one that begins at s or in front of it
             if (n > 1)
 #pragma unroll
-                for (int step = 32; step > 0; step >>= 1) if (__shfl(g.f0, at + step) <= s) at += step;
-            const int f0 = __shfl(g.f0, at), f1 = __shfl(g.f1, at), r0 = __shfl(g.v.r0, at), rows = __shfl(g.v.n, at), len = __shfl(g.v.len, at);
+                for (int step = 32; step > 0; step >>= 1) if (__shfl(groups.f0, at + step) <= s) at += step;
+            const int f0 = __shfl(groups.f0, at), f1 = __shfl(groups.f1, at), r0 = __shfl(groups.v.r0, at), rows = __shfl(groups.v.n, at), len = __shfl(groups.v.len, at);
             if (s >= f0 && s < f1 && v.n > 0 && v.r0 >= r0 && v.r0 + v.n <= r0 + rows && v.len - v.n >= len) { v.low = len; v.lead = f0; }
+            // Later groups begin at the end of these or behind it: where that is behind the sequences at hand, they wait for the next ones, so that a walk over all
+            // sequences is one over all groups too, whatever there are of either.
+            if (groups.top_f > s0 + 63 || g0 + 64 >= n) break;
             g0 += 64;
-            if (g0 >= n) break;
-            g.load(kv, g0, lane, false);
+            groups.load(kv, g0, lane, false);
         }
     }
 };
