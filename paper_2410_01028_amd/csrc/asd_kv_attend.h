@@ -497,6 +497,7 @@ __global__ __launch_bounds__(256, A::KE == 4 ? 1 : 2) void kv_attend_kernel(cons
 // bits, 64 / 8 heads, 209 us with the join, with a window of 2048 92 us.
 template <class C, int H> constexpr int KV_RING = 5 * KvLayout<C, H>::K_BYTES / 16 + (KvLayout<C, H>::Q8 ? 4 * 8 : 0);       // (bf16 at head dim 128: two of them are a unit's whole LDS)
 template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __forceinline__ void kv_many_rows(const Args& a, const KvItem& item, u32x4 (&mem)[KV_RING<C, H>]) {
+    static_assert(SEES != KV_OWN, "own keys behind shared ones, apart from them, are kv_few_rows'");
     using A = BF16;
     using L = KvLayout<C, H>;
     constexpr int AE = A::KE, KK = L::KK, HP = L::HP, US = KK / AE, QS = HP * US, HT = L::HT, KST = L::KST, VS = L::KV / AE, PS = KST * VS;
@@ -511,12 +512,12 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
     auto reach = [&](int row) { return SEES == KV_SHARED ? s.len - 1 : base + row / a.kv.group; };
     const int from = reach(tile * RT * 16), last = reach(min((tile + 1) * 16 * RT, rows) - 1);                 // ... of the workgroup's first and last row
     const int my_from = reach(row0), my_last = row0 < rows ? reach(min(row0 + 16 * NT, rows) - 1) : -1;           // ... of this wave's
-    int window = 0, sinks = 0, low = 0, low_last = 0, my_low = 0, my_low_last = 0;                               // first keys of those rows' windows (KV_OWN: of all rows)
+    int window = 0, sinks = 0, low = 0, low_last = 0, my_low = 0, my_low_last = 0;                               // first keys of those rows' windows (KV_BOTH: of all rows)
     if constexpr (SEES == KV_WINDOW) {
         window = a.window; sinks = a.sinks;
         low = from - window + 1; low_last = last - window + 1; my_low = my_from - window + 1; my_low_last = my_last - window + 1;
     }
-    if constexpr (SEES >= KV_OWN) low = low_last = my_low = my_low_last = s.low;
+    if constexpr (SEES == KV_BOTH) low = low_last = my_low = my_low_last = s.low;
     // Steps of one chunk: those of the workgroup's run, those that all its rows see whole
     const KvSteps steps = kv_steps<SEES>(a, low, 64);
     const int c0 = it.split * per, c_end = min((last + 64) / 64 - steps.skip, c0 + per);
@@ -605,7 +606,7 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
         };
         auto ask = [&]() { ask_v(src, n_bytes); ask_k(); };      // V^T of the next chunk, K of the one behind it
         // the written keys that belong to step c: first_key .. last_key - 1
-        auto first_key = [&](int c) { return SEES == KV_OWN || (SEES == KV_BOTH && c >= steps.first) ? low : 0; };
+        auto first_key = [&](int c) { return SEES == KV_BOTH && c >= steps.first ? low : 0; };
         auto last_key = [&](int c) { return SEES == KV_BOTH && c < steps.first ? low : s.len; };
         auto cleaned = [&]() {
             asm volatile("" ::: "memory");
@@ -674,7 +675,7 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
                             for (int j = 0; j < 4; ++j) if (score_key<C>(kt, j) > most) sc[t][kt][j] = -INFINITY;
                     }
                 }
-                if constexpr (SEES == KV_WINDOW || SEES >= KV_OWN) if (!first && r * 64 < my_low_last) {
+                if constexpr (SEES == KV_WINDOW || SEES == KV_BOTH) if (!first && r * 64 < my_low_last) {
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
                         const int least = (SEES == KV_WINDOW ? pos[t] - window + 1 : low) - at, after = SEES == KV_WINDOW ? max(sinks - at, -64) : -64;      // (hidden: after .. least - 1)
@@ -773,7 +774,7 @@ template <class C, int H, int NT, int NW, int SEES, class Args> __device__ __for
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
                         f[q][x] &= kv_kept<C>(n_keys, (w + NW * q) % KST, g, x);
-                        if constexpr (SEES >= KV_OWN) f[q][x] &= ~kv_kept<C>(cut, (w + NW * q) % KST, g, x);
+                        if constexpr (SEES == KV_BOTH) f[q][x] &= ~kv_kept<C>(cut, (w + NW * q) % KST, g, x);
                     }
 #pragma unroll
             for (int q = 0; q < LH; ++q)
