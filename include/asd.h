@@ -482,7 +482,10 @@ int asd_kv_attend_window(const asd_kv_shape* s, const asd_kv_batch* b, int32_t w
 
 /*
  * The same for groups of sequences that begin with the same tokens (samples of one prompt, drafts of one conversation, requests behind one system
- * prompt): these keys are read once for all rows of a group.  Group g is the sequences group_start[g] .. group_start[g+1]-1; sequences may be in no
+ * prompt).  Where sequences have few rows each (64 rows x heads of a KV head on average at most) and reading everything for each of them would be much, by the batch's
+ * bounds, these keys are read once for all rows of a group; else each sequence's tiles walk them.  It is worth it where much is shared beside what is a sequence's own: where
+ * that is little, where groups are many and small, and for many rows to a sequence, asd_kv_attend over a page table that holds the common pages (which then have to be whole)
+ * is about as fast, and in the first two cases up to a third faster.  Group g is the sequences group_start[g] .. group_start[g+1]-1; sequences may be in no
  * group.  The keys 0 .. shared_len[g]-1 of its sequences are those of its FIRST sequence, read through that one's page table; the keys behind
  * them are each sequence's own, read through its own.  So a sequence can leave a common beginning anywhere, inside a page too: its
  * page there holds its own tokens only, and nothing is copied.  A sequence is read through its own table altogether where it is in no group, where some new row

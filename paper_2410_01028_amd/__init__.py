@@ -709,8 +709,9 @@ class KVCache(_Fixed):
         return int(self._lib.asd_kv_attend_window_workspace(self._s, ctypes.addressof(bound), window, sinks))
 
     def attend_shared(self, batch: KVBatch, groups: KVGroups, q, out=None, scale: float | None = None, workspace=None):
-        """attend() where groups of sequences begin with the same tokens (asd_kv_attend_shared): those are read once for all rows of a group, through the
-        page table of its first sequence, the others through each sequence's own.  workspace: attend_shared_workspace(batch, groups) bytes."""
+        """attend() where groups of sequences begin with the same tokens (asd_kv_attend_shared): those are read through the page table of the group's
+        first sequence, once for all its rows where the sequences have few rows each and enough to read, the others through each sequence's own.  Where little is
+        shared beside a sequence's own tokens, attend() over the common pages is as fast or faster.  workspace: attend_shared_workspace(batch, groups) bytes."""
         if groups.device != self.device:
             raise AsdError(E_INVAL, "the groups are on another device than the pages")
         return self._attend(self._lib.asd_kv_attend_shared, self._lib.asd_kv_attend_shared_workspace, batch, (groups._at,), (self._key, groups.n_groups), q, out, scale, workspace)

@@ -59,9 +59,11 @@ struct SharedPlan {
 SharedPlan shared_plan(const asd_kv_shape* s, const asd_kv_batch* b, const asd_kv_groups* g) {
     SharedPlan p{};
     const int64_t chunks = (kv_args(s, b).cap + 63) / 64, group = s->n_heads / s->n_kv_heads;
-    // Apart costs a second launch, and is worth it where the sequences' tiles are not full by themselves (64 rows on average) and, walking both, would read much more than
-    // there is (64 / 8 heads, 8 bits, one token of 64 sequences behind 4000 shared ones: 32 us, walking both 62; of 4 behind 1000: 14.7 and 13.1; 130 rows of 24
-    // sequences: 309 and 272).
+    // Apart every row's parts are joined, and own keys are items of a wave each.  Worth it where the sequences' tiles are not full by themselves (64 rows on average) and, walking both, would
+    // read much more than there is (64 / 8 heads, 8 bits, one token of 64 sequences behind 4000 shared ones and up to 300 own: 36 us, walking both 63; of 4 behind 1000: 14.7 and 13.1;
+    // 130 rows of 24 sequences: 309 and 272).  The bounds do not say what is shared.  Where it is little beside the own keys the two are nearly even, and causal attention over tables that
+    // hold the common pages is ahead: 50, 500, 2000 shared tokens, one token of 16 sequences with up to 4000 of their own 30, 30, 30 us, walking both 27, 28, 38, causal 27, 27, 34; of 64
+    // with up to 8000 116, 115, 128 and 116, 115, 123, causal 106, 109, 117.  1024 sequences with up to 200 of their own in 256 groups of 1000: 485 and 550, causal 332 (in 32 groups 292, 479, 302).
     const int64_t cap = kv_args(s, b).cap, read = b->n_seqs * cap * (int64_t)(asd_kv_page_bytes(s) / s->page_tokens);
     p.apart = b->n_seqs / 2 >= g->n_groups && b->n_rows * group <= 64 * (int64_t)b->n_seqs && ((cap >= 512 && read >= 40 << 20) || read >= 256 << 20);
     if (!p.apart) {
